@@ -361,12 +361,121 @@ seg_status seg_layer_bwd(const seg_layout *L, const seg_sizes *sz, const seg_lay
                          size_t ws_bytes, hipStream_t stream);
 
 /*
+ * Rotary positions on three axes (time, height, width), as vision-language
+ * models place screenshots and clips.  The paper does not spell them out; the
+ * rule is the usual one: along a segment a counter n starts at 0; the rows of a
+ * prompt or text run have position (n, n, n), n counting on by one a row; a
+ * screenshot of t frames of h x w patches (t h w = its img_len, frame by frame,
+ * row by row) that opens at n has patch (f, y, x) at (n + e f, n + y, n + x), e
+ * its time step, and n continues behind its longest axis: n += max(e (t - 1) +
+ * 1, h, w).  Screenshots that a segment dropped take no positions.
+ *   p, sz: as for seg_build_layout.  grid: host [num_steps * 4], (t, h, w, e) of
+ *   each step's screenshot, read during the call (a step without a screenshot,
+ *   img_len = 0, has none; NULL where no step has one).
+ *   pos [3, packed_tokens] int32: time, height and width; -1 in padding rows.
+ * The run table is computed on the host and uploaded to `ws` (at least
+ * seg_mrope_positions_workspace_bytes(p) bytes); the call waits on `stream`
+ * once after that small upload, as seg_build_layout does.  Errors: SEG_ERR_ARG
+ * (invalid problem, or a grid that is not its screenshot's tokens),
+ * SEG_ERR_CAPACITY (a position past 2^31 - 1), SEG_ERR_WORKSPACE.
+ */
+size_t seg_mrope_positions_workspace_bytes(const seg_problem *p); /* 0: invalid problem */
+seg_status seg_mrope_positions(const seg_problem *p, const seg_sizes *sz, const int32_t *grid,
+                               int32_t *pos, void *ws, size_t ws_bytes, hipStream_t stream);
+
+typedef struct {
+  int32_t sections[3]; /* pairs that turn with time, height and width; they sum to d / 2 */
+  float base;          /* > 1 */
+} seg_mrope_cfg;
+
+/*
+ * Rotation of q [rows, hq, d] and k [rows, hkv, d] (hkv = 0: none, and k and
+ * k_out unused) by positions pos [3, rows]: the pair (i, i + d/2) of a head
+ * turns by pos[axis(i)][row] * base^(-2i/d), where the first sections[0] pairs
+ * are on axis 0, the next sections[1] on axis 1 and the last on axis 2; (d/2,
+ * 0, 0) is the one-dimensional embedding of seg_layer_fwd.  Angles are formed
+ * in fp64; fp32 tensors are rotated in fp32.  ldq, ldk, ldqo, ldko: elements
+ * between rows (at least heads * d), so q and k may be parts of one
+ * projection's rows; an output may be its input (same pointer and stride), and
+ * must not overlap an input otherwise.  Rows with a negative position on any
+ * axis are padding: seg_mrope_fwd copies them, and seg_mrope_bwd, which turns
+ * dq and dk back (the transpose: gradients of the unrotated q and k), writes
+ * zeros there.  Supported: d a multiple of 16 up to 256, rows on 16-byte
+ * boundaries (SEG_ERR_UNSUPPORTED otherwise), SEG_BF16 and SEG_F32.
+ */
+seg_status seg_mrope_fwd(int64_t rows, seg_dtype dt, const seg_mrope_cfg *cfg, int32_t hq,
+                         int32_t hkv, int32_t d, const int32_t *pos, const void *q, int64_t ldq,
+                         const void *k, int64_t ldk, void *q_out, int64_t ldqo, void *k_out,
+                         int64_t ldko, hipStream_t stream);
+seg_status seg_mrope_bwd(int64_t rows, seg_dtype dt, const seg_mrope_cfg *cfg, int32_t hq,
+                         int32_t hkv, int32_t d, const int32_t *pos, const void *dq, int64_t ldq,
+                         const void *dk, int64_t ldk, void *dq_out, int64_t ldqo, void *dk_out,
+                         int64_t ldko, hipStream_t stream);
+
+/*
+ * Activations in 8 bits, for what a backward pass reads again.  Blocks of 32
+ * consecutive columns of a row (a row's last block may be shorter) share one
+ * power of two: value = code * 2^(exp - 127), exp the least byte with max|x| <=
+ * 127 * 2^(exp - 127); code = the nearest integer (ties to even).  So a value
+ * is off by at most half a step, max|x| / 127 in its block, and zeros stay
+ * zero (but codes stop at 63 in blocks of exp = 249, where 64 steps are 2^128:
+ * finite values stay finite).  A block that holds an infinity or a NaN has exp
+ * = 255 and reads as NaN throughout.  Values have at most 8 significant bits: bf16 holds them
+ * exactly.
+ */
+typedef struct {
+  int8_t *code;  /* [rows, cols] */
+  uint8_t *exp;  /* [rows, ceil(cols / 32)] */
+} seg_act8;
+
+/* x [rows, cols] (dtype dt, ldx >= cols elements between rows) to 8 bits and
+ * back.  Any cols >= 1; 16-byte accesses where cols is a multiple of 8 and x's
+ * rows (codes: 8-byte) are aligned. */
+seg_status seg_act_pack(int64_t rows, int32_t cols, seg_dtype dt, const void *x, int64_t ldx,
+                        const seg_act8 *out, hipStream_t stream);
+seg_status seg_act_unpack(int64_t rows, int32_t cols, seg_dtype dt, const seg_act8 *in, void *x,
+                          int64_t ldx, hipStream_t stream);
+
+/*
+ * Gated feed-forward block (both projections, activation and product) on any
+ * rows: m = silu(g) * u, g = x wg^T, u = x wu^T.  bf16, fp32 accumulation, one
+ * rounding (of m).
+ *   x [rows, hidden] (ldx elements between rows, a multiple of 8); wg, wu
+ *   [inter, hidden]; m [rows, inter].  g8 and u8 (both or neither NULL): the
+ *   values g and u [rows, inter] in 8 bits, formed from the fp32 sums.
+ * Supported: hidden and inter multiples of 8, all sizes up to 2^20, tensors on
+ * 16-byte boundaries and codes on 8-byte ones (SEG_ERR_UNSUPPORTED otherwise).
+ */
+seg_status seg_glu_fwd(int32_t rows, int32_t hidden, int32_t inter, const void *x, int64_t ldx,
+                       const void *wg, const void *wu, void *m, const seg_act8 *g8,
+                       const seg_act8 *u8, hipStream_t stream);
+
+/* Workspace of seg_glu_bwd; kept: whether it is given g8 and u8. */
+size_t seg_glu_workspace_bytes(int32_t rows, int32_t hidden, int32_t inter, int32_t kept);
+
+/*
+ * Backward of seg_glu_fwd: given dm [rows, inter], the gradients of sum(m * dm),
+ * with g and u read from the forward's 8-bit arrays, or (g8 and u8 NULL)
+ * computed from x again:
+ *   dg = dm u silu'(g), du = dm silu(g); dx = dg wg + du wu [rows, hidden];
+ *   dwg = dg^T x, dwu = du^T x [inter, hidden] (dtype dw_dt; overwritten).
+ * m [rows, inter] or NULL: silu(g) * u again, which the weight gradient of the
+ * projection behind the block reads.  dg and du are rounded to bf16 for the
+ * products.
+ */
+seg_status seg_glu_bwd(int32_t rows, int32_t hidden, int32_t inter, const void *x, int64_t ldx,
+                       const void *wg, const void *wu, const seg_act8 *g8, const seg_act8 *u8,
+                       const void *dm, void *m, void *dx, seg_dtype dw_dt, void *dwg, void *dwu,
+                       void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
  * Kernel timing.  While enabled, every kernel the library launches is
  * bracketed by HIP events recorded on its launch stream.  seg_profile_read sums
  * the device time of all recorded launches of one kernel (names: "layout",
  * "attn_prep", "attn_fwd", "attn_delta" (fp32 inputs only: with bf16 inputs
  * the dQ kernel forms Delta itself), "attn_bwd_dkdv", "attn_bwd_dq", "logits", "row_loss", "dz", "lp_prep", "dh", "dw", and for the layer
- * "ly_norm", "ly_rope", "ly_proj", "ly_mlp", "ly_wgrad", "ly_misc"), waiting for them to
+ * "ly_norm", "ly_rope", "ly_proj", "ly_mlp", "ly_wgrad", "ly_misc"; "mrope_pos", "mrope", "act_pack",
+ * "act_unpack", "glu_fwd", "glu_act", "glu_dx", "glu_dw"), waiting for them to
  * finish; seg_profile_reset forgets the records.  Timing adds two event
  * records per launch and is off by default.  These three calls are the one
  * place with process-wide state (an atomic enable flag and a mutex-guarded

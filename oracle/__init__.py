@@ -15,5 +15,8 @@ attention  masked GQA softmax attention forward and backward
 loss       action-token log-prob, clipped policy-ratio loss, gradients
 layer      decoder layer (RMSNorm, rotary GQA attention, SwiGLU) around the
            segmented attention, forward and backward
+mrope      rotary positions on three axes: positions of a segment, rotation
+act8       activations in 8 bits (blocks of 32 columns, a power of two each)
+glu        gated feed-forward block, forward and backward
 """
-from . import layout, attention, loss, layer  # noqa: F401
+from . import layout, attention, loss, layer, mrope, act8, glu  # noqa: F401

@@ -25,7 +25,10 @@ SEG_ATTN_BWD_SCRATCH_BYTES = 64 << 20
 # every symbol include/seg.h declares
 EXPORTS = ["seg_layout_query", "seg_build_layout", "seg_attn_workspace_bytes", "seg_attn_fwd",
            "seg_attn_bwd", "seg_attn_bwd_noalloc", "seg_logprob_workspace_bytes", "seg_logprob_loss",
-           "seg_layer_workspace_bytes", "seg_layer_fwd", "seg_layer_bwd", "seg_profile_enable",
+           "seg_layer_workspace_bytes", "seg_layer_fwd", "seg_layer_bwd",
+           "seg_mrope_positions_workspace_bytes", "seg_mrope_positions", "seg_mrope_fwd",
+           "seg_mrope_bwd", "seg_act_pack", "seg_act_unpack", "seg_glu_fwd",
+           "seg_glu_workspace_bytes", "seg_glu_bwd", "seg_profile_enable",
            "seg_profile_reset", "seg_profile_read", "seg_last_error"]
 
 P32 = ctypes.POINTER(ctypes.c_int32)
@@ -94,6 +97,14 @@ class SegLayerGrads(ctypes.Structure):
     _fields_ = [(n, VP) for n in LAYER_WEIGHTS]
 
 
+class SegMropeCfg(ctypes.Structure):
+    _fields_ = [("sections", ctypes.c_int32 * 3), ("base", ctypes.c_float)]
+
+
+class SegAct8(ctypes.Structure):
+    _fields_ = [("code", VP), ("exp", VP)]
+
+
 class SegError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -158,6 +169,27 @@ def lib() -> ctypes.CDLL:
                                     ctypes.POINTER(SegLayerCfg), ctypes.POINTER(SegLayerWeights),
                                     VP, ctypes.POINTER(SegLayerSaved), VP, VP,
                                     ctypes.POINTER(SegLayerGrads), VP, ctypes.c_size_t, VP]
+        i32, i64, size, dtype, act8 = (ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_int,
+                                       ctypes.POINTER(SegAct8))
+        L.seg_mrope_positions_workspace_bytes.restype = size
+        L.seg_mrope_positions_workspace_bytes.argtypes = [ctypes.POINTER(SegProblem)]
+        L.seg_mrope_positions.restype = ctypes.c_int
+        L.seg_mrope_positions.argtypes = [ctypes.POINTER(SegProblem), ctypes.POINTER(SegSizes), VP, VP,
+                                          VP, size, VP]
+        for f in (L.seg_mrope_fwd, L.seg_mrope_bwd):
+            f.restype = ctypes.c_int
+            f.argtypes = [i64, dtype, ctypes.POINTER(SegMropeCfg), i32, i32, i32, VP, VP, i64, VP, i64,
+                          VP, i64, VP, i64, VP]
+        L.seg_act_pack.restype = L.seg_act_unpack.restype = ctypes.c_int
+        L.seg_act_pack.argtypes = [i64, i32, dtype, VP, i64, act8, VP]
+        L.seg_act_unpack.argtypes = [i64, i32, dtype, act8, VP, i64, VP]
+        L.seg_glu_fwd.restype = ctypes.c_int
+        L.seg_glu_fwd.argtypes = [i32, i32, i32, VP, i64, VP, VP, VP, act8, act8, VP]
+        L.seg_glu_workspace_bytes.restype = size
+        L.seg_glu_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.seg_glu_bwd.restype = ctypes.c_int
+        L.seg_glu_bwd.argtypes = [i32, i32, i32, VP, i64, VP, VP, act8, act8, VP, VP, VP, dtype, VP, VP,
+                                  VP, size, VP]
         L.seg_profile_enable.restype = None
         L.seg_profile_enable.argtypes = [ctypes.c_int32]
         L.seg_profile_reset.restype = None

@@ -1,0 +1,74 @@
+// Activations in 8 bits: signed codes in blocks of 32 consecutive columns of a
+// row (the last block of a row may be shorter), with one power of two a block:
+// value = code 2^s, s least with max|x| <= 127 2^s and s >= -127, stored as the
+// byte s + 127 (255: the block holds an infinity or a NaN, and reads as NaN; in
+// the last one that fp32 reaches, codes stop at 63 and finite values stay finite).
+// A power of two makes division and product exact, so the only rounding is that
+// of x 2^-s to the nearest integer (ties to even), and a value has at most 8
+// significant bits: bf16 holds it exactly, and so do the matrix products that
+// read it.
+#pragma once
+
+#include "common.h"
+
+namespace seg {
+namespace act8 {
+
+constexpr int BLOCK = 32;
+constexpr int LAST = 249;  // the byte of fp32's largest numbers: 64 steps are 2^128, codes stop at 63
+constexpr int NOT_FINITE = 255;
+
+inline long blocks_of(long cols) { return (cols + BLOCK - 1) / BLOCK; }
+
+// Magnitudes compare as their bits do, infinities and NaN above all numbers.
+__device__ __forceinline__ unsigned mag(float x) { return __builtin_bit_cast(unsigned, x) & 0x7fffffffu; }
+
+// exponent byte of a block whose largest magnitude has the bits a: with a =
+// 1.f 2^(e - 127), 127 2^s = 1.984375 2^(s + 6), so s + 127 is e - 6, or e - 5
+// where 1.f is above 1.984375
+__device__ __forceinline__ int exp_byte(unsigned a) {
+  if (a >= 0x7f800000u) return NOT_FINITE;
+  const int b = (int)(a >> 23) - 6 + ((a & 0x7fffffu) > 0x7e0000u ? 1 : 0);
+  return b < 0 ? 0 : b;
+}
+
+// 2^-s of a finite block (byte at most 249)
+__device__ __forceinline__ float inv_scale(int byte) {
+  return __builtin_bit_cast(float, (unsigned)(254 - byte) << 23);
+}
+
+// 2^s (2^-127 is a subnormal number), NaN for a block that is not finite
+__device__ __forceinline__ float scale(int byte) {
+  const unsigned b = byte == 0 ? 1u << 22 : (unsigned)byte << 23;
+  return __builtin_bit_cast(float, byte == NOT_FINITE ? 0x7fc00000u : b);
+}
+
+// codes of four values of a block with exponent byte `byte`, lowest byte first
+// (zeros where the block is not finite)
+__device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, int byte) {
+  if (byte >= LAST) {  // rare: the largest numbers of fp32
+    if (byte == NOT_FINITE) return 0u;
+    const float top = 63.f * 0x1p122f;
+    a = fminf(fmaxf(a, -top), top);
+    b = fminf(fmaxf(b, -top), top);
+    c = fminf(fmaxf(c, -top), top);
+    d = fminf(fmaxf(d, -top), top);
+  }
+  const float inv = inv_scale(byte);
+  const int i = (int)rintf(a * inv), j = (int)rintf(b * inv), k = (int)rintf(c * inv), l = (int)rintf(d * inv);
+  return (unsigned)(i & 255) | (unsigned)(j & 255) << 8 | (unsigned)(k & 255) << 16 | (unsigned)(l & 255) << 24;
+}
+
+// value j of four codes
+__device__ __forceinline__ float value(unsigned codes, int j, float scale) {
+  return (float)((int)(codes << (24 - 8 * j)) >> 24) * scale;
+}
+
+// Eight codes of a chunk of columns, their block's scale with them.
+__device__ __forceinline__ void values8(const unsigned (&w)[2], float sc, float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = value(w[j / 4], j & 3, sc);
+}
+
+}  // namespace act8
+}  // namespace seg

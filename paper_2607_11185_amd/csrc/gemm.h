@@ -239,8 +239,8 @@ struct Loader {
   const unsigned short *x;  // T: column c0 of row 0
   long ld;
   int width;                // T: columns of the last row, whole 16-byte chunks
-  gemm_i32x4 rs;
-  int voff[2], kchunk, stride, add;
+  gemm_i32x4 rs, rs2;       // rs2: of the odd loads of a pair
+  int voff[2], kchunk, stride, add;  // stride: between loads two apart
 
   template <bool T, int R>
   __device__ __forceinline__ void init(const unsigned short *X, long ld_, int row0, int rows, int w,
@@ -253,7 +253,7 @@ struct Loader {
       // chunk: ld is a multiple of 8 and every k row holds ld elements, so
       // that end stays inside the matrix
       width = (rows - row0 + 7) & ~7;
-      stride = (int)(4 * RPL * ld * 2);
+      stride = (int)(8 * RPL * ld * 2);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {  // load j: k rows RPL (w + 4 j) ..; the swizzle repeats with j + 2
         const int r = RPL * (w + 4 * j) + lane / CPR;
@@ -264,10 +264,26 @@ struct Loader {
       rs = gemm_desc(X + (long)row0 * ld, (long)(rows - row0 < R ? rows - row0 : R) * ld * 2);
       const int r = w * 8 + (lane >> 3);  // load j: rows 8 (w + 4 j) .. + 7
       kchunk = (lane & 7) ^ ((r >> 1) & 7);
-      stride = (int)(32 * ld * 2);
+      stride = (int)(64 * ld * 2);
       voff[0] = (int)(r * ld * 2) + kchunk * 16;
-      voff[1] = voff[0] + stride;
+      voff[1] = voff[0] + stride / 2;
+      rs2 = rs;
     }
+  }
+  // B of a pair: blocks of 32 rows of X and of Y (k-contiguous, row stride ld_) in turn,
+  // from row f0 of both to `rows`.  Load j reads rows 32 (j / 2) + 8 w .. + 7 of X where j
+  // is even, of Y where it is odd; rows past the end read as zeros.
+  template <int R>
+  __device__ __forceinline__ void init_pair(const unsigned short *X, const unsigned short *Y, long ld_,
+                                            int f0, int rows, int w, int lane) {
+    ld = ld_;
+    const long bytes = (long)(rows - f0 < R / 2 ? rows - f0 : R / 2) * ld * 2;
+    rs = gemm_desc(X + (long)f0 * ld, bytes);
+    rs2 = gemm_desc(Y + (long)f0 * ld, bytes);
+    const int r = w * 8 + (lane >> 3);
+    kchunk = (lane & 7) ^ ((r >> 1) & 7);
+    stride = (int)(32 * ld * 2);
+    voff[0] = voff[1] = (int)(r * ld * 2) + kchunk * 16;
   }
   // step at k0 of K: what lies at or past K (the whole step where k0 >= K)
   // reads as zero
@@ -281,8 +297,9 @@ struct Loader {
       add = k0 + kchunk * 8 < K ? k0 * 2 : 0x40000000;
     }
   }
+  template <bool PAIR>
   __device__ __forceinline__ void load(unsigned dst, int j, int w) const {
-    dma16(dst + (w + 4 * j) * 1024, voff[j & 1] + add + (j >> 1) * 2 * stride, rs);
+    dma16(dst + (w + 4 * j) * 1024, voff[j & 1] + add + (j >> 1) * stride, PAIR && (j & 1) ? rs2 : rs);
   }
 };
 
@@ -367,6 +384,16 @@ struct Problems {
   int splits, part;
 };
 
+// Whether an epilogue asks for a pair as B (kPair): the product's columns are blocks
+// of 32 rows of B and of its `second` matrix in turn (`features` rows each, N = 64
+// ceil(features / 32) columns), both k-contiguous.  So both projections of a gated
+// block come out of one product, and a 64-column wave tile holds both values of 32
+// features; no interleaved copy of the weights is made.
+template <class E, class = void>
+struct is_pair : std::false_type {};
+template <class E>
+struct is_pair<E, std::enable_if_t<E::kPair>> : std::true_type {};
+
 #define GEMM_FENCE() asm volatile("" ::: "memory")
 
 // Grid: 8 * ceil(tiles * splits / 8) x 512.
@@ -416,8 +443,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_gemm(const Problems<Epi, NP, NS>
   const int wm = grp, wn = wave & 3, w4 = wave & 3;
 
   Loader ldr;
+  constexpr bool PAIR = is_pair<Epi>::value;
+  static_assert(!PAIR || (!TA && !TB && NS == 1), "a pair is read k-contiguous, in one sum");
   auto open = [&](int s) __attribute__((always_inline)) {  // the group's operand of product s
     if (grp == 0) ldr.init<TA, BM>(pA[s], la[s], m0, M, w4, lane);
+    else if constexpr (PAIR) ldr.init_pair<BN>(pB[s], ep.second, lb[s], n0 / 2, ep.features, w4, lane);
     else ldr.init<TB, BN>(pB[s], lb[s], n0, N, w4, lane);
   };
   Frag<TA, BM, 2 * TM> fA;
@@ -473,7 +503,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_gemm(const Problems<Epi, NP, NS>
   constexpr int LA = BM / 32, LB = BN / 32;  // loads per wave of an A and of a B step
   const unsigned ring = base + (grp == 0 ? 0 : LDS_B);
   auto load = [&](int slot, int j) __attribute__((always_inline)) {
-    if (LA == LB || j < LA || grp == 1) ldr.load(ring + slot, j, w4);
+    if (LA == LB || j < LA || grp == 1) ldr.load<PAIR>(ring + slot, j, w4);
   };
   prep();
 #pragma unroll

@@ -546,10 +546,140 @@ __global__ void __launch_bounds__(256) k_build(const BuildArgs a) {
   if (b == 0 && tid == 0) *a.out.tile_nnz = a.qptr[a.G];
 }
 
+// ------------------------------------------------- positions on three axes
+
+// One run of tokens: its first packed row, its length, the position where it
+// starts, and the step whose screenshot it is (-1: a prompt or text).
+struct PosRun {
+  int32_t row, len, start, step;
+};
+
+// frames, rows and columns of patches of a step's screenshot, time step
+struct Grid {
+  int32_t t, h, w, e;
+};
+
+struct PosWs {
+  size_t run, grid, total;
+};
+
+PosWs pos_ws_layout(size_t pieces, size_t steps) {
+  PosWs w{};
+  w.run = 0;
+  w.grid = align_up(sizeof(PosRun) * std::max<size_t>(1, pieces));
+  w.total = w.grid + align_up(sizeof(Grid) * std::max<size_t>(1, steps));
+  return w;
+}
+
+// The runs of all segments with the positions they start at: a run of text
+// takes as many positions as tokens, a screenshot as many as its longest axis.
+std::vector<PosRun> pos_runs(const seg_problem *p, const Plan &pl, const Grid *grid) {
+  std::vector<PosRun> runs;
+  runs.reserve(pl.pieces.size());
+  for (size_t i = 0; i < pl.dsegs.size(); ++i) {
+    const DevSeg &d = pl.dsegs[i];
+    const int s0 = p->step_offsets[pl.seg_info[i * SEG_INFO_FIELDS + SEG_INFO_TRAJ]];
+    int64_t n = 0;
+    for (int k = 0; k < d.piece_count; ++k) {
+      const Piece &pc = pl.pieces[d.piece_base + k];
+      if (pc.len == 0) continue;
+      const bool image = (pc.meta & 3) == SEG_KIND_IMAGE;
+      const int step = image ? s0 + (pc.meta >> 2) - 1 : -1;
+      runs.push_back({d.start + pc.off, pc.len, (int32_t)n, step});
+      int64_t take = pc.len;
+      if (image) {
+        const Grid &g = grid[step];
+        take = std::max<int64_t>(std::max(g.h, g.w), (int64_t)g.e * (g.t - 1) + 1);
+      }
+      n += take;
+      SEG_CHECK(n <= INT32_MAX, SEG_ERR_CAPACITY, "a position of segment %zu passes 2^31-1", i);
+    }
+  }
+  return runs;
+}
+
+// pos[axis][row]: a block's rows lie in few runs, found once for the block.
+__global__ void __launch_bounds__(256) k_mrope_pos(const PosRun *__restrict__ runs, int n,
+                                                   const Grid *__restrict__ grid, int P,
+                                                   int32_t *__restrict__ pos) {
+  const int first = blockIdx.x * TOK_BLOCK, rows = min(TOK_BLOCK, P - first);
+  const int r0 = max(0, upper_index(n, first, [&](int i) { return runs[i].row; }));
+  const int cnt = upper_index(n - r0, first + (rows - 1), [&](int i) { return runs[r0 + i].row; }) + 1;
+  for (int o = threadIdx.x; o < rows; o += 256) {
+    const int r = first + o;
+    const PosRun u = runs[r0 + max(0, upper_index(cnt, r, [&](int i) { return runs[r0 + i].row; }))];
+    const int at = r - u.row;
+    int t = -1, h = -1, w = -1;
+    if (at >= 0 && at < u.len) {
+      t = h = w = u.start + at;
+      if (u.step >= 0) {
+        const Grid g = grid[u.step];
+        const int f = at / (g.h * g.w), in = at - f * (g.h * g.w), y = in / g.w;
+        t = u.start + g.e * f;
+        h = u.start + y;
+        w = u.start + (in - y * g.w);
+      }
+    }
+    pos[r] = t;
+    pos[(long)P + r] = h;
+    pos[2L * P + r] = w;
+  }
+}
+
 }  // namespace
 }  // namespace seg
 
 using namespace seg;
+
+extern "C" size_t seg_mrope_positions_workspace_bytes(const seg_problem *p) {
+  size_t n = 0;
+  (void)guarded([&] {
+    const Plan pl = make_plan(p);
+    n = pos_ws_layout(pl.pieces.size(), pl.sz.num_steps).total;
+  });
+  return n;
+}
+
+extern "C" seg_status seg_mrope_positions(const seg_problem *p, const seg_sizes *sz, const int32_t *grid,
+                                          int32_t *pos, void *ws, size_t ws_bytes, hipStream_t stream) {
+  return guarded([&] {
+    SEG_CHECK(sz != nullptr, SEG_ERR_ARG, "sizes is NULL");
+    const Plan pl = make_plan(p);
+    SEG_CHECK(std::memcmp(&pl.sz, sz, sizeof(seg_sizes)) == 0, SEG_ERR_ARG,
+              "sizes do not match seg_layout_query of this problem");
+    const Grid *g = reinterpret_cast<const Grid *>(grid);
+    for (int s = 0; s < sz->num_steps; ++s) {
+      if (p->img_len[s] == 0) continue;
+      SEG_CHECK(g, SEG_ERR_ARG, "grid is NULL, and step %d has a screenshot", s);
+      SEG_CHECK(g[s].t >= 1 && g[s].h >= 1 && g[s].w >= 1 && g[s].e >= 0, SEG_ERR_ARG,
+                "grid of step %d: %d x %d x %d, time step %d", s, g[s].t, g[s].h, g[s].w, g[s].e);
+      // (t h may pass 63 bits only where t h w does not fit img_len either)
+      const int64_t th = (int64_t)g[s].t * g[s].h;
+      SEG_CHECK(th <= INT32_MAX && th * g[s].w == p->img_len[s], SEG_ERR_ARG,
+                "grid of step %d: %d x %d x %d is not its %d tokens", s, g[s].t, g[s].h, g[s].w,
+                p->img_len[s]);
+    }
+    const std::vector<PosRun> runs = pos_runs(p, pl, g);
+    const PosWs w = pos_ws_layout(pl.pieces.size(), sz->num_steps);
+    SEG_CHECK(ws_bytes >= w.total, SEG_ERR_WORKSPACE, "workspace of %zu bytes < required %zu", ws_bytes,
+              w.total);
+    const int P = (int)sz->packed_tokens;
+    if (P == 0) return;
+    SEG_CHECK(pos && ws, SEG_ERR_ARG, "pos or ws is NULL");
+    std::vector<char> tab(w.total);
+    std::memcpy(tab.data() + w.run, runs.data(), runs.size() * sizeof(PosRun));
+    if (g) std::memcpy(tab.data() + w.grid, g, sz->num_steps * sizeof(Grid));
+    SEG_HIP(hipMemcpyAsync(ws, tab.data(), w.total, hipMemcpyHostToDevice, stream));
+    // the host tables are locals of this call: wait until they have been read
+    SEG_HIP(hipStreamSynchronize(stream));
+    ProfScope prof("mrope_pos", stream);
+    const char *base = static_cast<const char *>(ws);
+    k_mrope_pos<<<(unsigned)((P + (int64_t)TOK_BLOCK - 1) / TOK_BLOCK), 256, 0, stream>>>(
+        reinterpret_cast<const PosRun *>(base + w.run), (int)runs.size(),
+        reinterpret_cast<const Grid *>(base + w.grid), P, pos);
+    SEG_LAUNCH_CHECK();
+  });
+}
 
 extern "C" const char *seg_last_error(void) { return g_err.c_str(); }
 

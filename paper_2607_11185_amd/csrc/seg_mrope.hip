@@ -1,0 +1,196 @@
+// Rotary embedding with positions on several axes (time, height, width): pair
+// (x_i, x_{i + d/2}) of a head turns by pos[axis(i)] base^(-2i/d), where the
+// first pairs belong to the time axis, the next to the height and the last to
+// the width; the backward turns by minus that angle (the transpose).
+//
+// Bound by HBM: q and k are read once and written once.  A block takes a few
+// rows: it issues their loads, forms each row's d/2 cosines and sines once for
+// all heads while they are on their way, and keeps those in LDS.  An angle of a
+// far position needs more than fp32 (at position 10^6 its last place is 1/16
+// of a radian), so the turns are formed and reduced in fp64 and only the part
+// of a turn that is left goes to fp32.
+#include <cmath>
+
+#include "mrope.h"
+
+namespace seg {
+namespace {
+
+constexpr int MAX_ROWS = 16;       // rows of a block
+constexpr int CS = 512;            // (cos, sin) pairs of a block
+
+template <class T>
+struct Eight;
+template <>
+struct Eight<unsigned short> {
+  u16x8 v;
+  __device__ __forceinline__ float get(int j) const { return bf_bits2f(v[j]); }
+  __device__ __forceinline__ void set(int j, float f) { v[j] = f2bf_bits(f); }
+};
+template <>
+struct Eight<float> {
+  f32x4 v[2];
+  __device__ __forceinline__ float get(int j) const { return v[j / 4][j & 3]; }
+  __device__ __forceinline__ void set(int j, float f) { v[j / 4][j & 3] = f; }
+};
+
+// rows_per rows a block; half_pow: d/2 rounded up to a power of two
+template <class T>
+__global__ void __launch_bounds__(256) k_mrope(const mrope::Args g, int rows_per, int half_pow) {
+  __shared__ __attribute__((aligned(16))) float2 cs[CS];
+  __shared__ int ok[MAX_ROWS];
+  const int half = g.d / 2, per = half / 8, chunks = (g.a.heads + g.b.heads) * per;
+  const long row0 = (long)blockIdx.x * rows_per;
+  const int rows = (int)min((long)rows_per, g.rows - row0);
+  for (int e = threadIdx.x; e < rows * half_pow; e += 256) {
+    const int r = e / half_pow, i = e & (half_pow - 1);
+    const long row = row0 + r;
+    if (i == 0) {
+      bool y = true;
+      if (g.pad) y = g.pad[row] >= 0;
+      else
+        for (int a = 0; a < 3; ++a) y = y && g.pos[a * g.rows + row] >= 0;
+      ok[r] = y;
+    }
+    if (i < half) {
+      const int axis = i < g.s0 ? 0 : i < g.s01 ? 1 : 2;
+      // turns = pos base^(-2i/d) / (2 pi)
+      const double f = exp2(-(double)(2 * i) / g.d * g.log2_base) * 0.15915494309189535;
+      const double t = (double)g.pos[axis * g.rows + row] * f;
+      float s, c;
+      sincospif(2.f * (float)(t - rint(t)), &s, &c);
+      cs[r * half + i] = make_float2(c, g.inverse ? -s : s);
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < rows * chunks; e += 256) {
+    const int r = e / chunks, q = e - r * chunks, h = q / per, i = (q - h * per) * 8;
+    const long row = row0 + r;
+    const bool first = h < g.a.heads;
+    const long lx = first ? g.a.ldx : g.b.ldx, ly = first ? g.a.ldy : g.b.ldy;
+    const int hh = first ? h : h - g.a.heads;
+    const T *x = static_cast<const T *>(first ? g.a.x : g.b.x) + row * lx + hh * g.d + i;
+    T *y = static_cast<T *>(first ? g.a.y : g.b.y) + row * ly + hh * g.d + i;
+    typedef Eight<T> E;
+    E lo = *reinterpret_cast<const E *>(x), hi = *reinterpret_cast<const E *>(x + half), olo, ohi;
+    if (ok[r]) {
+      const f32x4 *t = reinterpret_cast<const f32x4 *>(cs + r * half + i);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const f32x4 w = t[j / 2];
+        const float c = w[(j & 1) * 2], s = w[(j & 1) * 2 + 1];
+        olo.set(j, lo.get(j) * c - hi.get(j) * s);
+        ohi.set(j, hi.get(j) * c + lo.get(j) * s);
+      }
+    } else if (g.inverse) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        olo.set(j, 0.f);
+        ohi.set(j, 0.f);
+      }
+    } else {
+      if (y == x) continue;
+      olo = lo;
+      ohi = hi;
+    }
+    *reinterpret_cast<E *>(y) = olo;
+    *reinterpret_cast<E *>(y + half) = ohi;
+  }
+  if (g.zero && g.inverse)
+    for (int r = 0; r < rows; ++r)
+      if (!ok[r])
+        for (int c = threadIdx.x; c < g.zero_width / 8; c += 256)
+          *reinterpret_cast<u16x8 *>(g.zero + (row0 + r) * g.zero_width + c * 8) =
+              u16x8{0, 0, 0, 0, 0, 0, 0, 0};
+}
+
+}  // namespace
+
+namespace mrope {
+
+void check_cfg(const seg_mrope_cfg *cfg, int32_t d) {
+  SEG_CHECK(cfg, SEG_ERR_ARG, "the rotary cfg is NULL");
+  SEG_CHECK(d >= 16 && d % 16 == 0 && d <= MAX_D, SEG_ERR_UNSUPPORTED,
+            "head_dim %d must be a multiple of 16 up to %d", d, MAX_D);
+  long sum = 0;
+  for (int a = 0; a < 3; ++a) {
+    SEG_CHECK(cfg->sections[a] >= 0, SEG_ERR_ARG, "sections[%d] < 0", a);
+    sum += cfg->sections[a];
+  }
+  SEG_CHECK(sum == d / 2, SEG_ERR_ARG, "the sections sum to %ld, not to head_dim / 2 = %d", sum, d / 2);
+  SEG_CHECK(std::isfinite(cfg->base) && cfg->base > 1.f, SEG_ERR_ARG, "the rotary base must be > 1");
+}
+
+void launch(seg_dtype dt, const Args &g, hipStream_t st) {
+  if (g.rows == 0) return;
+  const int half = g.d / 2, chunks = (g.a.heads + g.b.heads) * (half / 8);
+  int hp = 8;
+  while (hp < half) hp *= 2;
+  const int want = (1024 + chunks - 1) / chunks;  // about four chunks a thread
+  const int rows_per = std::max(1, std::min(std::min(want, MAX_ROWS), CS / hp));
+  const long nb = (g.rows + rows_per - 1) / rows_per;
+  SEG_CHECK(nb <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "too many rows for one launch");
+  ProfScope prof("mrope", st);
+  if (dt == SEG_BF16) k_mrope<unsigned short><<<(unsigned)nb, 256, 0, st>>>(g, rows_per, hp);
+  else k_mrope<float><<<(unsigned)nb, 256, 0, st>>>(g, rows_per, hp);
+  SEG_LAUNCH_CHECK();
+}
+
+}  // namespace mrope
+
+namespace {
+
+seg_status rotate(int64_t rows, seg_dtype dt, const seg_mrope_cfg *cfg, int32_t hq, int32_t hkv, int32_t d,
+                  const int32_t *pos, const void *q, int64_t ldq, const void *k, int64_t ldk, void *qo,
+                  int64_t ldqo, void *ko, int64_t ldko, int inverse, hipStream_t stream) {
+  return guarded([&] {
+    SEG_CHECK(dt == SEG_BF16 || dt == SEG_F32, SEG_ERR_UNSUPPORTED, "dtype %d not supported", (int)dt);
+    mrope::check_cfg(cfg, d);
+    SEG_CHECK(rows >= 0, SEG_ERR_ARG, "rows < 0");
+    SEG_CHECK(hq >= 1 && hkv >= 0 && hq <= 65536 && hkv <= 65536, SEG_ERR_ARG, "heads %d/%d out of range", hq, hkv);
+    SEG_CHECK(rows < (1LL << 31), SEG_ERR_CAPACITY, "more than 2^31-1 rows");
+    if (rows == 0) return;
+    SEG_CHECK(pos && q && qo && (hkv == 0 || (k && ko)), SEG_ERR_ARG, "pos, a tensor or an output is NULL");
+    const int64_t e = dt == SEG_BF16 ? 2 : 4;
+    const void *ptr[4] = {q, k, qo, ko};
+    const int64_t ld[4] = {ldq, ldk, ldqo, ldko};
+    for (int i = 0; i < 4; ++i) {
+      const int64_t heads = i & 1 ? hkv : hq;
+      if (heads == 0) continue;
+      SEG_CHECK(ld[i] >= heads * d && ld[i] < (1LL << 40), SEG_ERR_ARG, "row stride %lld does not hold %lld heads of %d",
+                (long long)ld[i], (long long)heads, d);
+      SEG_CHECK(reinterpret_cast<uintptr_t>(ptr[i]) % 16 == 0 && ld[i] * e % 16 == 0, SEG_ERR_UNSUPPORTED,
+                "rows must start on 16-byte boundaries");
+    }
+    mrope::Args g{};
+    g.a = mrope::Heads{q, qo, ldq, ldqo, hq};
+    g.b = mrope::Heads{k, ko, ldk, ldko, hkv};
+    g.rows = rows;
+    g.d = d;
+    g.inverse = inverse;
+    g.s0 = cfg->sections[0];
+    g.s01 = g.s0 + cfg->sections[1];
+    g.log2_base = std::log2((double)cfg->base);
+    g.pos = pos;
+    mrope::launch(dt, g, stream);
+  });
+}
+
+}  // namespace
+}  // namespace seg
+
+using namespace seg;
+
+extern "C" seg_status seg_mrope_fwd(int64_t rows, seg_dtype dt, const seg_mrope_cfg *cfg, int32_t hq,
+                                    int32_t hkv, int32_t d, const int32_t *pos, const void *q,
+                                    int64_t ldq, const void *k, int64_t ldk, void *q_out,
+                                    int64_t ldqo, void *k_out, int64_t ldko, hipStream_t stream) {
+  return rotate(rows, dt, cfg, hq, hkv, d, pos, q, ldq, k, ldk, q_out, ldqo, k_out, ldko, 0, stream);
+}
+
+extern "C" seg_status seg_mrope_bwd(int64_t rows, seg_dtype dt, const seg_mrope_cfg *cfg, int32_t hq,
+                                    int32_t hkv, int32_t d, const int32_t *pos, const void *dq,
+                                    int64_t ldq, const void *dk, int64_t ldk, void *dq_out,
+                                    int64_t ldqo, void *dk_out, int64_t ldko, hipStream_t stream) {
+  return rotate(rows, dt, cfg, hq, hkv, d, pos, dq, ldq, dk, ldk, dq_out, ldqo, dk_out, ldko, 1, stream);
+}

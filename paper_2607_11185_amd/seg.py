@@ -1,8 +1,9 @@
 """Python binding of the libseg entry points, on PyTorch device tensors.
 
 Functions carry the C names (seg_layout_query, seg_build_layout, seg_attn_fwd,
-seg_attn_bwd, seg_logprob_loss, seg_layer_fwd, seg_layer_bwd) and only marshal
-arguments: they allocate
+seg_attn_bwd, seg_logprob_loss, seg_layer_fwd, seg_layer_bwd, seg_mrope_positions,
+seg_mrope_fwd, seg_mrope_bwd, seg_act_pack, seg_act_unpack, seg_glu_fwd,
+seg_glu_bwd) and only marshal arguments: they allocate
 outputs and workspace with torch on the tensors' device and pass raw
 pointers plus torch's current stream to the library.
 """
@@ -361,3 +362,229 @@ def seg_layer_bwd(lay: Layout, cfg: LayerCfg, w: dict, x, saved: dict, dy, dx=No
                                    dy.data_ptr(), dx.data_ptr(), ctypes.byref(g), ws.data_ptr(),
                                    ws.numel(), _stream(dev)))
     return dx, grads
+
+
+def _device(*tensors):
+    """The GPU that all the tensors (None: left out) are on."""
+    dev = tensors[0].device
+    for t in tensors:
+        assert t is None or (t.is_cuda and t.device == dev), f"tensors on {dev} and {t.device}"
+    return dev
+
+
+def _on(dev):
+    """Calls are made with the tensors' GPU as the current one."""
+    import torch
+    return torch.cuda.device(dev)
+
+
+@dataclasses.dataclass
+class MropeCfg:
+    """Rotary positions on three axes: pairs that turn with time, height and
+    width (they sum to d / 2), and the base."""
+    sections: tuple
+    base: float = 1e6
+
+    def c(self) -> "_lib.SegMropeCfg":
+        if len(self.sections) != 3:
+            raise ValueError("sections: three numbers (time, height, width)")
+        return _lib.SegMropeCfg((ctypes.c_int32 * 3)(*self.sections), self.base)
+
+
+def seg_mrope_positions(problem: Problem, lay: Layout, grid, pos=None, ws=None):
+    """Time, height and width positions [3, P] int32 (-1 in padding rows) of a
+    problem's packed layout; grid: host [num_steps, 4] int32, the frames, patch
+    rows, patch columns and time step of each step's screenshot (None where no
+    step has one)."""
+    import torch
+    L = _lib.lib()
+    pc = problem.c()
+    if grid is not None:
+        grid = np.ascontiguousarray(np.asarray(grid, dtype=np.int32))
+        if grid.shape != (lay.sizes.num_steps, 4):
+            raise ValueError(f"grid of shape {grid.shape}, not ({lay.sizes.num_steps}, 4)")
+    if pos is None:
+        pos = torch.empty((3, lay.sizes.packed_tokens), dtype=torch.int32, device=lay.device)
+    assert pos.dtype == torch.int32 and pos.is_contiguous() and pos.shape == (3, lay.sizes.packed_tokens)
+    if ws is None:
+        n = L.seg_mrope_positions_workspace_bytes(ctypes.byref(pc))
+        ws = torch.empty(max(n, 1), dtype=torch.uint8, device=lay.device)
+    dev = _device(pos, ws)
+    with _on(dev):
+        check(L.seg_mrope_positions(ctypes.byref(pc), ctypes.byref(lay.sizes),
+                                    None if grid is None else grid.ctypes.data, pos.data_ptr(),
+                                    ws.data_ptr(), ws.numel(), _stream(dev)))
+    return pos
+
+
+def _mrope(f, q, k, pos, cfg: MropeCfg, q_out, k_out):
+    import torch
+    rows, hq, d = q.shape
+    hkv = 0 if k is None else k.shape[1]
+    dt = _dtype_code(q)
+    if q_out is None:
+        q_out = torch.empty((rows, hq, d), dtype=q.dtype, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty((rows, hkv, d), dtype=k.dtype, device=k.device)
+    for t, heads in ((q, hq), (k, hkv), (q_out, hq), (k_out, hkv)):
+        if t is not None:
+            # heads of a row side by side; rows at any distance
+            assert t.shape == (rows, heads, d) and t.dtype == q.dtype
+            assert t.stride(2) == 1 and (t.stride(1) == d or heads == 1), "heads of a row must be adjacent"
+    assert pos.shape == (3, rows) and pos.dtype == torch.int32 and pos.is_contiguous()
+    dev = _device(q, k, q_out, k_out, pos)
+
+    def ld(t, heads):
+        return heads * d if rows <= 1 else t.stride(0)
+    with _on(dev):
+        check(f(rows, dt, ctypes.byref(cfg.c()), hq, hkv, d, pos.data_ptr(), q.data_ptr(), ld(q, hq),
+                _ptr(k), 0 if k is None else ld(k, hkv), q_out.data_ptr(), ld(q_out, hq),
+                _ptr(k_out), 0 if k is None else ld(k_out, hkv), _stream(dev)))
+    return q_out, k_out
+
+
+def seg_mrope_fwd(q, k, pos, cfg: MropeCfg, q_out=None, k_out=None):
+    """q [rows, hq, d] and k [rows, hkv, d] (or None) rotated by pos [3, rows]
+    int32; rows may lie at any distance, outputs may be the inputs.  Returns
+    (q_out, k_out)."""
+    return _mrope(_lib.lib().seg_mrope_fwd, q, k, pos, cfg, q_out, k_out)
+
+
+def seg_mrope_bwd(dq, dk, pos, cfg: MropeCfg, dq_out=None, dk_out=None):
+    """Gradients of the unrotated q and k from those of the rotated ones."""
+    return _mrope(_lib.lib().seg_mrope_bwd, dq, dk, pos, cfg, dq_out, dk_out)
+
+
+@dataclasses.dataclass
+class Act8:
+    """Activations in 8 bits: code [rows, cols] int8 and exp [rows, ceil(cols / 32)]
+    uint8, value = code * 2^(exp - 127)."""
+    code: object
+    exp: object
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device) -> "Act8":
+        import torch
+        return cls(torch.empty((rows, cols), dtype=torch.int8, device=device),
+                   torch.empty((rows, -(-cols // 32)), dtype=torch.uint8, device=device))
+
+    def c(self) -> "_lib.SegAct8":
+        import torch
+        rows, cols = self.code.shape
+        assert self.code.dtype == torch.int8 and self.exp.dtype == torch.uint8
+        assert self.exp.shape == (rows, -(-cols // 32))
+        assert self.code.is_contiguous() and self.exp.is_contiguous()
+        return _lib.SegAct8(self.code.data_ptr(), self.exp.data_ptr())
+
+
+def _rows(t) -> int:
+    """Elements between the rows of t [rows, cols]."""
+    rows, cols = t.shape
+    assert cols <= 1 or t.stride(1) == 1, "columns must be adjacent"
+    return cols if rows <= 1 else t.stride(0)
+
+
+def seg_act_pack(x, out: Optional[Act8] = None) -> Act8:
+    """x [rows, cols] (rows at any distance) in 8 bits."""
+    rows, cols = x.shape
+    dt = _dtype_code(x)
+    if out is None:
+        out = Act8.empty(rows, cols, x.device)
+    assert out.code.shape == (rows, cols)
+    dev = _device(x, out.code, out.exp)
+    with _on(dev):
+        check(_lib.lib().seg_act_pack(rows, cols, dt, x.data_ptr(), _rows(x), ctypes.byref(out.c()),
+                                      _stream(dev)))
+    return out
+
+
+def seg_act_unpack(act: Act8, dtype=None, x=None):
+    """The values of `act` in `dtype` (bf16 by default), or into x [rows, cols]."""
+    import torch
+    rows, cols = act.code.shape
+    if x is None:
+        x = torch.empty((rows, cols), dtype=dtype or torch.bfloat16, device=act.code.device)
+    assert x.shape == (rows, cols) and (dtype is None or x.dtype == dtype)
+    dev = _device(x, act.code, act.exp)
+    with _on(dev):
+        check(_lib.lib().seg_act_unpack(rows, cols, _dtype_code(x), ctypes.byref(act.c()),
+                                        x.data_ptr(), _rows(x), _stream(dev)))
+    return x
+
+
+def _glu_args(x, wg, wu):
+    import torch
+    rows, hidden = x.shape
+    inter = wg.shape[0]
+    for t in (wg, wu):
+        assert t.shape == (inter, hidden) and t.dtype == torch.bfloat16 and t.is_contiguous()
+    assert x.dtype == torch.bfloat16
+    return rows, hidden, inter
+
+
+def _kept(kept, rows, inter):
+    """The two C structs of a kept pair, and its tensors."""
+    if kept is None:
+        return (None, None), ()
+    g, u = kept
+    assert g.code.shape == u.code.shape == (rows, inter)
+    return (ctypes.byref(g.c()), ctypes.byref(u.c())), (g.code, g.exp, u.code, u.exp)
+
+
+def seg_glu_fwd(x, wg, wu, keep=False, m=None):
+    """m = silu(x wg^T) * (x wu^T); x [rows, H] (rows at any distance), wg and wu
+    [I, H], bf16.  keep: True, or a pair (Act8, Act8) to fill, keeps the gate and
+    up values in 8 bits.  Returns (m, kept or None)."""
+    import torch
+    rows, hidden, inter = _glu_args(x, wg, wu)
+    if m is None:
+        m = torch.empty((rows, inter), dtype=torch.bfloat16, device=x.device)
+    assert m.shape == (rows, inter) and m.dtype == torch.bfloat16 and m.is_contiguous()
+    if keep is True:
+        keep = (Act8.empty(rows, inter, x.device), Act8.empty(rows, inter, x.device))
+    kept = keep or None
+    c, tensors = _kept(kept, rows, inter)
+    dev = _device(x, wg, wu, m, *tensors)
+    with _on(dev):
+        check(_lib.lib().seg_glu_fwd(rows, hidden, inter, x.data_ptr(), _rows(x), wg.data_ptr(),
+                                     wu.data_ptr(), m.data_ptr(), *c, _stream(dev)))
+    return m, kept
+
+
+def glu_workspace(rows, hidden, inter, kept: bool, device):
+    import torch
+    n = _lib.lib().seg_glu_workspace_bytes(rows, hidden, inter, int(kept))
+    return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
+
+
+def seg_glu_bwd(x, wg, wu, dm, kept=None, dw_dtype=None, want_m=True, out=None, ws=None):
+    """Gradients of sum(m * dm); kept: seg_glu_fwd's pair, or None to compute the
+    gate and up values again.  Returns dict(dx, dwg, dwu, m): the weight gradients
+    in dw_dtype (fp32 by default), m again unless want_m is false (then None)."""
+    import torch
+    rows, hidden, inter = _glu_args(x, wg, wu)
+    assert dm.shape == (rows, inter) and dm.dtype == torch.bfloat16 and dm.is_contiguous()
+    dev = x.device
+    if out is None:
+        dw = dict(dtype=dw_dtype or torch.float32, device=dev)
+        bf = dict(dtype=torch.bfloat16, device=dev)
+        out = {"dx": torch.empty((rows, hidden), **bf), "dwg": torch.empty((inter, hidden), **dw),
+               "dwu": torch.empty((inter, hidden), **dw),
+               "m": torch.empty((rows, inter), **bf) if want_m else None}
+    assert out["dwg"].dtype == out["dwu"].dtype
+    for n, shape in (("dx", (rows, hidden)), ("dwg", (inter, hidden)), ("dwu", (inter, hidden)),
+                     ("m", (rows, inter))):
+        t = out.get(n)
+        assert (n == "m" and t is None) or (t.shape == shape and t.is_contiguous()), n
+        assert t is None or n in ("dwg", "dwu") or t.dtype == torch.bfloat16, n
+    if ws is None:
+        ws = glu_workspace(rows, hidden, inter, kept is not None, dev)
+    c, tensors = _kept(kept, rows, inter)
+    _device(x, wg, wu, dm, out["dx"], out["dwg"], out["dwu"], out.get("m"), ws, *tensors)
+    with _on(dev):
+        check(_lib.lib().seg_glu_bwd(rows, hidden, inter, x.data_ptr(), _rows(x), wg.data_ptr(),
+                                     wu.data_ptr(), *c, dm.data_ptr(), _ptr(out.get("m")),
+                                     out["dx"].data_ptr(), _dtype_code(out["dwg"]),
+                                     out["dwg"].data_ptr(), out["dwu"].data_ptr(), ws.data_ptr(),
+                                     ws.numel(), _stream(dev)))
+    return out

@@ -1,0 +1,151 @@
+"""Host-side checks of the three-axis positions, the rotation, the 8-bit
+activations and the gated block (no GPU): structures, workspace sizes, and
+what each entry point refuses before any launch."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2607_11185_amd import _lib
+from paper_2607_11185_amd import seg as S
+from paper_2607_11185_amd import workload as WL
+from tests.test_abi_host import _lib_or_skip, _prob
+from tests import test_abi_structs as TS
+
+ARG, CAP, WS, UNS = (_lib.SEG_ERR_ARG, _lib.SEG_ERR_CAPACITY, _lib.SEG_ERR_WORKSPACE, _lib.SEG_ERR_UNSUPPORTED)
+STRUCTS = {"seg_mrope_cfg": _lib.SegMropeCfg, "seg_act8": _lib.SegAct8}
+
+
+def test_structures_match_header(tmp_path, monkeypatch):
+    monkeypatch.setattr(TS, "STRUCTS", STRUCTS)
+    TS.test_ctypes_structs_match_header(tmp_path)
+    TS.test_header_fields_all_mirrored()
+
+
+def _positions(pr, grid, sz=None, ws_bytes=1 << 30, pos=None, ws=None):
+    L = _lib_or_skip()
+    sz = sz or S.seg_layout_query(pr)
+    g = None if grid is None else np.ascontiguousarray(grid, np.int32)
+    return L.seg_mrope_positions(ctypes.byref(pr.c()), ctypes.byref(sz), None if g is None else g.ctypes.data, pos, ws,
+                                 ws_bytes, None)
+
+
+GOOD = [[1, 5, 1, 1], [1, 1, 5, 0], [5, 1, 1, 2]]
+
+
+@pytest.mark.parametrize("step,row,want", [
+    (0, [1, 2, 2, 1], ARG),            # four patches for five tokens
+    (1, [0, 5, 1, 1], ARG), (1, [-1, -5, 1, 1], ARG), (2, [1, -1, -5, 1], ARG),
+    (2, [5, 1, 1, -1], ARG),           # negative time step
+    (0, [2 ** 30, 2 ** 30, 2 ** 30, 1], ARG), (0, [65536, 65536, 5, 1], ARG),
+    (2, [5, 1, 1, 2 ** 30], CAP)])     # four steps of 2^30 positions
+def test_positions_refuse_bad_grids(step, row, want):
+    pr = _prob()
+    L = _lib_or_skip()
+    grid = [list(g) for g in GOOD]
+    grid[step] = row
+    assert _positions(pr, grid) == want
+    assert L.seg_last_error()
+
+
+def test_positions_refuse_bad_calls():
+    L = _lib_or_skip()
+    pr = _prob()
+    sz = S.seg_layout_query(pr)
+    need = L.seg_mrope_positions_workspace_bytes(ctypes.byref(pr.c()))
+    assert need > 0
+    assert _positions(pr, None) == ARG and b"grid" in L.seg_last_error()
+    assert _positions(pr, GOOD, ws_bytes=need - 1) == WS
+    assert _positions(pr, GOOD) == ARG and b"NULL" in L.seg_last_error()       # pos and ws
+    other = _lib.SegSizes.from_buffer_copy(sz)
+    other.packed_tokens += 1
+    assert _positions(pr, GOOD, sz=other) == ARG
+    assert L.seg_mrope_positions(None, ctypes.byref(sz), None, None, None, 0, None) == ARG
+    assert L.seg_mrope_positions(ctypes.byref(pr.c()), None, None, None, None, 0, None) == ARG
+    assert L.seg_mrope_positions_workspace_bytes(None) == 0
+    assert L.seg_mrope_positions_workspace_bytes(ctypes.byref(_prob(window=0).c())) == 0
+    # a problem without screenshots needs no grid, and one without trajectories no memory
+    text = S.Problem.from_spans(WL.explicit_spans([2], [3], [0, 0], [4, 4], [1, 1]), 1, 1)
+    assert _positions(text, None) == ARG and b"pos or ws" in L.seg_last_error()
+    none = S.Problem.from_spans(WL.explicit_spans([], [], [], [], []), 1, 1)
+    assert _positions(none, None) == _lib.SEG_OK
+
+
+def _rope(rows=4, dt=0, sections=(8, 12, 12), base=1e4, hq=2, hkv=1, d=64, pos=16, q=16, ldq=128, k=16, ldk=64,
+          qo=16, ldqo=128, ko=16, ldko=64, cfg=True):
+    L = _lib_or_skip()
+    c = _lib.SegMropeCfg((ctypes.c_int32 * 3)(*sections), base)
+    args = (rows, dt, ctypes.byref(c) if cfg else None, hq, hkv, d, pos, q, ldq, k, ldk, qo, ldqo, ko, ldko, None)
+    got = L.seg_mrope_fwd(*args), L.seg_mrope_bwd(*args)
+    assert got[0] == got[1]
+    return got[0]
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(cfg=False), ARG), (dict(rows=-1), ARG), (dict(rows=2 ** 31), CAP), (dict(dt=2), UNS),
+    (dict(sections=(8, 12, 11)), ARG), (dict(sections=(-8, 20, 20)), ARG), (dict(sections=(2 ** 31 - 1, 2 ** 31 - 1, 34)), ARG),
+    (dict(base=1.0), ARG), (dict(base=float("nan")), ARG), (dict(base=float("inf")), ARG),
+    (dict(d=72, sections=(36, 0, 0)), UNS), (dict(d=0, sections=(0, 0, 0)), UNS), (dict(d=272, sections=(136, 0, 0)), UNS),
+    (dict(hq=0), ARG), (dict(hkv=-1), ARG), (dict(hq=1 << 20), ARG),
+    (dict(pos=None), ARG), (dict(q=None), ARG), (dict(k=None), ARG), (dict(qo=None), ARG), (dict(ko=None), ARG),
+    (dict(ldq=127), ARG), (dict(ldk=32), ARG), (dict(ldqo=64), ARG), (dict(ldq=132), UNS), (dict(q=20), UNS), (dict(ko=8), UNS)])
+def test_rotation_refuses(kw, want):
+    assert _rope(**kw) == want
+
+
+def test_rotation_of_nothing():
+    assert _rope(rows=0, pos=None, q=None, k=None, qo=None, ko=None) == _lib.SEG_OK
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(rows=-1), ARG), (dict(cols=0), ARG), (dict(ldx=63), ARG), (dict(dt=5), UNS), (dict(x=None), ARG), (dict(p=None), ARG),
+    (dict(code=None), ARG), (dict(exp=None), ARG), (dict(x=17), ARG), (dict(x=18, dt=1), ARG), (dict(rows=1 << 41), CAP),
+    (dict(rows=1 << 39, cols=1 << 20, ldx=1 << 20), CAP), (dict(rows=1 << 36), CAP)])
+def test_packing_refuses(kw, want):
+    L = _lib_or_skip()
+    a = dict(rows=4, cols=64, ldx=64, dt=0, x=16, p=True, code=8, exp=1)
+    a.update(kw)
+    s = _lib.SegAct8(a["code"], a["exp"])
+    p = ctypes.byref(s) if a["p"] else None
+    assert L.seg_act_pack(a["rows"], a["cols"], a["dt"], a["x"], a["ldx"], p, None) == want
+    assert L.seg_act_unpack(a["rows"], a["cols"], a["dt"], p, a["x"], a["ldx"], None) == want
+
+
+def test_packing_of_nothing():
+    L = _lib_or_skip()
+    s = _lib.SegAct8(None, None)
+    assert L.seg_act_pack(0, 64, 0, None, 64, ctypes.byref(s), None) == _lib.SEG_OK
+    assert L.seg_act_unpack(0, 64, 0, ctypes.byref(s), None, 64, None) == _lib.SEG_OK
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(rows=-1), ARG), (dict(rows=(1 << 20) + 1), UNS), (dict(hidden=60), UNS), (dict(inter=100), UNS), (dict(hidden=0), UNS),
+    (dict(inter=(1 << 20) + 8), UNS), (dict(ldx=56), ARG), (dict(ldx=68), UNS), (dict(x=None), ARG), (dict(wu=None), ARG),
+    (dict(x=8), UNS), (dict(wg=24), UNS), (dict(u8=False), ARG), (dict(g8=False), ARG), (dict(code=None), ARG), (dict(code=4), UNS)])
+def test_gated_block_refuses(kw, want):
+    L = _lib_or_skip()
+    a = dict(rows=4, hidden=64, inter=96, ldx=64, x=16, wg=16, wu=16, g8=True, u8=True, code=8)
+    a.update(kw)
+    s = _lib.SegAct8(a["code"], 1)
+    g8, u8 = (ctypes.byref(s) if a[n] else None for n in ("g8", "u8"))
+    size = (a["rows"], a["hidden"], a["inter"], a["x"], a["ldx"], a["wg"], a["wu"])
+    assert L.seg_glu_fwd(*size, 16, g8, u8, None) == want
+    assert L.seg_glu_bwd(*size, g8, u8, 16, 16, 16, 0, 16, 16, 16, 1 << 40, None) == want
+
+
+def test_gated_block_backward_refuses():
+    L = _lib_or_skip()
+    size = (4, 64, 96, 16, 64, 16, 16)
+    need = L.seg_glu_workspace_bytes(4, 64, 96, 0)
+    kept = L.seg_glu_workspace_bytes(4, 64, 96, 1)
+    assert 0 < kept < need and L.seg_glu_workspace_bytes(-1, 64, 96, 1) == 0
+    s = _lib.SegAct8(8, 1)
+    g = ctypes.byref(s)
+
+    def bwd(g8=None, dm=16, m=16, dx=16, dt=0, dwg=16, dwu=16, ws=16, n=1 << 40):
+        return L.seg_glu_bwd(*size, g8, g8, dm, m, dx, dt, dwg, dwu, ws, n, None)
+    assert bwd(n=need - 1) == WS and bwd(g8=g, n=kept - 1) == WS
+    assert bwd(dm=None) == bwd(dx=None) == bwd(dwg=None) == bwd(dwu=None) == bwd(ws=None) == ARG
+    assert bwd(dm=8) == bwd(m=8) == bwd(dx=8) == bwd(dwg=8) == bwd(dwu=8) == bwd(ws=8) == bwd(dt=3) == UNS
+    assert L.seg_glu_fwd(*size, None, None, None, None) == ARG
+    assert L.seg_glu_fwd(0, 64, 96, None, 64, None, None, None, None, None, None) == _lib.SEG_OK

@@ -1,0 +1,173 @@
+"""Gated feed-forward block on the GPU against the float64 oracle.
+
+Forward: g and u are fp32 sums of exact products, off by at most e_g = (H + 1)
+2^-24 sum|x w|; silu has slope at most 1.1, its fp32 evaluation is good to
+(|g| + 8) 2^-23 (the exponent's argument and a few roundings); m rounds once to
+bf16 (2^-8).  Kept values are off by half a step, at most max|g| / 127 of the
+block, and e_g.
+
+Backward, from given kept values: dg and du round to bf16 (2^-8), the products
+are exact, their sums in fp32, the outputs round again where they are bf16.
+Elementwise that is at most 2^-8 sum|dg w| + 2^-8 |out| and the sums' part; over a
+whole tensor the two roundings are independent and uniform, 2^-8 / sqrt(3) each,
+so the relative Frobenius error stays below 2^-8."""
+import numpy as np
+import pytest
+
+from oracle import act8 as OA8
+from oracle import glu as OG
+from paper_2607_11185_amd import seg as S
+from tests.gpu_helpers import rel, say
+
+pytestmark = pytest.mark.gpu
+
+# rows, hidden, inter: one row and few, widths around the tiles of 32, 64, 128 and 256
+SHAPES = [(1, 8, 8), (1, 64, 40), (3, 72, 104), (17, 328, 200), (64, 256, 256), (130, 264, 520), (300, 128, 1032),
+          (257, 512, 72), (16, 1024, 2048), (33, 2048, 264)]
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _within(got, ref, tol, name):
+    over = np.abs(got - ref) - tol
+    worst = float(over.max())
+    assert worst <= 0, (name, worst, int((over > 0).sum()))
+
+
+def _inputs(rows, hidden, inter, seed=0, pad=0):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed * 1000 + rows)
+
+    def r(*s, std=1.0):
+        return (torch.randn(*s, generator=gen, device="cuda") * std).to(torch.bfloat16)
+    x = r(rows, hidden + pad)[:, :hidden]
+    return x, r(inter, hidden, std=2 / hidden ** 0.5), r(inter, hidden, std=1 / hidden ** 0.5), r(rows, inter)
+
+
+def _forward_bounds(x, wg, wu):
+    m, g, u = OG.forward(x, wg, wu)
+    n = (x.shape[1] + 1) * 2.0 ** -24
+    eg, eu = n * (np.abs(x) @ np.abs(wg).T), n * (np.abs(x) @ np.abs(wu).T)
+    silu = np.abs(g * OG.sigmoid(g))
+    em = 1.1 * eg * (np.abs(u) + eu) + silu * eu + silu * np.abs(u) * (np.abs(g) + 8) * 2.0 ** -23
+    return m, g, u, eg, eu, em + 2.0 ** -8 * (np.abs(m) + em) + 1e-38
+
+
+@pytest.mark.parametrize("keep", [False, True])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_forward(shape, keep):
+    import torch
+    rows, hidden, inter = shape
+    say(shape)
+    x, wg, wu, _ = _inputs(*shape, pad=8)
+    m, kept = S.seg_glu_fwd(x, wg, wu, keep=keep)
+    ref, g, u, eg, eu, em = _forward_bounds(_np(x), _np(wg), _np(wu))
+    _within(_np(m), ref, em, "m")
+    assert (kept is not None) == keep
+    for a, v, e in zip(kept or (), (g, u), (eg, eu)):
+        got = _np(S.seg_act_unpack(a, torch.float32))
+        top = np.abs(np.pad(v, ((0, 0), (0, -inter % 32)))).reshape(rows, -1, 32).max(-1)
+        top = np.repeat(top, 32, 1)[:, :inter]
+        _within(got, v, (top + e) / 127 + e, "kept")
+    if keep:
+        assert torch.equal(m, S.seg_glu_fwd(x, wg, wu)[0])     # the same m either way
+
+
+def _kept_of(g, u):
+    import torch
+    out = []
+    for v in (g, u):
+        code, exp = OA8.pack(v)
+        out.append(S.Act8(torch.from_numpy(code).cuda(), torch.from_numpy(exp).cuda()))
+    return tuple(out), tuple(OA8.unpack(*OA8.pack(v)) for v in (g, u))
+
+
+@pytest.mark.parametrize("dw", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_backward_from_kept_values(shape, dw):
+    import torch
+    rows, hidden, inter = shape
+    x, wg, wu, dm = _inputs(*shape, seed=1, pad=16)
+    xn, wgn, wun, dmn = (_np(t) for t in (x, wg, wu, dm))
+    _, g, u = OG.forward(xn, wgn, wun)
+    kept, (gv, uv) = _kept_of(g, u)
+    out = S.seg_glu_bwd(x, wg, wu, dm, kept, dw_dtype=torch.bfloat16 if dw == "bf16" else torch.float32)
+    dg, du = OG.backward_act(gv, uv, dmn)
+    dx, dwg, dwu = OG.backward(xn, wgn, wun, gv, uv, dmn)
+    h = 2.0 ** -8
+    ag, au = np.abs(dg), np.abs(du)
+    # the activation's own fp32 error joins the rounding of dg and du
+    ag_e, au_e = ag * h + (np.abs(dmn * uv) * (np.abs(gv) + 8) * 2.0 ** -22), au * h + (np.abs(dmn * gv) * 2.0 ** -22)
+    n = (2 * inter + 1) * 2.0 ** -24
+    sums = (ag + ag_e) @ np.abs(wgn) + (au + au_e) @ np.abs(wun)
+    checks = [("dx", dx, ag_e @ np.abs(wgn) + au_e @ np.abs(wun) + n * sums, True)]
+    n = (rows + 1) * 2.0 ** -24
+    for name, ref, e, a in (("dwg", dwg, ag_e, ag), ("dwu", dwu, au_e, au)):
+        checks.append((name, ref, e.T @ np.abs(xn) + n * ((a + e).T @ np.abs(xn)), dw == "bf16"))
+    for name, ref, tol, bf in checks:
+        got = _np(out[name])
+        tol = tol + (h * (np.abs(ref) + tol) if bf else 0) + 1e-38
+        _within(got, ref, tol, name)
+        if ref.size >= 4096:
+            assert rel(got, ref) < h, (name, rel(got, ref))
+    m = gv * OG.sigmoid(gv) * uv
+    _within(_np(out["m"]), m, h * np.abs(m) * (1 + 1e-5) + np.abs(m) * (np.abs(gv) + 8) * 2.0 ** -22 + 1e-38, "m")
+
+
+@pytest.mark.parametrize("shape", [(17, 328, 200), (300, 128, 1032)], ids=str)
+def test_backward_without_kept_values(shape):
+    """Gate and up values computed again, in bf16: their rounding (2^-8) moves dg and du
+    by a few times that, independently, so 2^-6 bounds the relative Frobenius error."""
+    import torch
+    x, wg, wu, dm = _inputs(*shape, seed=2)
+    xn, wgn, wun, dmn = (_np(t) for t in (x, wg, wu, dm))
+    m, g, u = OG.forward(xn, wgn, wun)
+    out = S.seg_glu_bwd(x, wg, wu, dm, None)
+    for name, ref in zip(("dx", "dwg", "dwu", "m"), (*OG.backward(xn, wgn, wun, g, u, dmn), m)):
+        assert rel(_np(out[name]), ref) < 2.0 ** -6, name
+    only = S.seg_glu_bwd(x, wg, wu, dm, None, want_m=False)
+    assert only["m"] is None and all(torch.equal(only[n], out[n]) for n in ("dx", "dwg", "dwu"))
+
+
+def test_forward_and_backward_as_used():
+    """The kept values of a forward through the backward: gradients of the block within
+    what 8 bits take (steps of at most 2 / 127 of a block's largest value, about 1 % of a
+    value in the mean, twice where g enters as product and slope)."""
+    shape = (200, 256, 512)
+    x, wg, wu, dm = _inputs(*shape, seed=3)
+    m, kept = S.seg_glu_fwd(x, wg, wu, keep=True)
+    out = S.seg_glu_bwd(x, wg, wu, dm, kept)
+    xn, wgn, wun, dmn = (_np(t) for t in (x, wg, wu, dm))
+    _, g, u = OG.forward(xn, wgn, wun)
+    for name, ref in zip(("dx", "dwg", "dwu"), OG.backward(xn, wgn, wun, g, u, dmn)):
+        assert rel(_np(out[name]), ref) < 2.0 / 63.5, name
+    assert rel(_np(out["m"]), _np(m)) < 2.0 / 63.5
+
+
+def test_extremes():
+    """A row of zeros, gates far from zero on both sides, and an infinity that stays in its row."""
+    import torch
+    x, wg, wu, dm = _inputs(40, 64, 96, seed=4)
+    x[3] = 0
+    x[4] *= 100
+    m, kept = S.seg_glu_fwd(x, wg, wu, keep=True)
+    assert not m[3].any() and not kept[0].exp[3].any() and not kept[1].code[3].any()
+    ref = OG.forward(*(_np(t) for t in (x, wg, wu)))[0]
+    assert rel(_np(m)[4], ref[4]) < 2.0 ** -8
+    x[7, 5] = float("inf")
+    m2, kept2 = S.seg_glu_fwd(x, wg, wu, keep=True)
+    rows = torch.arange(40, device="cuda") != 7
+    assert torch.equal(m2[rows], m[rows]) and bool((kept2[0].exp[7] == 255).all())
+    assert torch.equal(kept2[0].code[rows], kept[0].code[rows])
+
+
+def test_no_rows_give_zero_weight_gradients():
+    import torch
+    x, wg, wu, dm = _inputs(4, 64, 72)
+    assert S.seg_glu_fwd(x[:0], wg, wu, keep=True)[0].shape == (0, 72)
+    for dt in (torch.bfloat16, torch.float32):
+        nan = {n: torch.full((72, 64), float("nan"), dtype=dt, device="cuda") for n in ("dwg", "dwu")}
+        S.seg_glu_bwd(x[:0], wg, wu, dm[:0], None, out=dict(nan, dx=x[:0].contiguous(), m=None))
+        assert not nan["dwg"].any() and not nan["dwu"].any()
