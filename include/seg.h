@@ -469,12 +469,54 @@ seg_status seg_glu_bwd(int32_t rows, int32_t hidden, int32_t inter, const void *
                        void *ws, size_t ws_bytes, hipStream_t stream);
 
 /*
+ * The decoder layer with positions on three axes and 8-bit saved activations
+ * (either, both, or with ext NULL seg_layer_fwd / seg_layer_bwd themselves).
+ *   rope, pos: q and k turn by pos [3, P] (seg_mrope_positions) with rope's
+ *   sections and base, in place of the row inside the segment and rope_base;
+ *   padding is where the layout says so, whatever pos holds there.  The same
+ *   positions are given to the backward.
+ *   saved8: what the backward reads is kept in 8 bits here, x among it: a layer
+ *   of the 7B-class widths keeps 15.8 KB a row, not 30.7.  `saved` is unused
+ *   and may be NULL, and so may x in the backward.  The backward is that of the
+ *   kept values: it computes what seg_layer_bwd does from x, q, k, v, o and y1
+ *   read back (seg_act_unpack) and lse, rstd1 and rstd2 of the forward.  With
+ *   codes for g and u (both or none) the gate and up values are kept too, and
+ *   the backward does not compute the two projections again.  y is the same,
+ *   bit for bit, with saved8 or without.
+ */
+typedef struct {
+  seg_act8 x, y1;       /* [P, H] */
+  seg_act8 q, o;        /* [P, hq * d] */
+  seg_act8 k, v;        /* [P, hkv * d] */
+  seg_act8 g, u;        /* [P, I], or code NULL */
+  float *lse;           /* [hq, P] */
+  float *rstd1, *rstd2; /* [P] */
+} seg_layer_saved8;
+typedef struct {
+  const seg_mrope_cfg *rope;      /* NULL: one axis */
+  const int32_t *pos;             /* device [3, P], with rope */
+  const seg_layer_saved8 *saved8; /* NULL: `saved` in bf16 */
+} seg_layer_ext;
+
+size_t seg_layer_ext_workspace_bytes(const seg_sizes *sz, const seg_layer_cfg *cfg,
+                                     int32_t saved8, int32_t bwd);
+seg_status seg_layer_fwd_ext(const seg_layout *L, const seg_sizes *sz, const seg_layer_cfg *cfg,
+                             const seg_layer_ext *ext, const seg_layer_weights *w, const void *x,
+                             void *y, const seg_layer_saved *saved, void *ws, size_t ws_bytes,
+                             hipStream_t stream);
+seg_status seg_layer_bwd_ext(const seg_layout *L, const seg_sizes *sz, const seg_layer_cfg *cfg,
+                             const seg_layer_ext *ext, const seg_layer_weights *w, const void *x,
+                             const seg_layer_saved *saved, const void *dy, void *dx,
+                             const seg_layer_grads *g, void *ws, size_t ws_bytes,
+                             hipStream_t stream);
+
+/*
  * Kernel timing.  While enabled, every kernel the library launches is
  * bracketed by HIP events recorded on its launch stream.  seg_profile_read sums
  * the device time of all recorded launches of one kernel (names: "layout",
  * "attn_prep", "attn_fwd", "attn_delta" (fp32 inputs only: with bf16 inputs
  * the dQ kernel forms Delta itself), "attn_bwd_dkdv", "attn_bwd_dq", "logits", "row_loss", "dz", "lp_prep", "dh", "dw", and for the layer
- * "ly_norm", "ly_rope", "ly_proj", "ly_mlp", "ly_wgrad", "ly_misc"; "mrope_pos", "mrope", "act_pack",
+ * "ly_norm", "ly_rope", "ly_proj", "ly_mlp", "ly_wgrad", "ly_misc", "ly_act8"; "mrope_pos", "mrope", "act_pack",
  * "act_unpack", "glu_fwd", "glu_act", "glu_dx", "glu_dw"), waiting for them to
  * finish; seg_profile_reset forgets the records.  Timing adds two event
  * records per launch and is off by default.  These three calls are the one

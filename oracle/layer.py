@@ -89,10 +89,11 @@ class Weights:
         self.__dict__.update(kw)
 
 
-def forward(x, w, segments, masks, hq, hkv, d, eps, base):
+def forward(x, w, segments, masks, hq, hkv, d, eps, base, rot=None):
     """x [P, H] (padding rows are carried through unchanged apart from the
     residual path), masks: one visibility mask per segment.  Returns y and
-    the saved intermediates."""
+    the saved intermediates.  rot(x, inverse): the rotation of all rows, in place
+    of the rotary embedding by the row in the segment."""
     P = x.shape[0]
     pos = segment_positions(segments, P)
     a, r1 = rms_forward(x, w.g1, eps)
@@ -100,7 +101,8 @@ def forward(x, w, segments, masks, hq, hkv, d, eps, base):
     k = (a @ w.wk.T).reshape(P, hkv, d)
     v = (a @ w.wv.T).reshape(P, hkv, d)
     pz = np.maximum(pos, 0)
-    qr, kr = rope(q, pz, base), rope(k, pz, base)
+    rot = rot or (lambda t, inverse: rope(t, pz, base, inverse))
+    qr, kr = rot(q, False), rot(k, False)
     o = np.zeros((P, hq, d))
     lse = np.zeros((hq, P))
     scale = 1.0 / np.sqrt(d)
@@ -117,7 +119,7 @@ def forward(x, w, segments, masks, hq, hkv, d, eps, base):
     return y, saved
 
 
-def backward(x, w, segments, masks, hq, hkv, d, eps, base, saved, dy):
+def backward(x, w, segments, masks, hq, hkv, d, eps, base, saved, dy, rot=None):
     """Gradients of sum(y * dy) over the segment rows: dx and the weight
     gradients (a dict).  Padding rows carry no gradient (their dy counts as 0)."""
     P = x.shape[0]
@@ -146,8 +148,9 @@ def backward(x, w, segments, masks, hq, hkv, d, eps, base, saved, dy):
         dq[rows], dk[rows], dv[rows] = OA.backward(s["qr"][rows], s["kr"][rows], s["v"][rows],
                                                     m, scale, do[rows])
     pz = np.maximum(s["pos"], 0)
-    dq = rope(dq, pz, base, inverse=True).reshape(P, hq * d)
-    dk = rope(dk, pz, base, inverse=True).reshape(P, hkv * d)
+    rot = rot or (lambda t, inverse: rope(t, pz, base, inverse))
+    dq = rot(dq, True).reshape(P, hq * d)
+    dk = rot(dk, True).reshape(P, hkv * d)
     dv = dv.reshape(P, hkv * d)
     grads["wq"] = dq.T @ s["a"]
     grads["wk"] = dk.T @ s["a"]

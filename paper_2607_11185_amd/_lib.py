@@ -28,7 +28,8 @@ EXPORTS = ["seg_layout_query", "seg_build_layout", "seg_attn_workspace_bytes", "
            "seg_layer_workspace_bytes", "seg_layer_fwd", "seg_layer_bwd",
            "seg_mrope_positions_workspace_bytes", "seg_mrope_positions", "seg_mrope_fwd",
            "seg_mrope_bwd", "seg_act_pack", "seg_act_unpack", "seg_glu_fwd",
-           "seg_glu_workspace_bytes", "seg_glu_bwd", "seg_profile_enable",
+           "seg_glu_workspace_bytes", "seg_glu_bwd", "seg_layer_ext_workspace_bytes",
+           "seg_layer_fwd_ext", "seg_layer_bwd_ext", "seg_profile_enable",
            "seg_profile_reset", "seg_profile_read", "seg_last_error"]
 
 P32 = ctypes.POINTER(ctypes.c_int32)
@@ -103,6 +104,18 @@ class SegMropeCfg(ctypes.Structure):
 
 class SegAct8(ctypes.Structure):
     _fields_ = [("code", VP), ("exp", VP)]
+
+
+SAVED8 = ("x", "y1", "q", "o", "k", "v", "g", "u")
+
+
+class SegLayerSaved8(ctypes.Structure):
+    _fields_ = [(n, SegAct8) for n in SAVED8] + [("lse", VP), ("rstd1", VP), ("rstd2", VP)]
+
+
+class SegLayerExt(ctypes.Structure):
+    _fields_ = [("rope", ctypes.POINTER(SegMropeCfg)), ("pos", VP),
+                ("saved8", ctypes.POINTER(SegLayerSaved8))]
 
 
 class SegError(RuntimeError):
@@ -190,6 +203,14 @@ def lib() -> ctypes.CDLL:
         L.seg_glu_bwd.restype = ctypes.c_int
         L.seg_glu_bwd.argtypes = [i32, i32, i32, VP, i64, VP, VP, act8, act8, VP, VP, VP, dtype, VP, VP,
                                   VP, size, VP]
+        layer = [ctypes.POINTER(SegLayout), ctypes.POINTER(SegSizes), ctypes.POINTER(SegLayerCfg),
+                 ctypes.POINTER(SegLayerExt), ctypes.POINTER(SegLayerWeights), VP]
+        L.seg_layer_ext_workspace_bytes.restype = size
+        L.seg_layer_ext_workspace_bytes.argtypes = [*layer[1:3], i32, i32]
+        L.seg_layer_fwd_ext.restype = L.seg_layer_bwd_ext.restype = ctypes.c_int
+        L.seg_layer_fwd_ext.argtypes = [*layer, VP, ctypes.POINTER(SegLayerSaved), VP, size, VP]
+        L.seg_layer_bwd_ext.argtypes = [*layer, ctypes.POINTER(SegLayerSaved), VP, VP,
+                                        ctypes.POINTER(SegLayerGrads), VP, size, VP]
         L.seg_profile_enable.restype = None
         L.seg_profile_enable.argtypes = [ctypes.c_int32]
         L.seg_profile_reset.restype = None

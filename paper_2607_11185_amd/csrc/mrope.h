@@ -2,6 +2,8 @@
 // the decoder layer.
 #pragma once
 
+#include <cmath>
+
 #include "common.h"
 
 namespace seg {
@@ -30,6 +32,12 @@ struct Args {
   const int32_t *pad;
   unsigned short *zero;
   int zero_width;
+
+  void set(const seg_mrope_cfg &c) {
+    s0 = c.sections[0];
+    s01 = s0 + c.sections[1];
+    log2_base = std::log2((double)c.base);
+  }
 };
 
 // sections, base, head counts and head size as seg_mrope_fwd takes them

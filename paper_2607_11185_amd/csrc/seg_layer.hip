@@ -12,8 +12,11 @@
 // through fixed-order partial sums, so results are bitwise reproducible.
 #include <cmath>
 
+#include "act8.h"
 #include "common.h"
 #include "gemm.h"
+#include "glu.h"
+#include "mrope.h"
 
 extern "C" seg_status seg_attn_fwd(const seg_layout *, const seg_sizes *, seg_dtype, int32_t,
                                    int32_t, int32_t, float, const void *, const void *,
@@ -288,111 +291,6 @@ __global__ void __launch_bounds__(256) k_zero_pad(unsigned short *__restrict__ x
         *reinterpret_cast<u16x8 *>(x + row * W + c * 8) = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
 }
 
-__device__ __forceinline__ float sigmoidf_(float g) { return 1.f / (1.f + __expf(-g)); }
-
-// Gate and up projections side by side: block j of 64 rows of wgu holds
-// wg rows 32j..32j+31 then wu rows 32j..32j+31 (zero rows past I), so one
-// GEMM against wgu gives, in each 64-column wave tile, the gate and up
-// values of the same 32 features.  Grid-stride over 16-byte chunks.
-constexpr int GU_BLOCK = 32;
-
-__global__ void k_interleave_gu(const unsigned short *__restrict__ wg,
-                                const unsigned short *__restrict__ wu, int I, int H, long rows2,
-                                unsigned short *__restrict__ wgu) {
-  const long h8 = H / 8, n = rows2 * h8;
-  for (long c = (long)blockIdx.x * blockDim.x + threadIdx.x; c < n; c += (long)gridDim.x * blockDim.x) {
-    const long R = c / h8, k = (c - R * h8) * 8;
-    const long j = R / (2 * GU_BLOCK), w = R % (2 * GU_BLOCK);
-    const long f = j * GU_BLOCK + (w % GU_BLOCK);
-    u16x8 v = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
-    if (f < I) v = *reinterpret_cast<const u16x8 *>((w < GU_BLOCK ? wg : wu) + f * H + k);
-    *reinterpret_cast<u16x8 *>(wgu + R * H + k) = v;
-  }
-}
-
-// Epilogue of the GEMM against wgu: m = silu(g) * u for the wave's 32
-// features, in fp32 from the accumulators (columns 0..31 of the wave tile hold
-// the gate, 32..63 the up values of the same features); with g and u set,
-// also stores the gate and up values (the backward's recompute).  Outputs are
-// workspace arrays [rows][ld] bf16 at feature columns, ld a multiple of 8.  32
-// rows x 32 features at a time go through the wave's LDS, so a lane stores 8
-// features (16 bytes) of a row.
-struct EpiSwiGLU {
-  static constexpr bool kSwap = true;
-  unsigned short *m, *g, *u;
-  long ld;
-  int I;
-  template <int NI, int NJ>
-  __device__ __forceinline__ void operator()(const f32x4 (&acc)[NI][NJ],
-                                             const gemm::Tile &t) const {
-    static_assert(NJ == 4, "SwiGLU epilogue expects 64-column wave tiles");
-    const int lane = t.grp * 16 + t.col, q = lane & 3;
-    const int f = (t.n0 + t.wc) / 2 + q * 8;  // the lane's features when storing
-    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-    // [3 outputs][32 rows][8 chunks of 4 features] (2 KB each), chunk c of row
-    // r in slot c ^ (r & 6): pairs of chunks stay together
-    gemm::u32x2 *w = reinterpret_cast<gemm::u32x2 *>(t.lds);
-#pragma unroll
-    for (int bm = 0; bm < NI / 2; ++bm) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const f32x4 gv = acc[bm * 2 + i][j], uv = acc[bm * 2 + i][j + 2];
-          float mv[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) mv[r] = gv[r] * sigmoidf_(gv[r]) * uv[r];
-          const int at = (i * 16 + t.col) * 8 + ((j * 4 + t.grp) ^ (t.col & 6));
-          w[at] = gemm::u32x2{gemm::pack2(mv[0], mv[1]), gemm::pack2(mv[2], mv[3])};
-          if (g) {
-            w[256 + at] = gemm::u32x2{gemm::pack2(gv[0], gv[1]), gemm::pack2(gv[2], gv[3])};
-            w[512 + at] = gemm::u32x2{gemm::pack2(uv[0], uv[1]), gemm::pack2(uv[2], uv[3])};
-          }
-        }
-      __builtin_amdgcn_wave_barrier();
-      if (f < I) {  // I is a multiple of 8
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const int r = p * 16 + (lane >> 2), row = t.m0 + t.wr + bm * 32 + r;
-          const int at = r * 8 + ((2 * q) ^ (r & 6));
-          if (row < t.M) {
-            const long off = (long)row * ld + f;
-            *reinterpret_cast<u32x4 *>(m + off) = *reinterpret_cast<const u32x4 *>(w + at);
-            if (g) {
-              *reinterpret_cast<u32x4 *>(g + off) = *reinterpret_cast<const u32x4 *>(w + 256 + at);
-              *reinterpret_cast<u32x4 *>(u + off) = *reinterpret_cast<const u32x4 *>(w + 512 + at);
-            }
-          }
-        }
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
-  }
-};
-
-// dg = dm * u * silu'(g), du = dm * silu(g), silu'(g) = s (1 + g (1 - s)),
-// s = sigmoid(g) (8 elements per thread).  A streaming kernel: folded into the
-// dm GEMM's epilogue its loads of g and u stall the one wave per SIMD.
-__global__ void k_swiglu_bwd(const unsigned short *__restrict__ g, const unsigned short *__restrict__ u,
-                             const unsigned short *__restrict__ dm, unsigned short *__restrict__ dg,
-                             unsigned short *__restrict__ du, long n8) {
-  for (long c = (long)blockIdx.x * blockDim.x + threadIdx.x; c < n8; c += (long)gridDim.x * blockDim.x) {
-    const u16x8 gv = *reinterpret_cast<const u16x8 *>(g + c * 8);
-    const u16x8 uv = *reinterpret_cast<const u16x8 *>(u + c * 8);
-    const u16x8 mv = *reinterpret_cast<const u16x8 *>(dm + c * 8);
-    u16x8 og, ou;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float gf = bf_bits2f(gv[j]), uf = bf_bits2f(uv[j]), d = bf_bits2f(mv[j]);
-      const float s = sigmoidf_(gf);
-      og[j] = f2bf_bits(d * uf * s * (1.f + gf * (1.f - s)));
-      ou[j] = f2bf_bits(d * gf * s);
-    }
-    *reinterpret_cast<u16x8 *>(dg + c * 8) = og;
-    *reinterpret_cast<u16x8 *>(du + c * 8) = ou;
-  }
-}
-
 // dst[r] = pos[r] >= 0 ? src[r] : 0 for rows of W bf16 values
 __global__ void k_mask_rows(const unsigned short *src, const int32_t *__restrict__ pos, long P, int W,
                             unsigned short *dst) {
@@ -431,14 +329,15 @@ Dims dims_of(const seg_sizes &sz, const seg_layer_cfg &c) {
 }
 
 struct LayerWs {
-  size_t pos, tab, a, m, wgu, sums, attn;                        // forward
+  size_t pos, tab, a, m, sums, attn;                             // forward
   size_t dy1, dO, dq, dk, dv;  // backward
   size_t g, u, dm, dg, du, dbf, part;
+  size_t x, q, k, v, o, y1;  // with 8-bit saved activations: their values
   long sum_elems;
   size_t total;
 };
 
-LayerWs layer_ws(const seg_sizes &sz, const seg_layer_cfg &c, int bwd) {
+LayerWs layer_ws(const seg_sizes &sz, const seg_layer_cfg &c, int bwd, bool packed = false) {
   const Dims m = dims_of(sz, c);
   LayerWs w{};
   size_t off = 0;
@@ -448,17 +347,23 @@ LayerWs layer_ws(const seg_sizes &sz, const seg_layer_cfg &c, int bwd) {
     return o;
   };
   const size_t P = std::max<long>(m.P, 1), C = m.C, H = m.H, I = m.I;
-  const size_t Ip = (I + GU_BLOCK - 1) / GU_BLOCK * GU_BLOCK;
   w.pos = take(P * 4);
   w.tab = take((size_t)std::max(sz.max_seg_len, 1) * (c.d / 2) * sizeof(float2));
   w.a = take(C * H * 2);
   w.m = take(C * I * 2);
-  w.wgu = take(2 * Ip * H * 2);
   // partial sums of products cut over K: what the largest cut product takes, up
   // to 128 MB (larger ones fill the chip uncut); the same for every chunk size
   w.sum_elems = (long)std::min<size_t>(
       (size_t)32 << 20, 16 * std::max(std::max(P, H) * std::max<size_t>(H, m.QD + 2 * m.KD), H * I));
   w.sums = take(w.sum_elems * 4);
+  if (packed) {
+    if (bwd) w.x = take(P * H * 2);
+    w.q = take(P * m.QD * 2);
+    w.k = take(P * m.KD * 2);
+    w.v = take(P * m.KD * 2);
+    w.o = take(P * m.QD * 2);
+    w.y1 = take(P * H * 2);
+  }
   w.attn = take(seg_attn_workspace_bytes(&sz, SEG_BF16, c.hq, c.hkv, c.d, bwd));
   if (bwd) {
     w.dy1 = take(P * H * 2);
@@ -503,21 +408,6 @@ void check_layer(const seg_layout *L, const seg_sizes *sz, const seg_layer_cfg *
 
 #define US(p) reinterpret_cast<unsigned short *>(p)
 #define CUS(p) reinterpret_cast<const unsigned short *>(p)
-
-void build_wgu(const seg_layer_weights &w, int I, int H, unsigned short *wgu, hipStream_t st) {
-  const long rows2 = 2L * ((I + GU_BLOCK - 1) / GU_BLOCK * GU_BLOCK);
-  k_interleave_gu<<<blocks_for(rows2 * (H / 8)), 256, 0, st>>>(CUS(w.wg), CUS(w.wu), I, H, rows2, wgu);
-  SEG_LAUNCH_CHECK();
-}
-
-// rows x [gate | up] of a chunk against the interleaved weights, consumed by
-// the SwiGLU epilogue (which pairs the two 32-column halves of a 64-column
-// wave tile)
-void gate_up(const unsigned short *a, const unsigned short *wgu, int rows, int H, int I,
-             const EpiSwiGLU &ep, hipStream_t st) {
-  const int N = 2 * ((I + GU_BLOCK - 1) / GU_BLOCK * GU_BLOCK);
-  gemm::launch_one<false, false>(a, H, wgu, H, rows, N, H, ep, st);
-}
 
 void rms_fwd(const unsigned short *x, long ldx, const void *g, float eps, int rows, int H,
              const int32_t *pos, unsigned short *y, float *rstd, hipStream_t st) {
@@ -572,22 +462,67 @@ void check_status(seg_status s) {
   if (s != SEG_OK) throw Fail{s};
 }
 
+// What the extended entry points add to the layer.
+struct Ext {
+  const seg_mrope_cfg *rope;       // positions on three axes, or NULL
+  const int32_t *pos;              // [3, P]
+  const seg_layer_saved8 *packed;  // 8-bit saved activations, or NULL
+};
+
+void rotate(const seg_sizes &sz, const seg_layer_cfg &c, const Ext &ext, const RopeArgs &g, float2 *tab,
+            hipStream_t st) {
+  if (!ext.rope) {
+    rope_table(sz, c, tab, st);
+    rope(g, st);
+    return;
+  }
+  mrope::Args r{};
+  r.a = mrope::Heads{g.a, g.a, (long)g.ha * g.d, (long)g.ha * g.d, g.ha};
+  r.b = mrope::Heads{g.b, g.b, (long)g.hb * g.d, (long)g.hb * g.d, g.hb};
+  r.rows = g.P;
+  r.d = g.d;
+  r.inverse = g.inverse;
+  r.set(*ext.rope);
+  r.pos = ext.pos;
+  r.pad = g.pos;
+  r.zero = g.c;
+  r.zero_width = g.hc * g.d;
+  mrope::launch(SEG_BF16, r, st);
+}
+
+// the kept gate and up values from row r0 on (none: codes NULL)
+glu::Kept kept_rows(const Ext &ext, long r0, int I) {
+  glu::Kept k{};
+  if (!ext.packed || !ext.packed->g.code) return k;
+  const long nb = act8::blocks_of(I);
+  k.g8 = seg_act8{ext.packed->g.code + r0 * I, ext.packed->g.exp + r0 * nb};
+  k.u8 = seg_act8{ext.packed->u.code + r0 * I, ext.packed->u.exp + r0 * nb};
+  return k;
+}
+
+void pack(long rows, int cols, const unsigned short *x, const seg_act8 &to, hipStream_t st) {
+  check_status(seg_act_pack(rows, cols, SEG_BF16, x, cols, &to, st));
+}
+
+void unpack(long rows, int cols, const seg_act8 &from, unsigned short *x, hipStream_t st) {
+  check_status(seg_act_unpack(rows, cols, SEG_BF16, &from, x, cols, st));
+}
+
 void layer_fwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cfg &c,
-                    const seg_layer_weights &w, const unsigned short *x, unsigned short *y,
-                    const seg_layer_saved &sv, char *base, const LayerWs &W, size_t ws_bytes,
-                    hipStream_t st) {
+                    const Ext &ext, const seg_layer_weights &w, const unsigned short *x,
+                    unsigned short *y, const seg_layer_saved &sv, char *base, const LayerWs &W,
+                    size_t ws_bytes, hipStream_t st) {
   const Dims m = dims_of(*sz, c);
   const long P = m.P;
   const int H = m.H, I = m.I;
   int32_t *pos = reinterpret_cast<int32_t *>(base + W.pos);
   float2 *tab = reinterpret_cast<float2 *>(base + W.tab);
   const gemm::Scratch sums{reinterpret_cast<float *>(base + W.sums), W.sum_elems};
-  unsigned short *a = US(base + W.a), *mb = US(base + W.m), *wgu = US(base + W.wgu);
+  unsigned short *a = US(base + W.a), *mb = US(base + W.m);
   unsigned short *q = US(sv.q), *k = US(sv.k), *v = US(sv.v), *o = US(sv.o), *y1 = US(sv.y1);
   {
     ProfScope prof("ly_misc", st);
     positions(L, sz, P, pos, st);
-    build_wgu(w, I, H, wgu, st);
   }
   for (long r0 = 0; r0 < P; r0 += m.C) {
     const int cr = (int)std::min<long>(m.C, P - r0);
@@ -605,8 +540,7 @@ void layer_fwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cf
   }
   {
     ProfScope prof("ly_rope", st);
-    rope_table(*sz, c, tab, st);
-    rope(RopeArgs{q, k, nullptr, m.hq, m.hkv, 0, m.d, 0, P, pos, tab}, st);
+    rotate(*sz, c, ext, RopeArgs{q, k, nullptr, m.hq, m.hkv, 0, m.d, 0, P, pos, tab}, tab, st);
   }
   check_status(seg_attn_fwd(L, sz, SEG_BF16, m.hq, m.hkv, m.d, 1.f / std::sqrt((float)m.d), q, k, v,
                             o, sv.lse, base + W.attn, ws_bytes - W.attn, st));
@@ -627,24 +561,34 @@ void layer_fwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cf
       rms_fwd(y1 + r0 * H, H, w.g2, c.rms_eps, cr, H, pos + r0, a, sv.rstd2 + r0, st);
     }
     ProfScope prof("ly_mlp", st);
-    gate_up(a, wgu, cr, H, I, EpiSwiGLU{mb, nullptr, nullptr, I, I}, st);
+    glu::forward(a, H, CUS(w.wg), CUS(w.wu), cr, H, I, mb, kept_rows(ext, r0, I), st);
     gemm::launch_one<false, false>(mb, I, CUS(w.wd), I, cr, H, I,
                                    OutResid::make(y + r0 * H, H, 1.f, y1 + r0 * H, H), sums, P, st);
+  }
+  if (ext.packed) {
+    const seg_layer_saved8 &s8 = *ext.packed;
+    ProfScope prof("ly_act8", st);
+    pack(P, H, x, s8.x, st);
+    pack(P, m.QD, q, s8.q, st);
+    pack(P, m.KD, k, s8.k, st);
+    pack(P, m.KD, v, s8.v, st);
+    pack(P, m.QD, o, s8.o, st);
+    pack(P, H, y1, s8.y1, st);
   }
 }
 
 void layer_bwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cfg &c,
-                    const seg_layer_weights &w, const unsigned short *x, const seg_layer_saved &sv,
-                    const unsigned short *dy, unsigned short *dx, const seg_layer_grads &gr,
-                    char *base, const LayerWs &W, size_t ws_bytes, hipStream_t st) {
+                    const Ext &ext, const seg_layer_weights &w, const unsigned short *x,
+                    const seg_layer_saved &sv, const unsigned short *dy, unsigned short *dx,
+                    const seg_layer_grads &gr, char *base, const LayerWs &W, size_t ws_bytes,
+                    hipStream_t st) {
   const Dims m = dims_of(*sz, c);
   const long P = m.P;
   const int H = m.H, I = m.I;
   int32_t *pos = reinterpret_cast<int32_t *>(base + W.pos);
   float2 *tab = reinterpret_cast<float2 *>(base + W.tab);
   const gemm::Scratch sums{reinterpret_cast<float *>(base + W.sums), W.sum_elems};
-  unsigned short *a = US(base + W.a), *gb = US(base + W.g), *ub = US(base + W.u), *mb = US(base + W.m),
-                 *wgu = US(base + W.wgu);
+  unsigned short *a = US(base + W.a), *mb = US(base + W.m);
   unsigned short *dy1 = US(base + W.dy1), *dO = US(base + W.dO), *dq = US(base + W.dq),
                  *dk = US(base + W.dk), *dv = US(base + W.dv);
   unsigned short *dm = US(base + W.dm), *dgb = US(base + W.dg), *dub = US(base + W.du);
@@ -657,10 +601,19 @@ void layer_bwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cf
     fill32(gr.g1, H, 0u, st);
     fill32(gr.g2, H, 0u, st);
     positions(L, sz, P, pos, st);
-    build_wgu(w, I, H, wgu, st);
     // dy1 starts as dy with the padding rows zeroed
     k_mask_rows<<<blocks_for(P * (H / 8)), 256, 0, st>>>(dy, pos, P, H, dy1);
     SEG_LAUNCH_CHECK();
+  }
+  if (ext.packed) {
+    const seg_layer_saved8 &s8 = *ext.packed;
+    ProfScope prof("ly_act8", st);
+    unpack(P, H, s8.x, US(base + W.x), st);
+    unpack(P, m.QD, s8.q, US(base + W.q), st);
+    unpack(P, m.KD, s8.k, US(base + W.k), st);
+    unpack(P, m.KD, s8.v, US(base + W.v), st);
+    unpack(P, m.QD, s8.o, US(base + W.o), st);
+    unpack(P, H, s8.y1, US(base + W.y1), st);
   }
   // MLP and output projection, chunk by chunk
   for (long r0 = 0; r0 < P; r0 += m.C) {
@@ -672,11 +625,15 @@ void layer_bwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cf
     }
     {
       ProfScope prof("ly_mlp", st);
-      gate_up(a, wgu, cr, H, I, EpiSwiGLU{mb, gb, ub, I, I}, st);  // m, g, u
+      // m, g and u: kept by the forward, or computed again
+      glu::Kept kept = kept_rows(ext, r0, I);
+      if (!kept.g8.code) {
+        kept.g16 = US(base + W.g);
+        kept.u16 = US(base + W.u);
+        glu::forward(a, H, CUS(w.wg), CUS(w.wu), cr, H, I, mb, kept, st);
+      }
       gemm::launch_one<false, true>(dy1c, H, CUS(w.wd), I, cr, I, H, OutBf::make(dm, I), sums, P, st);  // dm = dy wd
-      const long n8 = (long)cr * I / 8;
-      k_swiglu_bwd<<<blocks_for(n8), 256, 0, st>>>(gb, ub, dm, dgb, dub, n8);
-      SEG_LAUNCH_CHECK();
+      glu::backward_act(kept, dm, cr, I, dgb, dub, kept.g8.code ? mb : nullptr, st);
       // db = dg wg + du wu, one sum over both contractions
       gemm::Problems<OutF32, 1, 2> g{{{dgb, dub}}, {{CUS(w.wg), CUS(w.wu)}}, {{I, I}}, {{H, H}}, {I, I},
                                      {cr}, {H}, {OutF32::make(dbf, H)}, {}, 1, 0};
@@ -707,8 +664,7 @@ void layer_bwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cf
                             o, sv.lse, dO, dq, dk, dv, base + W.attn, ws_bytes - W.attn, st));
   {
     ProfScope prof("ly_rope", st);
-    rope_table(*sz, c, tab, st);
-    rope(RopeArgs{dq, dk, dv, m.hq, m.hkv, m.hkv, m.d, 1, P, pos, tab}, st);
+    rotate(*sz, c, ext, RopeArgs{dq, dk, dv, m.hq, m.hkv, m.hkv, m.d, 1, P, pos, tab}, tab, st);
   }
   // q/k/v projections and the first norm, chunk by chunk
   for (long r0 = 0; r0 < P; r0 += m.C) {
@@ -761,39 +717,95 @@ extern "C" void seg_layer_gemm_choice(const seg_sizes *sz, const seg_layer_cfg *
 
 extern "C" size_t seg_layer_workspace_bytes(const seg_sizes *sz, const seg_layer_cfg *cfg,
                                             int32_t bwd) {
+  return seg_layer_ext_workspace_bytes(sz, cfg, 0, bwd);
+}
+
+extern "C" size_t seg_layer_ext_workspace_bytes(const seg_sizes *sz, const seg_layer_cfg *cfg,
+                                                int32_t saved8, int32_t bwd) {
   if (!sz || !cfg || cfg->hidden < 1 || cfg->inter < 1 || cfg->hq < 1 || cfg->hkv < 1 ||
       cfg->d < 1)
     return 0;
-  return layer_ws(*sz, *cfg, bwd ? 1 : 0).total;
+  return layer_ws(*sz, *cfg, bwd ? 1 : 0, saved8 != 0).total;
+}
+
+namespace {
+
+Ext check_ext(const seg_layer_ext *e, const seg_layer_cfg &c) {
+  Ext x{};
+  if (!e) return x;
+  if (e->rope) {
+    mrope::check_cfg(e->rope, c.d);
+    SEG_CHECK(e->pos, SEG_ERR_ARG, "rope without pos");
+  }
+  if (e->saved8) {
+    const seg_act8 *a[] = {&e->saved8->x, &e->saved8->q, &e->saved8->k,
+                           &e->saved8->v, &e->saved8->o, &e->saved8->y1};
+    for (const seg_act8 *p : a) SEG_CHECK(p->code && p->exp, SEG_ERR_ARG, "an 8-bit saved array is NULL");
+    const seg_act8 &g = e->saved8->g, &u = e->saved8->u;
+    SEG_CHECK(!g.code == !u.code && (!g.code || (g.exp && u.exp)), SEG_ERR_ARG,
+              "the gate's and the up values' 8-bit arrays: both or none");
+    SEG_CHECK((reinterpret_cast<uintptr_t>(g.code) | reinterpret_cast<uintptr_t>(u.code)) % 8 == 0,
+              SEG_ERR_UNSUPPORTED, "the gate's and up values' codes must start on 8-byte boundaries");
+    SEG_CHECK(e->saved8->lse && e->saved8->rstd1 && e->saved8->rstd2, SEG_ERR_ARG, "a saved vector is NULL");
+  }
+  x.rope = e->rope;
+  x.pos = e->pos;
+  x.packed = e->saved8;
+  return x;
+}
+
+// bf16 saved activations as the caller's struct says, or those of the workspace with
+// the vectors of the 8-bit struct
+seg_layer_saved saved_of(const Ext &ext, const seg_layer_saved *saved, char *base, const LayerWs &W) {
+  if (!ext.packed) {
+    SEG_CHECK(saved, SEG_ERR_ARG, "saved is NULL");
+    SEG_CHECK(saved->q && saved->k && saved->v && saved->o && saved->lse && saved->y1 &&
+                  saved->rstd1 && saved->rstd2,
+              SEG_ERR_ARG, "a saved-buffer pointer is NULL");
+    return *saved;
+  }
+  return seg_layer_saved{base + W.q,  base + W.k,       base + W.v,         base + W.o, ext.packed->lse,
+                         base + W.y1, ext.packed->rstd1, ext.packed->rstd2};
+}
+
+}  // namespace
+
+extern "C" seg_status seg_layer_fwd_ext(const seg_layout *L, const seg_sizes *sz,
+                                        const seg_layer_cfg *cfg, const seg_layer_ext *ext,
+                                        const seg_layer_weights *w, const void *x, void *y,
+                                        const seg_layer_saved *saved, void *ws, size_t ws_bytes,
+                                        hipStream_t stream) {
+  return guarded([&] {
+    check_layer(L, sz, cfg, w);
+    const Ext e = check_ext(ext, *cfg);
+    const LayerWs W = layer_ws(*sz, *cfg, 0, e.packed != nullptr);
+    SEG_CHECK(ws_bytes >= W.total, SEG_ERR_WORKSPACE, "workspace of %zu bytes < required %zu",
+              ws_bytes, W.total);
+    if (sz->packed_tokens == 0) return;
+    SEG_CHECK(x && y && ws, SEG_ERR_ARG, "x, y or ws is NULL");
+    char *base = static_cast<char *>(ws);
+    layer_fwd_impl(L, sz, *cfg, e, *w, CUS(x), US(y), saved_of(e, saved, base, W), base, W, ws_bytes,
+                   stream);
+  });
 }
 
 extern "C" seg_status seg_layer_fwd(const seg_layout *L, const seg_sizes *sz,
                                     const seg_layer_cfg *cfg, const seg_layer_weights *w,
                                     const void *x, void *y, const seg_layer_saved *saved, void *ws,
                                     size_t ws_bytes, hipStream_t stream) {
-  return guarded([&] {
-    check_layer(L, sz, cfg, w);
-    const LayerWs W = layer_ws(*sz, *cfg, 0);
-    SEG_CHECK(ws_bytes >= W.total, SEG_ERR_WORKSPACE, "workspace of %zu bytes < required %zu",
-              ws_bytes, W.total);
-    if (sz->packed_tokens == 0) return;
-    SEG_CHECK(x && y && saved && ws, SEG_ERR_ARG, "x, y, saved or ws is NULL");
-    SEG_CHECK(saved->q && saved->k && saved->v && saved->o && saved->lse && saved->y1 &&
-                  saved->rstd1 && saved->rstd2,
-              SEG_ERR_ARG, "a saved-buffer pointer is NULL");
-    layer_fwd_impl(L, sz, *cfg, *w, CUS(x), US(y), *saved, static_cast<char *>(ws), W, ws_bytes,
-                   stream);
-  });
+  return seg_layer_fwd_ext(L, sz, cfg, nullptr, w, x, y, saved, ws, ws_bytes, stream);
 }
 
-extern "C" seg_status seg_layer_bwd(const seg_layout *L, const seg_sizes *sz,
-                                    const seg_layer_cfg *cfg, const seg_layer_weights *w,
-                                    const void *x, const seg_layer_saved *saved, const void *dy,
-                                    void *dx, const seg_layer_grads *g, void *ws, size_t ws_bytes,
-                                    hipStream_t stream) {
+extern "C" seg_status seg_layer_bwd_ext(const seg_layout *L, const seg_sizes *sz,
+                                        const seg_layer_cfg *cfg, const seg_layer_ext *ext,
+                                        const seg_layer_weights *w, const void *x,
+                                        const seg_layer_saved *saved, const void *dy, void *dx,
+                                        const seg_layer_grads *g, void *ws, size_t ws_bytes,
+                                        hipStream_t stream) {
   return guarded([&] {
     check_layer(L, sz, cfg, w);
-    const LayerWs W = layer_ws(*sz, *cfg, 1);
+    const Ext e = check_ext(ext, *cfg);
+    const LayerWs W = layer_ws(*sz, *cfg, 1, e.packed != nullptr);
     SEG_CHECK(ws_bytes >= W.total, SEG_ERR_WORKSPACE, "workspace of %zu bytes < required %zu",
               ws_bytes, W.total);
     SEG_CHECK(g && g->g1 && g->wq && g->wk && g->wv && g->wo && g->g2 && g->wg && g->wu && g->wd,
@@ -802,11 +814,18 @@ extern "C" seg_status seg_layer_bwd(const seg_layout *L, const seg_sizes *sz,
       zero_grads(*g, *cfg, stream);
       return;
     }
-    SEG_CHECK(x && saved && dy && dx && ws, SEG_ERR_ARG, "x, saved, dy, dx or ws is NULL");
-    SEG_CHECK(saved->q && saved->k && saved->v && saved->o && saved->lse && saved->y1 &&
-                  saved->rstd1 && saved->rstd2,
-              SEG_ERR_ARG, "a saved-buffer pointer is NULL");
-    layer_bwd_impl(L, sz, *cfg, *w, CUS(x), *saved, CUS(dy), US(dx), *g, static_cast<char *>(ws), W,
+    SEG_CHECK((x || e.packed) && dy && dx && ws, SEG_ERR_ARG, "x, dy, dx or ws is NULL");
+    char *base = static_cast<char *>(ws);
+    const unsigned short *xs = e.packed ? CUS(base + W.x) : CUS(x);
+    layer_bwd_impl(L, sz, *cfg, e, *w, xs, saved_of(e, saved, base, W), CUS(dy), US(dx), *g, base, W,
                    ws_bytes, stream);
   });
+}
+
+extern "C" seg_status seg_layer_bwd(const seg_layout *L, const seg_sizes *sz,
+                                    const seg_layer_cfg *cfg, const seg_layer_weights *w,
+                                    const void *x, const seg_layer_saved *saved, const void *dy,
+                                    void *dx, const seg_layer_grads *g, void *ws, size_t ws_bytes,
+                                    hipStream_t stream) {
+  return seg_layer_bwd_ext(L, sz, cfg, nullptr, w, x, saved, dy, dx, g, ws, ws_bytes, stream);
 }

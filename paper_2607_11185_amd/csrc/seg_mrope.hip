@@ -130,7 +130,6 @@ void launch(seg_dtype dt, const Args &g, hipStream_t st) {
   const int rows_per = std::max(1, std::min(std::min(want, MAX_ROWS), CS / hp));
   const long nb = (g.rows + rows_per - 1) / rows_per;
   SEG_CHECK(nb <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "too many rows for one launch");
-  ProfScope prof("mrope", st);
   if (dt == SEG_BF16) k_mrope<unsigned short><<<(unsigned)nb, 256, 0, st>>>(g, rows_per, hp);
   else k_mrope<float><<<(unsigned)nb, 256, 0, st>>>(g, rows_per, hp);
   SEG_LAUNCH_CHECK();
@@ -168,10 +167,9 @@ seg_status rotate(int64_t rows, seg_dtype dt, const seg_mrope_cfg *cfg, int32_t 
     g.rows = rows;
     g.d = d;
     g.inverse = inverse;
-    g.s0 = cfg->sections[0];
-    g.s01 = g.s0 + cfg->sections[1];
-    g.log2_base = std::log2((double)cfg->base);
+    g.set(*cfg);
     g.pos = pos;
+    ProfScope prof("mrope", stream);
     mrope::launch(dt, g, stream);
   });
 }

@@ -3,7 +3,7 @@
 Functions carry the C names (seg_layout_query, seg_build_layout, seg_attn_fwd,
 seg_attn_bwd, seg_logprob_loss, seg_layer_fwd, seg_layer_bwd, seg_mrope_positions,
 seg_mrope_fwd, seg_mrope_bwd, seg_act_pack, seg_act_unpack, seg_glu_fwd,
-seg_glu_bwd) and only marshal arguments: they allocate
+seg_glu_bwd, seg_layer_fwd_ext, seg_layer_bwd_ext) and only marshal arguments: they allocate
 outputs and workspace with torch on the tensors' device and pass raw
 pointers plus torch's current stream to the library.
 """
@@ -588,3 +588,147 @@ def seg_glu_bwd(x, wg, wu, dm, kept=None, dw_dtype=None, want_m=True, out=None, 
                                      out["dwg"].data_ptr(), out["dwu"].data_ptr(), ws.data_ptr(),
                                      ws.numel(), _stream(dev)))
     return out
+
+
+def _saved8_widths(cfg: LayerCfg) -> dict:
+    return {"x": cfg.hidden, "y1": cfg.hidden, "q": cfg.hq * cfg.d, "o": cfg.hq * cfg.d,
+            "k": cfg.hkv * cfg.d, "v": cfg.hkv * cfg.d, "g": cfg.inter, "u": cfg.inter}
+
+
+def layer_saved8(lay: Layout, cfg: LayerCfg, keep_gate=False) -> dict:
+    """Empty 8-bit saved activations of the layer over `lay` (Act8 by name, and the
+    fp32 vectors lse, rstd1 and rstd2); keep_gate: with the gate and up values."""
+    import torch
+    P, dev = lay.sizes.packed_tokens, lay.device
+    out = {n: Act8.empty(P, c, dev) for n, c in _saved8_widths(cfg).items()
+           if keep_gate or n not in ("g", "u")}
+    out.update(lse=torch.empty((cfg.hq, P), dtype=torch.float32, device=dev),
+               rstd1=torch.empty(P, dtype=torch.float32, device=dev),
+               rstd2=torch.empty(P, dtype=torch.float32, device=dev))
+    return out
+
+
+def _layer_ext(lay, cfg, rope, pos, saved8):
+    """The C struct, and the tensors it points to."""
+    P = lay.sizes.packed_tokens
+    e, tensors = _lib.SegLayerExt(), []
+    if rope is not None:
+        import torch
+        assert pos.shape == (3, P) and pos.dtype == torch.int32 and pos.is_contiguous()
+        e.rope = ctypes.pointer(rope.c())
+        e.pos = pos.data_ptr()
+        tensors.append(pos)
+    if saved8 is not None:
+        want = _saved8_widths(cfg)
+        s = _lib.SegLayerSaved8()
+        for n in _lib.SAVED8:
+            a = saved8.get(n)
+            if a is None:
+                assert n in ("g", "u"), f"saved8 has no {n}"
+                continue
+            assert a.code.shape == (P, want[n]), n
+            setattr(s, n, a.c())
+            tensors += [a.code, a.exp]
+        for n, size in (("lse", cfg.hq * P), ("rstd1", P), ("rstd2", P)):
+            t = saved8[n]
+            assert t.numel() == size and t.is_contiguous() and t.element_size() == 4, n
+            setattr(s, n, t.data_ptr())
+            tensors.append(t)
+        e.saved8 = ctypes.pointer(s)
+    return e, tensors
+
+
+def layer_ext_workspace(lay: Layout, cfg: LayerCfg, saved8: bool, bwd: bool):
+    import torch
+    n = _lib.lib().seg_layer_ext_workspace_bytes(ctypes.byref(lay.sizes), ctypes.byref(cfg.c()),
+                                                 int(saved8), int(bwd))
+    return torch.empty(max(n, 1), dtype=torch.uint8, device=lay.device)
+
+
+def _layer_saved(saved, cfg, P, H, dev):
+    """The bf16 saved buffers (allocated where None) and their C struct."""
+    import torch
+    shapes = {"q": (P, cfg.hq, cfg.d), "k": (P, cfg.hkv, cfg.d), "v": (P, cfg.hkv, cfg.d),
+              "o": (P, cfg.hq, cfg.d), "lse": (cfg.hq, P), "y1": (P, H), "rstd1": (P,), "rstd2": (P,)}
+    f32 = ("lse", "rstd1", "rstd2")
+    if saved is None:
+        saved = {n: torch.empty(s, dtype=torch.float32 if n in f32 else torch.bfloat16, device=dev)
+                 for n, s in shapes.items()}
+    for n, s in shapes.items():
+        assert saved[n].shape == s and saved[n].is_contiguous(), n
+        assert saved[n].dtype == (torch.float32 if n in f32 else torch.bfloat16), n
+    return saved, _lib.SegLayerSaved(*[saved[n].data_ptr() for n in shapes])
+
+
+def _layer_args(lay, cfg, w, x):
+    import torch
+    assert x.shape == (lay.sizes.packed_tokens, cfg.hidden)
+    assert x.dtype == torch.bfloat16 and x.is_contiguous()
+    H, I, QD, KD = cfg.hidden, cfg.inter, cfg.hq * cfg.d, cfg.hkv * cfg.d
+    shapes = {"g1": (H,), "wq": (QD, H), "wk": (KD, H), "wv": (KD, H), "wo": (H, QD), "g2": (H,),
+              "wg": (I, H), "wu": (I, H), "wd": (H, I)}
+    for n in _lib.LAYER_WEIGHTS:
+        assert w[n].shape == shapes[n] and w[n].dtype == torch.bfloat16 and w[n].is_contiguous(), n
+    return [w[n] for n in _lib.LAYER_WEIGHTS]
+
+
+def seg_layer_fwd_ext(lay: Layout, cfg: LayerCfg, w: dict, x, rope: Optional[MropeCfg] = None,
+                      pos=None, saved8=None, y=None, saved=None, ws=None):
+    """seg_layer_fwd with positions on three axes (rope, pos [3, P] int32) and 8-bit
+    saved activations (saved8: layer_saved8's dict, filled here).  Returns (y,
+    saved8), or (y, saved) without saved8."""
+    import torch
+    P, H = x.shape
+    weights = _layer_args(lay, cfg, w, x)
+    e, tensors = _layer_ext(lay, cfg, rope, pos, saved8)
+    if y is None:
+        y = torch.empty_like(x)
+    assert y.shape == x.shape and y.dtype == x.dtype and y.is_contiguous()
+    sv = None
+    if saved8 is None:
+        saved, c = _layer_saved(saved, cfg, P, H, x.device)
+        sv = ctypes.byref(c)
+        tensors += list(saved.values())
+    if ws is None:
+        ws = layer_ext_workspace(lay, cfg, saved8 is not None, False)
+    dev = _device(x, y, ws, *weights, *tensors)
+    with _on(dev):
+        check(_lib.lib().seg_layer_fwd_ext(
+            ctypes.byref(lay.c), ctypes.byref(lay.sizes), ctypes.byref(cfg.c()), ctypes.byref(e),
+            ctypes.byref(_layer_weights(w)), x.data_ptr(), y.data_ptr(), sv, ws.data_ptr(),
+            ws.numel(), _stream(dev)))
+    return y, saved if saved8 is None else saved8
+
+
+def seg_layer_bwd_ext(lay: Layout, cfg: LayerCfg, w: dict, dy, rope: Optional[MropeCfg] = None,
+                      pos=None, saved8=None, x=None, saved=None, dx=None, grads=None, ws=None):
+    """seg_layer_bwd with rope and pos of the forward, from saved8 alone or from x and
+    saved: returns (dx, grads) with fp32 weight gradients by name."""
+    import torch
+    weights = _layer_args(lay, cfg, w, dy)
+    dev, (P, H) = dy.device, dy.shape
+    e, tensors = _layer_ext(lay, cfg, rope, pos, saved8)
+    sv = None
+    if saved8 is None:
+        assert x.shape == dy.shape and x.dtype == dy.dtype and x.is_contiguous()
+        saved, c = _layer_saved(saved, cfg, P, H, dev)
+        sv = ctypes.byref(c)
+        tensors += [x, *saved.values()]
+    if dx is None:
+        dx = torch.empty_like(dy)
+    assert dx.shape == dy.shape and dx.dtype == dy.dtype and dx.is_contiguous()
+    if grads is None:
+        grads = {n: torch.empty(w[n].shape, dtype=torch.float32, device=dev) for n in _lib.LAYER_WEIGHTS}
+    for n in _lib.LAYER_WEIGHTS:
+        assert grads[n].shape == w[n].shape and grads[n].dtype == torch.float32, n
+        assert grads[n].is_contiguous(), n
+    if ws is None:
+        ws = layer_ext_workspace(lay, cfg, saved8 is not None, True)
+    _device(dy, dx, ws, *weights, *tensors, *grads.values())
+    g = _lib.SegLayerGrads(*[grads[n].data_ptr() for n in _lib.LAYER_WEIGHTS])
+    with _on(dev):
+        check(_lib.lib().seg_layer_bwd_ext(
+            ctypes.byref(lay.c), ctypes.byref(lay.sizes), ctypes.byref(cfg.c()), ctypes.byref(e),
+            ctypes.byref(_layer_weights(w)), None if saved8 is not None else x.data_ptr(), sv,
+            dy.data_ptr(), dx.data_ptr(), ctypes.byref(g), ws.data_ptr(), ws.numel(), _stream(dev)))
+    return dx, grads

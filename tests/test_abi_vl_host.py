@@ -13,7 +13,8 @@ from tests.test_abi_host import _lib_or_skip, _prob
 from tests import test_abi_structs as TS
 
 ARG, CAP, WS, UNS = (_lib.SEG_ERR_ARG, _lib.SEG_ERR_CAPACITY, _lib.SEG_ERR_WORKSPACE, _lib.SEG_ERR_UNSUPPORTED)
-STRUCTS = {"seg_mrope_cfg": _lib.SegMropeCfg, "seg_act8": _lib.SegAct8}
+STRUCTS = {"seg_mrope_cfg": _lib.SegMropeCfg, "seg_act8": _lib.SegAct8, "seg_layer_saved8": _lib.SegLayerSaved8,
+           "seg_layer_ext": _lib.SegLayerExt}
 
 
 def test_structures_match_header(tmp_path, monkeypatch):
@@ -149,3 +150,49 @@ def test_gated_block_backward_refuses():
     assert bwd(dm=8) == bwd(m=8) == bwd(dx=8) == bwd(dwg=8) == bwd(dwu=8) == bwd(ws=8) == bwd(dt=3) == UNS
     assert L.seg_glu_fwd(*size, None, None, None, None) == ARG
     assert L.seg_glu_fwd(0, 64, 96, None, 64, None, None, None, None, None, None) == _lib.SEG_OK
+
+
+def test_extended_layer_refuses():
+    L = _lib_or_skip()
+    sz = S.seg_layout_query(_prob())
+    lay = _lib.SegLayout()
+    lay.tile, lay.window = 128, 2
+    cfg = S.LayerCfg(256, 512, 4, 2, 64).c()
+    w = _lib.SegLayerWeights(*([1] * 9))
+    g = _lib.SegLayerGrads(*([1] * 9))
+    sv = _lib.SegLayerSaved(*([1] * 8))
+
+    def size(saved8, bwd):
+        return L.seg_layer_ext_workspace_bytes(ctypes.byref(sz), ctypes.byref(cfg), saved8, bwd)
+    for bwd in (0, 1):
+        assert size(0, bwd) == L.seg_layer_workspace_bytes(ctypes.byref(sz), ctypes.byref(cfg), bwd) < size(1, bwd)
+    assert L.seg_layer_ext_workspace_bytes(None, ctypes.byref(cfg), 1, 0) == 0
+
+    def both(e, want, saved=sv, x=1, n=1 << 40):
+        e, saved = (None if v is None else ctypes.byref(v) for v in (e, saved))
+        head = (ctypes.byref(lay), ctypes.byref(sz), ctypes.byref(cfg), e, ctypes.byref(w), x)
+        assert L.seg_layer_fwd_ext(*head, 1, saved, 1, n, None) == want
+        assert L.seg_layer_bwd_ext(*head, saved, 1, 1, ctypes.byref(g), 1, n, None) == want
+
+    def ext(sections=(8, 12, 12), base=1e4, pos=1, drop=(), gate=True, code=8):
+        e = _lib.SegLayerExt()
+        if sections:
+            e.rope = ctypes.pointer(_lib.SegMropeCfg((ctypes.c_int32 * 3)(*sections), base))
+        e.pos = pos
+        s = _lib.SegLayerSaved8()
+        for n in _lib.SAVED8:
+            if gate or n not in ("g", "u"):
+                setattr(s, n, _lib.SegAct8(None if n in drop else code, None if n + ".exp" in drop else 1))
+        for n in ("lse", "rstd1", "rstd2"):
+            setattr(s, n, None if n in drop else 1)
+        e.saved8 = ctypes.pointer(s)
+        return e
+    for bad in (dict(sections=(8, 12, 13)), dict(sections=(40, -4, -4)), dict(base=1.0), dict(pos=None), dict(drop=("g",)),
+                dict(drop=("u",)), dict(drop=("u.exp",)), *(dict(drop=(n,)) for n in ("x", "q", "k", "v", "o", "y1", "lse", "rstd2")),
+                dict(drop=("y1.exp",), gate=False)):
+        both(ext(**bad), ARG)
+    both(ext(code=4), UNS)
+    both(ext(), WS, n=size(1, 0) - 1)
+    both(ext(sections=None, gate=False), WS, n=size(1, 0) - 1)
+    both(None, ARG, saved=None)              # nothing to save into
+    both(_lib.SegLayerExt(), ARG, x=None)

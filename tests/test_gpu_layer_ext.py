@@ -1,0 +1,236 @@
+"""The decoder layer with positions on three axes and 8-bit saved activations
+(seg_layer_fwd_ext / seg_layer_bwd_ext): against the float64 oracle layer, and
+against the parts it is made of, bit for bit."""
+import numpy as np
+import pytest
+
+from oracle import act8 as OA8
+from oracle import layer as OLY
+from oracle import layout as OL
+from oracle import mrope as OM
+from paper_2607_11185_amd import _lib
+from paper_2607_11185_amd import seg as S
+from paper_2607_11185_amd import workload as WL
+from tests.gpu_helpers import TOL, rel, say, vis_window
+from tests.test_gpu_layer import BASE, EPS, MED, LayerRun, _np
+
+pytestmark = pytest.mark.gpu
+
+# screenshots of 150 tokens are 10 x 15 patches, or clips of 2 frames of 5 x 15
+CASES = {
+    "d64_gqa2_ragged": (MED, 328, 200, 0, (8, 12, 12)),
+    "d128_chunked": (MED.with_(head_dim=128, seed=1), 256, 688, 300, (16, 24, 24)),
+    "d64_gqa4_buffers": (MED.with_(hq=8, hkv=2, buffer_tokens=1400, seed=2, steps=(3, 5)), 384, 520, 512, (32, 0, 0)),
+    "anchored_k2_d3": (MED.with_(mode="anchored", window=2, seg_steps=3, seed=4, steps=(8, 9)), 264, 320, 0, (0, 5, 27)),
+}
+
+
+class ExtRun(LayerRun):
+    def __init__(self, cfg, H, I, chunk, sections):
+        import torch
+        super().__init__(cfg, H, I, chunk)
+        rng = np.random.default_rng(cfg.seed)
+        n = self.run.spans.num_steps
+        self.grid = np.where((rng.random(n) < 0.5)[:, None], [[1, 10, 15, 1]], [[2, 5, 15, 3]]).astype(np.int32)
+        self.rope = S.MropeCfg(sections, BASE)
+        self.pos = S.seg_mrope_positions(self.run.problem, self.lay, self.grid)
+        # what lies in padding rows does not count
+        pad = torch.from_numpy(self.run.host["tok_src"] < 0).to(self.dev)
+        self.pad = pad
+        self.x[pad] = float("nan")
+        self.dy[pad] = float("inf")
+        self.pos[:, pad] = 77
+
+    def oracle_parts(self):
+        c = self.cfg
+        ref = OL.build(self.run.spans, c.window, c.seg_steps, 128, c.max_seg_tokens, c.buffer_tokens, with_tiles=False,
+                       mode=c.mode)
+        pos = np.maximum(OM.positions(ref, self.run.spans, self.grid, ref.packed_tokens), 0)
+        x = WL.layer_rows_np(self.seed, "x", self.src, self.H)
+        x[ref.tok_src < 0] = 0
+        dy = WL.layer_rows_np(self.seed, "dy", np.arange(self.P), self.H)
+        w = OLY.Weights(**WL.layer_weights_np(self.seed, self.H, self.I, c.hq, c.hkv, c.head_dim))
+        masks = [OL.visibility(sg, vis_window(c)) for sg in ref.segments]
+        a = dict(hq=c.hq, hkv=c.hkv, d=c.head_dim, eps=EPS, base=BASE,
+                 rot=lambda t, inverse: OM.rotate(t, pos, self.rope.sections, BASE, inverse))
+        return x, w, ref, masks, a, dy
+
+
+def _rows(pad, t):
+    return t[~pad]
+
+
+@pytest.mark.parametrize("name", list(CASES))
+def test_three_axes_full_parity(name):
+    """y, dx and all weight gradients against the oracle with three-axis rotation."""
+    say(name)
+    lr = ExtRun(*CASES[name])
+    y, saved = S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, lr.rope, lr.pos)
+    dx, grads = S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, lr.dy, lr.rope, lr.pos, x=lr.x, saved=saved)
+    x, w, ref, masks, a, dy = lr.oracle_parts()
+    y_ref, sv = OLY.forward(x, w, ref.segments, masks, **a)
+    dx_ref, g_ref = OLY.backward(x, w, ref.segments, masks, **a, saved=sv, dy=dy)
+    ok = ref.tok_src >= 0
+    assert rel(_np(y)[ok], y_ref[ok]) < TOL and rel(_np(saved["q"])[ok], sv["qr"][ok]) < TOL
+    assert rel(_np(dx)[ok], dx_ref[ok]) < TOL and not dx[lr.pad].any()
+    for n in _lib.LAYER_WEIGHTS:
+        assert rel(_np(grads[n]), g_ref[n]) < TOL, n
+
+
+@pytest.mark.parametrize("keep_gate", [False, True])
+@pytest.mark.parametrize("name", list(CASES))
+def test_saved_in_8_bits(name, keep_gate):
+    """The forward's output is that without; what is kept is the packed form of what the
+    layer saves in bf16; the backward is the layer's on the kept values: bit for bit
+    where the gate and up values are computed again, against the oracle on the same kept
+    values where they are kept."""
+    import torch
+    say(name, keep_gate)
+    lr = ExtRun(*CASES[name])
+    H = lr.H
+    y, saved = S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, lr.rope, lr.pos)
+    s8 = S.layer_saved8(lr.lay, lr.lc, keep_gate)
+    y8, back = S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, lr.rope, lr.pos, saved8=s8)
+    assert back is s8 and torch.equal(_rows(lr.pad, y8), _rows(lr.pad, y))
+    for n in ("lse", "rstd1", "rstd2"):
+        t, u = (s8[n], saved[n]) if n != "lse" else (s8[n].T, saved[n].T)
+        assert torch.equal(_rows(lr.pad, t), _rows(lr.pad, u)), n
+    for n in ("x", "q", "k", "v", "o", "y1"):
+        t = lr.x if n == "x" else saved[n].reshape(lr.P, -1)
+        want = S.seg_act_pack(t)
+        assert torch.equal(_rows(lr.pad, s8[n].code), _rows(lr.pad, want.code)), n
+        assert torch.equal(_rows(lr.pad, s8[n].exp), _rows(lr.pad, want.exp)), n
+    dx, grads = S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, lr.dy, lr.rope, lr.pos, saved8=s8)
+    c = lr.cfg
+    val = {n: S.seg_act_unpack(s8[n]) for n in ("x", "q", "k", "v", "o", "y1")}
+    if not keep_gate:
+        sv = {"q": val["q"].view(lr.P, c.hq, -1), "k": val["k"].view(lr.P, c.hkv, -1), "v": val["v"].view(lr.P, c.hkv, -1),
+              "o": val["o"].view(lr.P, c.hq, -1), "y1": val["y1"], **{n: s8[n] for n in ("lse", "rstd1", "rstd2")}}
+        dx1, g1 = S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, lr.dy, lr.rope, lr.pos, x=val["x"], saved=sv)
+        assert torch.equal(dx, dx1)
+        for n in _lib.LAYER_WEIGHTS:
+            assert torch.equal(grads[n], g1[n]), n
+        return
+    x, w, ref, masks, a, dy = lr.oracle_parts()
+    ok = ref.tok_src >= 0
+
+    def f(t, *shape):
+        t = _np(t)
+        t[~ok] = 0
+        return t.reshape(lr.P, *shape) if shape else t
+    pos = OLY.segment_positions(ref.segments, lr.P)
+    r1, r2 = (np.where(ok, _np(s8[n]), 0) for n in ("rstd1", "rstd2"))
+    sv = dict(pos=pos, a=f(val["x"]) * r1[:, None] * w.g1, r1=r1, qr=f(val["q"], c.hq, c.head_dim), kr=f(val["k"], c.hkv, c.head_dim),
+              v=f(val["v"], c.hkv, c.head_dim), o=f(val["o"], c.hq, c.head_dim), y1=f(val["y1"]),
+              b=f(val["y1"]) * r2[:, None] * w.g2, r2=r2, gt=f(S.seg_act_unpack(s8["g"])), ut=f(S.seg_act_unpack(s8["u"])))
+    sv["mm"] = OLY.silu(sv["gt"]) * sv["ut"]
+    dx_ref, g_ref = OLY.backward(f(val["x"]), w, ref.segments, masks, **a, saved=sv, dy=dy)
+    # the layer forms rstd from the kept x and y1 again, and the scores from the kept q and k
+    # against the forward's lse: both are off by at most the 8 bits' 1 % of a value
+    assert rel(_np(dx)[ok], dx_ref[ok]) < 2 * TOL and not dx[lr.pad].any()
+    for n in _lib.LAYER_WEIGHTS:
+        assert rel(_np(grads[n]), g_ref[n]) < 2 * TOL, n
+
+
+def test_gradients_next_to_those_in_bf16():
+    """What 8 bits cost: gradients against the layer's own in bf16.  Each kept value is off by
+    at most 1 / 127 of its block's largest, about 1 % of a value of normal blocks, and six
+    of them enter a gradient: below 6 %."""
+    lr = ExtRun(*CASES["d128_chunked"])
+    y, saved = S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, lr.rope, lr.pos)
+    dx, grads = S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, lr.dy, lr.rope, lr.pos, x=lr.x, saved=saved)
+    for keep in (False, True):
+        s8 = S.layer_saved8(lr.lay, lr.lc, keep)
+        S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, lr.rope, lr.pos, saved8=s8)
+        dx8, g8 = S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, lr.dy, lr.rope, lr.pos, saved8=s8)
+        assert rel(_np(dx8), _np(dx)) < 0.06
+        for n in _lib.LAYER_WEIGHTS:
+            say(keep, n, rel(_np(g8[n]), _np(grads[n])))
+            assert rel(_np(g8[n]), _np(grads[n])) < 0.06, n
+
+
+def test_without_extensions_it_is_the_layer():
+    import torch
+    lr = LayerRun(*CASES["d64_gqa4_buffers"][:4])
+    y, saved, dx, grads = lr.gpu()
+    y2, saved2 = S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x)
+    dx2, grads2 = S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, lr.dy, x=lr.x, saved=saved2)
+    pad = torch.from_numpy(lr.run.host["tok_src"] < 0).to(lr.dev)
+    assert torch.equal(_rows(pad, y), _rows(pad, y2)) and torch.equal(dx, dx2)
+    assert all(torch.equal(grads[n], grads2[n]) for n in grads)
+
+
+def test_three_axes_all_equal_are_the_row():
+    """Positions equal to the row in the segment on every axis: the layer's own embedding, up
+    to the last bits of its angles (fp32 sines of two roundings)."""
+    lr = ExtRun(*CASES["d128_chunked"])
+    row = OLY.segment_positions(OL.build(lr.run.spans, lr.cfg.window, lr.cfg.seg_steps, 128, with_tiles=False).segments, lr.P)
+    import torch
+    pos = torch.from_numpy(np.stack([row] * 3).astype(np.int32)).to(lr.dev)
+    y, saved = S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, S.MropeCfg((16, 24, 24), BASE), pos)
+    y2, saved2 = S.seg_layer_fwd(lr.lay, lr.lc, lr.w, lr.x)
+    assert rel(_np(saved["q"]), _np(saved2["q"])) < 2.0 ** -9 and rel(_np(y), _np(y2)) < 2.0 ** -8
+
+
+def test_chunking_leaves_what_is_kept_unchanged():
+    import torch
+    cfg, H, I, _, sections = CASES["d64_gqa4_buffers"]
+    kept = []
+    for chunk in (0, 97):
+        lr = ExtRun(cfg, H, I, chunk, sections)
+        s8 = S.layer_saved8(lr.lay, lr.lc, True)
+        y, _ = S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, lr.rope, lr.pos, saved8=s8)
+        kept.append((y, s8))
+    pad = lr.pad
+    assert torch.equal(_rows(pad, kept[0][0]), _rows(pad, kept[1][0]))
+    for n in _lib.SAVED8:
+        for f in ("code", "exp"):
+            assert torch.equal(_rows(pad, getattr(kept[0][1][n], f)), _rows(pad, getattr(kept[1][1][n], f))), (n, f)
+
+
+def test_capture_and_replay_of_the_operators_together():
+    """Rotation, packing, the gated block and the extended layer in one graph, replayed
+    between eager work: every replay equals the eager run."""
+    import torch
+    lr = ExtRun(*CASES["d64_gqa4_buffers"])
+    H, I = lr.H, lr.I
+    x2 = torch.randn(150, H, device=lr.dev, generator=torch.Generator(device=lr.dev).manual_seed(3)).to(torch.bfloat16)
+    dm = torch.randn(150, I, device=lr.dev, generator=torch.Generator(device=lr.dev).manual_seed(4)).to(torch.bfloat16)
+    qk = torch.randn(150, 6, 64, device=lr.dev, generator=torch.Generator(device=lr.dev).manual_seed(5))
+    pos = lr.pos[:, :150].contiguous()
+
+    def step():
+        s8 = S.layer_saved8(lr.lay, lr.lc, True)
+        y, _ = S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, lr.rope, lr.pos, saved8=s8)
+        dx, grads = S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, lr.dy, lr.rope, lr.pos, saved8=s8)
+        q, k = S.seg_mrope_fwd(qk[:, :4], qk[:, 4:], pos, lr.rope)
+        xv = S.seg_act_unpack(S.seg_act_pack(x2))
+        m, kept = S.seg_glu_fwd(xv, lr.w["wg"], lr.w["wu"], keep=True)
+        g = S.seg_glu_bwd(xv, lr.w["wg"], lr.w["wu"], dm, kept)
+        return {"y": y, "dx": dx, "q": q, "k": k, "xv": xv, "m": m, **{"l" + n: t for n, t in grads.items()},
+                **{"b" + n: t for n, t in g.items()}}
+    eager = {n: t.clone() for n, t in step().items()}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    scratch = torch.randn(1 << 20, device=lr.dev)
+    for rep in range(3):
+        scratch.mul_(1.0001).add_(0.5)
+        torch.cuda.synchronize()
+        for t in out.values():
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for n, t in out.items():
+            if n == "y":
+                t, e = _rows(lr.pad, t), _rows(lr.pad, eager[n])
+            else:
+                e = eager[n]
+            assert torch.equal(t, e), (rep, n)
+        say("replay", rep)
