@@ -448,10 +448,13 @@ seg_status seg_act_unpack(int64_t rows, int32_t cols, seg_dtype dt, const seg_ac
  */
 seg_status seg_glu_fwd(int32_t rows, int32_t hidden, int32_t inter, const void *x, int64_t ldx,
                        const void *wg, const void *wu, void *m, const seg_act8 *g8,
-                       const seg_act8 *u8, hipStream_t stream);
+                       const seg_act8 *u8, void *ws, size_t ws_bytes, hipStream_t stream);
 
-/* Workspace of seg_glu_bwd; kept: whether it is given g8 and u8. */
-size_t seg_glu_workspace_bytes(int32_t rows, int32_t hidden, int32_t inter, int32_t kept);
+/* Workspace of seg_glu_fwd (bwd = 0) or seg_glu_bwd (bwd = 1; kept: whether it
+ * is given g8 and u8): partial sums, and in the backward dg and du (without g8
+ * and u8 also g, u and m).  0 for sizes out of range. */
+size_t seg_glu_workspace_bytes(int32_t rows, int32_t hidden, int32_t inter, int32_t bwd,
+                               int32_t kept);
 
 /*
  * Backward of seg_glu_fwd: given dm [rows, inter], the gradients of sum(m * dm),

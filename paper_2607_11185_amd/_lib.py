@@ -197,9 +197,9 @@ def lib() -> ctypes.CDLL:
         L.seg_act_pack.argtypes = [i64, i32, dtype, VP, i64, act8, VP]
         L.seg_act_unpack.argtypes = [i64, i32, dtype, act8, VP, i64, VP]
         L.seg_glu_fwd.restype = ctypes.c_int
-        L.seg_glu_fwd.argtypes = [i32, i32, i32, VP, i64, VP, VP, VP, act8, act8, VP]
+        L.seg_glu_fwd.argtypes = [i32, i32, i32, VP, i64, VP, VP, VP, act8, act8, VP, size, VP]
         L.seg_glu_workspace_bytes.restype = size
-        L.seg_glu_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.seg_glu_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
         L.seg_glu_bwd.restype = ctypes.c_int
         L.seg_glu_bwd.argtypes = [i32, i32, i32, VP, i64, VP, VP, act8, act8, VP, VP, VP, dtype, VP, VP,
                                   VP, size, VP]

@@ -372,7 +372,8 @@ __device__ __forceinline__ void tile_of(int idx, int nM, int nN, int &mt, int &n
 // K a multiple of 8; 256 * ld * 2 < 2^30 (N), 64 * ld * 2 < 2^31 (T).  The
 // steps of 64 of the K ranges, in order, may be cut into `splits` parts of
 // `part` steps, each a set of tiles of its own: the epilogue then gets partial
-// sums.
+// sums.  A launch of a rest (Rest below) takes the `cnt` tiles of 256 rows from
+// tile t0 on.
 template <class Epi, int NP, int NS>
 struct Problems {
   const unsigned short *A[NP][NS], *B[NP][NS];
@@ -382,7 +383,14 @@ struct Problems {
   Epi ep[NP];
   int start[NP + 1];  // first tile of each problem; start[NP] = all tiles
   int splits, part;
+  int t0, cnt;
 };
+
+// What a launch covers: WHOLE, all its tiles (of 64 TM rows) times all parts of K;
+// DIRECT and PARTS, the rest behind a launch of whole rounds of 256-row tiles, in
+// tiles of the same grid (TM = 2: in halves of them), finished at once or as
+// partial sums [part][tile][256][256] (EpiPart).
+enum Rest { WHOLE, DIRECT, PARTS };
 
 // Whether an epilogue asks for a pair as B (kPair): the product's columns are blocks
 // of 32 rows of B and of its `second` matrix in turn (`features` rows each, N = 64
@@ -396,16 +404,35 @@ struct is_pair<E, std::enable_if_t<E::kPair>> : std::true_type {};
 
 #define GEMM_FENCE() asm volatile("" ::: "memory")
 
+// Partial sums of a rest's tiles; PAIR: B is a pair.
+template <bool PAIR>
+struct EpiPart {
+  static constexpr bool kSwap = true, kPair = PAIR;
+  const unsigned short *second;
+  int features;
+  float *c;
+  template <int NI, int NJ>
+  __device__ __forceinline__ void operator()(const f32x4 (&acc)[NI][NJ], const Tile &t) const {
+    EpiOut<float, ST> e{c, BN, nullptr, 0, 1.f, 1, 1, 0};
+    e(acc, t);
+  }
+};
+
 // Grid: 8 * ceil(tiles * splits / 8) x 512.
-template <bool TA, bool TB, int TM, class Epi, int NP, int NS>
+template <bool TA, bool TB, int TM, class Epi, int NP, int NS, Rest REST = WHOLE>
 __global__ void __launch_bounds__(THREADS, 1) k_gemm(const Problems<Epi, NP, NS> g) {
   constexpr int BM = bm_of(TM), SA = BM * BK * 2, SB = BN * BK * 2;  // bytes of a slot
   constexpr int LDS_B = SA * SLOTS_A;                                // the B ring follows the A ring
   __shared__ __attribute__((aligned(1024))) char lds[LDS_B + SB * SLOTS_B];
-  int idx = xcd_index(g.start[NP] * g.splits);
-  if (idx >= g.start[NP] * g.splits) return;
-  const int split = idx / g.start[NP];
-  idx -= split * g.start[NP];
+  constexpr int HALVES = REST != WHOLE && TM == 2 ? 2 : 1;
+  constexpr int GRID_M = REST != WHOLE ? bm_of(4) : BM;  // rows of a tile of the grid
+  const int tiles = REST != WHOLE ? g.cnt * HALVES : g.start[NP];
+  int idx = xcd_index(tiles * g.splits);
+  if (idx >= tiles * g.splits) return;
+  const int split = idx / tiles;
+  idx -= split * tiles;
+  const int half = HALVES == 2 ? idx & 1 : 0, local = idx / HALVES;
+  if constexpr (REST != WHOLE) idx = g.t0 + local;
   // the problem's fields by unrolled selects (no dynamic indexing of the
   // kernel argument, which would copy it to scratch)
   int M = g.M[0], N = g.N[0], first = 0;
@@ -435,8 +462,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_gemm(const Problems<Epi, NP, NS>
       }
     }
   int mt, nt;
-  tile_of(idx - first, (M + BM - 1) / BM, (N + BN - 1) / BN, mt, nt);
-  const int m0 = mt * BM, n0 = nt * BN;
+  tile_of(idx - first, (M + GRID_M - 1) / GRID_M, (N + BN - 1) / BN, mt, nt);
+  const int m0 = mt * GRID_M + half * BM, n0 = nt * BN;
+  if (HALVES == 2 && m0 >= M) return;
+  if constexpr (REST == PARTS)
+    ep.c += (long)(split * g.cnt + local) * (GRID_M * BN) - ((long)mt * GRID_M * BN + n0);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = wave >> 2;  // waves w and w + 4 share a SIMD
@@ -590,6 +620,13 @@ inline long tiles_of(long M, long N, int TM) {
   return M <= 0 || N <= 0 ? 0 : ((M + bm_of(TM) - 1) / bm_of(TM)) * ((N + BN - 1) / BN);
 }
 
+template <bool TA, bool TB, int TM, Rest REST, class Epi, int NP, int NS>
+inline void launch_rest(const Problems<Epi, NP, NS> &g, hipStream_t st) {
+  const long total = (long)g.cnt * (TM == 2 ? 2 : 1) * g.splits;
+  k_gemm<TA, TB, TM, Epi, NP, NS, REST><<<(unsigned)((total + 7) / 8 * 8), THREADS, 0, st>>>(g);
+  SEG_LAUNCH_CHECK();
+}
+
 template <bool TA, bool TB, int TM, class Epi, int NP, int NS>
 inline void launch_tm(Problems<Epi, NP, NS> &g, hipStream_t st) {
   g.start[0] = 0;
@@ -613,6 +650,31 @@ struct Finish {
   const float *part;
   int parts;
 };
+
+// the epilogue of 8 whole columns of a row, from their sums
+template <class TO, OutMode MODE>
+__device__ __forceinline__ void finish8(const EpiOut<TO, MODE> &e, long m, long n, float (&v)[8]) {
+  TO *d = e.c + m * e.ldc + n;
+  const unsigned short *r = MODE == RESID ? e.r + m * e.ldr + n : nullptr;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    v[j] *= e.scale;
+    if constexpr (MODE == RESID) v[j] += bf_bits2f(r[j]);
+    if constexpr (MODE == ACC)
+      if (!e.first) v[j] += (float)d[j];
+  }
+  if constexpr (sizeof(TO) == 2) {
+    if (e.vec) {
+      u16x8 o;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = f2bf_bits(v[j]);
+      *reinterpret_cast<u16x8 *>(d) = o;
+      return;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) store_val(d, j, v[j]);
+}
 
 template <class TO, OutMode MODE, int NP>
 __global__ void __launch_bounds__(256) k_finish(const Finish<TO, MODE, NP> f) {
@@ -639,27 +701,64 @@ __global__ void __launch_bounds__(256) k_finish(const Finish<TO, MODE, NP> f) {
         v[4 + j] += b[j];
       }
     }
-    TO *d = e.c + m * e.ldc + n;
-    const unsigned short *r = MODE == RESID ? e.r + m * e.ldr + n : nullptr;
+    finish8(e, m, n, v);
+  }
+}
+
+// Where the partial sums of a rest's tiles sit, and their problems.
+template <int NP>
+struct RestTiles {
+  const float *part;
+  int parts, t0, cnt;
+  int M[NP], N[NP], start[NP + 1];
+
+  // the sums of 8 columns from (r, c) of tile `local` on, parts in order
+  __device__ __forceinline__ void sum8(int local, int r, int c, float (&v)[8]) const {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[j] *= e.scale;
-      if constexpr (MODE == RESID) v[j] += bf_bits2f(r[j]);
-      if constexpr (MODE == ACC)
-        if (!e.first) v[j] += (float)d[j];
-    }
-    if constexpr (sizeof(TO) == 2) {
-      if (e.vec) {
-        u16x8 o;
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    for (int k = 0; k < parts; ++k) {
+      const f32x4 *p = reinterpret_cast<const f32x4 *>(
+          part + ((long)(k * cnt + local) * bm_of(4) + r) * BN + c);
+      const f32x4 a = p[0], b = p[1];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = f2bf_bits(v[j]);
-        *reinterpret_cast<u16x8 *>(d) = o;
-        continue;
+      for (int j = 0; j < 4; ++j) {
+        v[j] += a[j];
+        v[4 + j] += b[j];
       }
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) store_val(d, j, v[j]);
   }
+};
+
+// Sums and finishes a rest's tiles: 32 blocks a tile, 8 columns of a row a thread
+// (N a multiple of 8).
+template <class TO, OutMode MODE, int NP>
+struct FinishRest {
+  RestTiles<NP> t;
+  EpiOut<TO, MODE> ep[NP];
+};
+
+template <class TO, OutMode MODE, int NP>
+__global__ void __launch_bounds__(256) k_finish_rest(const FinishRest<TO, MODE, NP> f) {
+  const int local = blockIdx.x / 32, chunk = (blockIdx.x % 32) * 256 + threadIdx.x;
+  const int idx = f.t.t0 + local;
+  EpiOut<TO, MODE> e = f.ep[0];
+  int M = f.t.M[0], N = f.t.N[0], first = 0;
+#pragma unroll
+  for (int q = 1; q < NP; ++q)
+    if (idx >= f.t.start[q]) {
+      e = f.ep[q];
+      M = f.t.M[q];
+      N = f.t.N[q];
+      first = f.t.start[q];
+    }
+  int mt, nt;
+  tile_of(idx - first, (M + bm_of(4) - 1) / bm_of(4), (N + BN - 1) / BN, mt, nt);
+  const int r = chunk / 32, c = chunk % 32 * 8;
+  const int m = mt * bm_of(4) + r, n = nt * BN + c;
+  if (m >= M || n >= N) return;
+  float v[8];
+  f.t.sum8(local, r, c, v);
+  finish8(e, m, n, v);
 }
 
 // Workspace for partial sums.
@@ -679,6 +778,9 @@ struct Scratch {
 // 15 us in eight.
 struct Choice {
   int tm, parts, part;  // part: steps of 64
+  int full = 0;         // 256-row tiles in whole rounds before the rest (choose_even)
+  bool rest = false;    // the tiles behind them as a rest
+  double us = 0;        // the time that is expected
 };
 
 inline Choice choose(long t4, long t2, long steps, double elems, long scratch) {
@@ -693,6 +795,40 @@ inline Choice choose(long t4, long t2, long steps, double elems, long scratch) {
       if ((s == 1 && tm == 4) || us < best_us) {
         best = Choice{tm, s, (int)per};
         best_us = us;
+      }
+    }
+  }
+  best.us = best_us;
+  return best;
+}
+
+// The same for a product that may be launched in two pieces: whole rounds of
+// 256-row tiles over the chip, and the rest in halves of tiles or in parts of K
+// that fill it again.  So a grid a little larger than the chip does not cost
+// another whole round.  Measured, one piece / two: 1,500 rows, 2 x 5,504 features
+// over 2,048 (258 tiles), 106 / 89 us a call; 8,192 rows, dx of 3,584 columns over
+// 2 x 18,944 (448 tiles) and both weight gradients (2,072 tiles), 3.64 / 3.57 ms a
+// call: less than the idle CUs, as power bounds the full chip.  A row's sum then
+// depends on the number of rows, so the decoder layer, whose results do not depend
+// on the chunks it works in, launches its products in one piece.
+inline Choice choose_even(const Choice &one, long t4, long steps, long scratch) {
+  Choice best = one;
+  const long rounds = t4 / NUM_CU;
+  for (long r = rounds; r >= 0 && r + 1 >= rounds; --r) {
+    const long rest = t4 - r * NUM_CU;
+    if (rest == 0) continue;
+    const double full = r * (1.5 * steps + 4) + (r > 0 ? 3 : 0);
+    for (int s = 1; s <= 16; ++s) {
+      const long per = (steps + s - 1) / s;
+      if (s > 1 && (per < 4 || s * rest * bm_of(4) * BN > scratch || (s - 1) * per >= steps)) continue;
+      for (int tm = s > 1 ? 4 : 2; tm >= 2; tm -= 2) {
+        const double waves = (double)((rest * (tm == 2 ? 2 : 1) * s + NUM_CU - 1) / NUM_CU);
+        const double us = full + waves * ((tm == 4 ? 1.5 : 0.93) * per + 4) +
+                          (s > 1 ? (double)s * rest * bm_of(4) * BN / 5e5 + 5 : 0);
+        if (us < best.us) {
+          best = Choice{tm, s, (int)per, (int)(r * NUM_CU), true};
+          best.us = us;
+        }
       }
     }
   }
@@ -715,6 +851,17 @@ inline Choice choose_group(int np, const int *M, const int *N, int ns, const int
   }
   for (int s = 0; s < ns; ++s) steps += (K[s] + BK - 1) / BK;
   return choose(t4, t2, steps, elems, whole ? scratch : 0);
+}
+
+inline Choice choose_even_group(int np, const int *M, const int *N, int ns, const int *K, long scratch) {
+  long t4 = 0, steps = 0;
+  bool whole = true;
+  for (int q = 0; q < np; ++q) {
+    t4 += tiles_of(M[q], N[q], 4);
+    whole = whole && N[q] % 8 == 0;
+  }
+  for (int s = 0; s < ns; ++s) steps += (K[s] + BK - 1) / BK;
+  return choose_even(choose_group(np, M, N, ns, K, scratch, 0), t4, steps, whole ? scratch : 0);
 }
 
 template <class Epi, int NP, int NS>
@@ -774,6 +921,72 @@ inline void launch(const Problems<EpiOut<TO, MODE>, NP, NS> &g, const Scratch &s
   f.parts = c.parts;
   k_finish<TO, MODE, NP><<<(unsigned)std::min<long>(8192, (total / 8 + 255) / 256), 256, 0, st>>>(f);
   SEG_LAUNCH_CHECK();
+}
+
+// A group of products in the two pieces of choose_even: whole rounds, then the rest,
+// finished at once or through finish(RestTiles).
+template <bool TA, bool TB, class Epi, int NP, int NS, class F>
+inline void launch_even(Problems<Epi, NP, NS> g, const Choice &c, float *part, F &&finish, hipStream_t st) {
+  constexpr bool PAIR = is_pair<Epi>::value;
+  int start[NP + 1] = {0};
+  for (int q = 0; q < NP; ++q) start[q + 1] = start[q] + (int)tiles_of(g.M[q], g.N[q], 4);
+  g.splits = 1;
+  for (int s = 0; s < NS; ++s) g.part += (g.K[s] + BK - 1) / BK;  // all steps
+  if (c.full > 0) {
+    for (int q = 0; q <= NP; ++q) g.start[q] = std::min(start[q], c.full);
+    k_gemm<TA, TB, 4, Epi, NP, NS><<<(unsigned)((c.full + 7) / 8 * 8), THREADS, 0, st>>>(g);
+    SEG_LAUNCH_CHECK();
+  }
+  for (int q = 0; q <= NP; ++q) g.start[q] = start[q];
+  g.t0 = c.full;
+  g.cnt = start[NP] - c.full;
+  if (c.parts == 1) {
+    launch_rest<TA, TB, 2, DIRECT>(g, st);
+    return;
+  }
+  Problems<EpiPart<PAIR>, NP, NS> h{};
+  RestTiles<NP> t{part, c.parts, g.t0, g.cnt, {}, {}, {}};
+  for (int q = 0; q < NP; ++q) {
+    for (int s = 0; s < NS; ++s) {
+      h.A[q][s] = g.A[q][s];
+      h.B[q][s] = g.B[q][s];
+      h.lda[q][s] = g.lda[q][s];
+      h.ldb[q][s] = g.ldb[q][s];
+    }
+    t.M[q] = h.M[q] = g.M[q];
+    t.N[q] = h.N[q] = g.N[q];
+    h.ep[q].c = part;
+    if constexpr (PAIR) {
+      h.ep[q].second = g.ep[q].second;
+      h.ep[q].features = g.ep[q].features;
+    }
+  }
+  for (int s = 0; s < NS; ++s) h.K[s] = g.K[s];
+  for (int q = 0; q <= NP; ++q) t.start[q] = h.start[q] = start[q];
+  h.splits = c.parts;
+  h.part = c.part;
+  h.t0 = g.t0;
+  h.cnt = g.cnt;
+  if (c.tm == 2) launch_rest<TA, TB, 2, PARTS>(h, st);
+  else launch_rest<TA, TB, 4, PARTS>(h, st);
+  finish(t);
+}
+
+// The group in one piece or two, whichever is expected to be faster; a row's sum may
+// depend on the number of rows.
+template <bool TA, bool TB, class TO, OutMode MODE, int NP, int NS>
+inline void launch_even(const Problems<EpiOut<TO, MODE>, NP, NS> &g, const Scratch &sc, hipStream_t st) {
+  const Choice c = choose_even_group(NP, g.M, g.N, NS, g.K, sc.elems);
+  if (!c.rest) {
+    launch<TA, TB>(g, sc, 0, st);
+    return;
+  }
+  launch_even<TA, TB>(g, c, sc.p, [&](const RestTiles<NP> &t) {
+    FinishRest<TO, MODE, NP> f{t, {}};
+    for (int q = 0; q < NP; ++q) f.ep[q] = g.ep[q];
+    k_finish_rest<TO, MODE, NP><<<(unsigned)(t.cnt * 32), 256, 0, st>>>(f);
+    SEG_LAUNCH_CHECK();
+  }, st);
 }
 
 // One product.

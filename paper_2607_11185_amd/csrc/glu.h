@@ -15,9 +15,12 @@ struct Kept {
   seg_act8 g8, u8;
 };
 
-// m = silu(x wg^T) * (x wu^T), with the gate and up values to `keep`
+// m = silu(x wg^T) * (x wu^T), with the gate and up values to `keep`.  sums: memory for
+// partial sums (seg_glu_workspace_bytes), or NULL: a row's result then does not depend
+// on the other rows
 void forward(const unsigned short *x, long ldx, const unsigned short *wg, const unsigned short *wu,
-             int rows, int hidden, int inter, unsigned short *m, const Kept &keep, hipStream_t st);
+             int rows, int hidden, int inter, unsigned short *m, const Kept &keep, float *sums,
+             hipStream_t st);
 
 // dg = dm * u * silu'(g), du = dm * silu(g), from the kept values; with m set
 // also m = silu(g) * u.  All [rows, inter].

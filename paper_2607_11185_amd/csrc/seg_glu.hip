@@ -20,6 +20,7 @@ using gemm::EpiOut;
 using gemm::ST;
 
 constexpr int MAX_DIM = 1 << 20;  // GEMM rows are addressed with 32-bit offsets
+constexpr long MAX_SUMS = 64L << 20;  // fp32 partial sums of a launch at most (256 MB)
 
 __device__ __forceinline__ float sigmoidf_(float g) { return 1.f / (1.f + __expf(-g)); }
 
@@ -122,6 +123,69 @@ struct EpiGlu {
   }
 };
 
+// The epilogue's work on a rest's tiles from their partial sums: 16 blocks a tile,
+// 8 features of a row a thread, four lanes a block of 32 features.
+template <Keep KEEP>
+__global__ void __launch_bounds__(256) k_finish_glu(const gemm::RestTiles<1> t, const EpiGlu<KEEP> ep) {
+  const int local = blockIdx.x / 16, chunk = (blockIdx.x % 16) * 256 + threadIdx.x;
+  int mt, nt;
+  gemm::tile_of(t.t0 + local, (t.M[0] + 255) / 256, (t.N[0] + gemm::BN - 1) / gemm::BN, mt, nt);
+  const int r = chunk / 16, c = chunk % 16, col = c / 4 * 64 + c % 4 * 8;  // the gate's columns in the tile
+  const int row = mt * 256 + r, f = nt * (gemm::BN / 2) + c * 8;
+  const long I = ep.features;
+  const bool in = row < t.M[0] && f < I;
+  float g[8], u[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) g[j] = u[j] = 0.f;
+  if (in) {
+    t.sum8(local, r, col, g);
+    t.sum8(local, r, col + 32, u);
+  }
+  int eg = 0, eu = 0;
+  if constexpr (KEEP == CODES) {
+    unsigned tg = 0, tu = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      tg = max(tg, act8::mag(g[j]));
+      tu = max(tu, act8::mag(u[j]));
+    }
+#pragma unroll
+    for (int o = 1; o <= 2; o *= 2) {
+      tg = max(tg, (unsigned)__shfl_xor((int)tg, o, 64));
+      tu = max(tu, (unsigned)__shfl_xor((int)tu, o, 64));
+    }
+    eg = act8::exp_byte(tg);
+    eu = act8::exp_byte(tu);
+  }
+  if (!in) return;
+  const long off = (long)row * I + f;
+  u16x8 m;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m[j] = f2bf_bits(g[j] * sigmoidf_(g[j]) * u[j]);
+  *reinterpret_cast<u16x8 *>(ep.m + off) = m;
+  if constexpr (KEEP == BF16) {
+    u16x8 a, b;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      a[j] = f2bf_bits(g[j]);
+      b[j] = f2bf_bits(u[j]);
+    }
+    *reinterpret_cast<u16x8 *>(ep.k.g16 + off) = a;
+    *reinterpret_cast<u16x8 *>(ep.k.u16 + off) = b;
+  }
+  if constexpr (KEEP == CODES) {
+    const long at = (long)row * ((I + act8::BLOCK - 1) / act8::BLOCK) + f / act8::BLOCK;
+    if (c % 4 == 0) {
+      ep.k.g8.exp[at] = (uint8_t)eg;
+      ep.k.u8.exp[at] = (uint8_t)eu;
+    }
+    *reinterpret_cast<uint2 *>(ep.k.g8.code + off) = make_uint2(act8::codes4(g[0], g[1], g[2], g[3], eg),
+                                                                 act8::codes4(g[4], g[5], g[6], g[7], eg));
+    *reinterpret_cast<uint2 *>(ep.k.u8.code + off) = make_uint2(act8::codes4(u[0], u[1], u[2], u[3], eu),
+                                                                 act8::codes4(u[4], u[5], u[6], u[7], eu));
+  }
+}
+
 // dg = dm * u * silu'(g), du = dm * silu(g), silu'(g) = s (1 + g (1 - s)),
 // s = sigmoid(g), and m = silu(g) * u; 8 features a thread.  A streaming kernel:
 // folded into the epilogue of the GEMM that makes dm its loads stall the one
@@ -164,14 +228,42 @@ __global__ void __launch_bounds__(256) k_glu_bwd(const glu::Kept k, const unsign
   }
 }
 
+int pair_columns(int inter) { return 2 * (int)act8::blocks_of(inter) * act8::BLOCK; }
+
+// How a forward of its own (not a chunk of a layer) is launched, with up to MAX_SUMS
+// partial sums.
+gemm::Choice choose_fwd(int rows, int hidden, int inter) {
+  const int N = pair_columns(inter);
+  const long steps = (hidden + gemm::BK - 1) / gemm::BK;
+  const long t4 = gemm::tiles_of(rows, N, 4), t2 = gemm::tiles_of(rows, N, 2);
+  return gemm::choose_even(gemm::choose(t4, t2, steps, 1, 0), t4, steps, MAX_SUMS);
+}
+
+size_t fwd_sums(int rows, int hidden, int inter) {
+  const gemm::Choice c = choose_fwd(rows, hidden, inter);
+  if (!c.rest || c.parts == 1) return 256;
+  return (size_t)c.parts * (gemm::tiles_of(rows, pair_columns(inter), 4) - c.full) * gemm::bm_of(4) * gemm::BN * 4;
+}
+
 }  // namespace
 
 namespace glu {
 
 void forward(const unsigned short *x, long ldx, const unsigned short *wg, const unsigned short *wu, int rows,
-             int hidden, int inter, unsigned short *m, const Kept &keep, hipStream_t st) {
-  const int N = 2 * (int)act8::blocks_of(inter) * act8::BLOCK;
-  auto go = [&](auto ep) { gemm::launch_one<false, false>(x, ldx, wg, hidden, rows, N, hidden, ep, st); };
+             int hidden, int inter, unsigned short *m, const Kept &keep, float *sums, hipStream_t st) {
+  const int N = pair_columns(inter);
+  const gemm::Choice c = sums ? choose_fwd(rows, hidden, inter) : gemm::Choice{4, 1, 0};
+  auto go = [&](auto ep) {
+    const auto g = gemm::one<false, false>(x, ldx, wg, hidden, rows, N, hidden, ep);
+    if (!c.rest) {
+      gemm::launch<false, false>(g, st);
+      return;
+    }
+    gemm::launch_even<false, false>(g, c, sums, [&](const gemm::RestTiles<1> &t) {
+      k_finish_glu<<<(unsigned)(t.cnt * 16), 256, 0, st>>>(t, ep);
+      SEG_LAUNCH_CHECK();
+    }, st);
+  };
   if (keep.g16) go(EpiGlu<BF16>{wu, inter, m, keep});
   else if (keep.g8.code) go(EpiGlu<CODES>{wu, inter, m, keep});
   else go(EpiGlu<NONE>{wu, inter, m, keep});
@@ -211,10 +303,11 @@ GluWs glu_ws(int rows, int hidden, int inter, bool kept) {
     w.u = take(R * I * 2);
     w.m = take(R * I * 2);
   }
-  // partial sums of products cut over K: what the largest cut product takes, up
-  // to 128 MB (larger ones fill the chip uncut)
-  w.sum_elems = (long)std::min<size_t>((size_t)32 << 20, 16 * std::max(R * H, 2 * H * I));
-  w.sums = take(w.sum_elems * 4);
+  // partial sums of products cut over K: what 16 parts of the larger one take, its
+  // tiles whole, up to MAX_SUMS (larger ones fill the chip uncut)
+  const size_t t = std::max(gemm::tiles_of(R, H, 4), 2 * gemm::tiles_of(I, H, 4));
+  w.sum_elems = (long)std::min<size_t>(MAX_SUMS, 16 * t * gemm::bm_of(4) * gemm::BN);
+  w.sums = take(std::max<size_t>(w.sum_elems * 4, kept ? 0 : fwd_sums(rows, hidden, inter)));
   w.total = c.off;
   return w;
 }
@@ -253,27 +346,52 @@ bool check_kept(const seg_act8 *g, const seg_act8 *u) {
 
 using namespace seg;
 
+// For tests (not in seg.h; host only): how the forward (which = 0), dx (1) and the
+// weight gradients (2) are launched; out = {rows of a tile, parts of K, 256-row
+// tiles in whole rounds, whether there is a rest}.
+extern "C" void seg_glu_gemm_choice(int32_t rows, int32_t hidden, int32_t inter, int32_t which, int32_t *out) {
+  gemm::Choice c;
+  const long sums = glu_ws(rows, hidden, inter, true).sum_elems;
+  if (which == 0) {
+    c = choose_fwd(rows, hidden, inter);
+  } else if (which == 1) {
+    const int K[2] = {inter, inter};
+    c = gemm::choose_even_group(1, &rows, &hidden, 2, K, sums);
+  } else {
+    const int M[2] = {inter, inter}, N[2] = {hidden, hidden};
+    c = gemm::choose_even_group(2, M, N, 1, &rows, sums);
+  }
+  out[0] = gemm::bm_of(c.tm);
+  out[1] = c.parts;
+  out[2] = c.full;
+  out[3] = c.rest;
+}
+
 extern "C" seg_status seg_glu_fwd(int32_t rows, int32_t hidden, int32_t inter, const void *x, int64_t ldx,
                                   const void *wg, const void *wu, void *m, const seg_act8 *g8,
-                                  const seg_act8 *u8, hipStream_t stream) {
+                                  const seg_act8 *u8, void *ws, size_t ws_bytes, hipStream_t stream) {
   return guarded([&] {
     check_glu(rows, hidden, inter, ldx);
     if (rows == 0) return;
     SEG_CHECK(x && wg && wu && m, SEG_ERR_ARG, "x, a weight or m is NULL");
     check_aligned({x, wg, wu, m}, 16);
+    const size_t need = fwd_sums(rows, hidden, inter);
+    SEG_CHECK(ws_bytes >= need, SEG_ERR_WORKSPACE, "workspace of %zu bytes < required %zu", ws_bytes, need);
+    SEG_CHECK(ws, SEG_ERR_ARG, "ws is NULL");
+    check_aligned({ws}, 16);
     glu::Kept keep{};
     if (check_kept(g8, u8)) {
       keep.g8 = *g8;
       keep.u8 = *u8;
     }
     ProfScope prof("glu_fwd", stream);
-    glu::forward(CUS(x), ldx, CUS(wg), CUS(wu), rows, hidden, inter, US(m), keep, stream);
+    glu::forward(CUS(x), ldx, CUS(wg), CUS(wu), rows, hidden, inter, US(m), keep, static_cast<float *>(ws), stream);
   });
 }
 
-extern "C" size_t seg_glu_workspace_bytes(int32_t rows, int32_t hidden, int32_t inter, int32_t kept) {
-  if (rows < 0 || hidden < 1 || inter < 1) return 0;
-  return glu_ws(rows, hidden, inter, kept != 0).total;
+extern "C" size_t seg_glu_workspace_bytes(int32_t rows, int32_t hidden, int32_t inter, int32_t bwd, int32_t kept) {
+  if (rows < 0 || rows > MAX_DIM || hidden < 1 || hidden > MAX_DIM || inter < 1 || inter > MAX_DIM) return 0;
+  return bwd ? glu_ws(rows, hidden, inter, kept != 0).total : fwd_sums(rows, hidden, inter);
 }
 
 extern "C" seg_status seg_glu_bwd(int32_t rows, int32_t hidden, int32_t inter, const void *x, int64_t ldx,
@@ -311,7 +429,7 @@ extern "C" seg_status seg_glu_bwd(int32_t rows, int32_t hidden, int32_t inter, c
         kept.g16 = US(base + W.g);
         kept.u16 = US(base + W.u);
         unsigned short *mm = m ? US(m) : US(base + W.m);
-        glu::forward(CUS(x), ldx, CUS(wg), CUS(wu), rows, hidden, inter, mm, kept, stream);
+        glu::forward(CUS(x), ldx, CUS(wg), CUS(wu), rows, hidden, inter, mm, kept, sums.p, stream);
       }
       glu::backward_act(kept, CUS(dm), rows, inter, dg, du, has ? US(m) : nullptr, stream);
     }
@@ -320,7 +438,7 @@ extern "C" seg_status seg_glu_bwd(int32_t rows, int32_t hidden, int32_t inter, c
       ProfScope prof("glu_dx", stream);
       gemm::Problems<OutBf, 1, 2> g{{{dg, du}}, {{CUS(wg), CUS(wu)}}, {{inter, inter}}, {{hidden, hidden}},
                                     {inter, inter}, {rows}, {hidden}, {OutBf::make(US(dx), hidden)}, {}, 1, 0};
-      gemm::launch<false, true>(g, sums, 0, stream);
+      gemm::launch_even<false, true>(g, sums, stream);
     }
     ProfScope prof("glu_dw", stream);
     auto dw = [&](auto *a, auto *b) {
@@ -328,7 +446,7 @@ extern "C" seg_status seg_glu_bwd(int32_t rows, int32_t hidden, int32_t inter, c
       gemm::Problems<Out, 2, 1> g{{{dg}, {du}}, {{CUS(x)}, {CUS(x)}}, {{inter}, {inter}}, {{ldx}, {ldx}}, {rows},
                                   {inter, inter}, {hidden, hidden}, {Out::make(a, hidden), Out::make(b, hidden)},
                                   {}, 1, 0};
-      gemm::launch<true, true>(g, sums, 0, stream);
+      gemm::launch_even<true, true>(g, sums, stream);
     };
     if (dw_dt == SEG_BF16) dw(US(dwg), US(dwu));
     else dw(static_cast<float *>(dwg), static_cast<float *>(dwu));

@@ -561,7 +561,7 @@ void layer_fwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cf
       rms_fwd(y1 + r0 * H, H, w.g2, c.rms_eps, cr, H, pos + r0, a, sv.rstd2 + r0, st);
     }
     ProfScope prof("ly_mlp", st);
-    glu::forward(a, H, CUS(w.wg), CUS(w.wu), cr, H, I, mb, kept_rows(ext, r0, I), st);
+    glu::forward(a, H, CUS(w.wg), CUS(w.wu), cr, H, I, mb, kept_rows(ext, r0, I), nullptr, st);
     gemm::launch_one<false, false>(mb, I, CUS(w.wd), I, cr, H, I,
                                    OutResid::make(y + r0 * H, H, 1.f, y1 + r0 * H, H), sums, P, st);
   }
@@ -630,7 +630,7 @@ void layer_bwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cf
       if (!kept.g8.code) {
         kept.g16 = US(base + W.g);
         kept.u16 = US(base + W.u);
-        glu::forward(a, H, CUS(w.wg), CUS(w.wu), cr, H, I, mb, kept, st);
+        glu::forward(a, H, CUS(w.wg), CUS(w.wu), cr, H, I, mb, kept, nullptr, st);
       }
       gemm::launch_one<false, true>(dy1c, H, CUS(w.wd), I, cr, I, H, OutBf::make(dm, I), sums, P, st);  // dm = dy wd
       glu::backward_act(kept, dm, cr, I, dgb, dub, kept.g8.code ? mb : nullptr, st);

@@ -531,7 +531,13 @@ def _kept(kept, rows, inter):
     return (ctypes.byref(g.c()), ctypes.byref(u.c())), (g.code, g.exp, u.code, u.exp)
 
 
-def seg_glu_fwd(x, wg, wu, keep=False, m=None):
+def glu_workspace(rows, hidden, inter, bwd: bool, kept: bool, device):
+    import torch
+    n = _lib.lib().seg_glu_workspace_bytes(rows, hidden, inter, int(bwd), int(kept))
+    return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
+
+
+def seg_glu_fwd(x, wg, wu, keep=False, m=None, ws=None):
     """m = silu(x wg^T) * (x wu^T); x [rows, H] (rows at any distance), wg and wu
     [I, H], bf16.  keep: True, or a pair (Act8, Act8) to fill, keeps the gate and
     up values in 8 bits.  Returns (m, kept or None)."""
@@ -544,17 +550,14 @@ def seg_glu_fwd(x, wg, wu, keep=False, m=None):
         keep = (Act8.empty(rows, inter, x.device), Act8.empty(rows, inter, x.device))
     kept = keep or None
     c, tensors = _kept(kept, rows, inter)
-    dev = _device(x, wg, wu, m, *tensors)
+    if ws is None:
+        ws = glu_workspace(rows, hidden, inter, False, False, x.device)
+    dev = _device(x, wg, wu, m, ws, *tensors)
     with _on(dev):
         check(_lib.lib().seg_glu_fwd(rows, hidden, inter, x.data_ptr(), _rows(x), wg.data_ptr(),
-                                     wu.data_ptr(), m.data_ptr(), *c, _stream(dev)))
+                                     wu.data_ptr(), m.data_ptr(), *c, ws.data_ptr(), ws.numel(),
+                                     _stream(dev)))
     return m, kept
-
-
-def glu_workspace(rows, hidden, inter, kept: bool, device):
-    import torch
-    n = _lib.lib().seg_glu_workspace_bytes(rows, hidden, inter, int(kept))
-    return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
 
 
 def seg_glu_bwd(x, wg, wu, dm, kept=None, dw_dtype=None, want_m=True, out=None, ws=None):
@@ -578,7 +581,7 @@ def seg_glu_bwd(x, wg, wu, dm, kept=None, dw_dtype=None, want_m=True, out=None, 
         assert (n == "m" and t is None) or (t.shape == shape and t.is_contiguous()), n
         assert t is None or n in ("dwg", "dwu") or t.dtype == torch.bfloat16, n
     if ws is None:
-        ws = glu_workspace(rows, hidden, inter, kept is not None, dev)
+        ws = glu_workspace(rows, hidden, inter, True, kept is not None, dev)
     c, tensors = _kept(kept, rows, inter)
     _device(x, wg, wu, dm, out["dx"], out["dwg"], out["dwu"], out.get("m"), ws, *tensors)
     with _on(dev):

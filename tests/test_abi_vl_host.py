@@ -130,16 +130,18 @@ def test_gated_block_refuses(kw, want):
     s = _lib.SegAct8(a["code"], 1)
     g8, u8 = (ctypes.byref(s) if a[n] else None for n in ("g8", "u8"))
     size = (a["rows"], a["hidden"], a["inter"], a["x"], a["ldx"], a["wg"], a["wu"])
-    assert L.seg_glu_fwd(*size, 16, g8, u8, None) == want
+    assert L.seg_glu_fwd(*size, 16, g8, u8, 16, 1 << 40, None) == want
     assert L.seg_glu_bwd(*size, g8, u8, 16, 16, 16, 0, 16, 16, 16, 1 << 40, None) == want
 
 
 def test_gated_block_backward_refuses():
     L = _lib_or_skip()
     size = (4, 64, 96, 16, 64, 16, 16)
-    need = L.seg_glu_workspace_bytes(4, 64, 96, 0)
-    kept = L.seg_glu_workspace_bytes(4, 64, 96, 1)
-    assert 0 < kept < need and L.seg_glu_workspace_bytes(-1, 64, 96, 1) == 0
+    need = L.seg_glu_workspace_bytes(4, 64, 96, 1, 0)
+    kept = L.seg_glu_workspace_bytes(4, 64, 96, 1, 1)
+    fwd = L.seg_glu_workspace_bytes(4, 64, 96, 0, 0)
+    assert 0 < fwd < kept < need and L.seg_glu_workspace_bytes(-1, 64, 96, 1, 1) == 0
+    assert L.seg_glu_workspace_bytes((1 << 20) + 1, 64, 96, 0, 0) == 0
     s = _lib.SegAct8(8, 1)
     g = ctypes.byref(s)
 
@@ -148,8 +150,11 @@ def test_gated_block_backward_refuses():
     assert bwd(n=need - 1) == WS and bwd(g8=g, n=kept - 1) == WS
     assert bwd(dm=None) == bwd(dx=None) == bwd(dwg=None) == bwd(dwu=None) == bwd(ws=None) == ARG
     assert bwd(dm=8) == bwd(m=8) == bwd(dx=8) == bwd(dwg=8) == bwd(dwu=8) == bwd(ws=8) == bwd(dt=3) == UNS
-    assert L.seg_glu_fwd(*size, None, None, None, None) == ARG
-    assert L.seg_glu_fwd(0, 64, 96, None, 64, None, None, None, None, None, None) == _lib.SEG_OK
+    assert L.seg_glu_fwd(*size, None, None, None, 16, fwd, None) == ARG
+    assert L.seg_glu_fwd(*size, 16, None, None, 16, fwd - 1, None) == WS
+    assert L.seg_glu_fwd(*size, 16, None, None, None, fwd, None) == ARG
+    assert L.seg_glu_fwd(*size, 16, None, None, 8, fwd, None) == UNS
+    assert L.seg_glu_fwd(0, 64, 96, None, 64, None, None, None, None, None, None, 0, None) == _lib.SEG_OK
 
 
 def test_extended_layer_refuses():

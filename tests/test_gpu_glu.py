@@ -16,6 +16,7 @@ import pytest
 
 from oracle import act8 as OA8
 from oracle import glu as OG
+from paper_2607_11185_amd import _lib
 from paper_2607_11185_amd import seg as S
 from tests.gpu_helpers import rel, say
 
@@ -23,7 +24,11 @@ pytestmark = pytest.mark.gpu
 
 # rows, hidden, inter: one row and few, widths around the tiles of 32, 64, 128 and 256
 SHAPES = [(1, 8, 8), (1, 64, 40), (3, 72, 104), (17, 328, 200), (64, 256, 256), (130, 264, 520), (300, 128, 1032),
-          (257, 512, 72), (16, 1024, 2048), (33, 2048, 264)]
+          (257, 512, 72), (16, 1024, 2048), (33, 2048, 264),
+          # each way a product is cut (test_every_way_of_cutting): parts of K and halves of tiles
+          (2, 1040, 8), (674, 8, 5512), (1, 24, 320), (1624, 8, 8), (2, 8, 2712), (1813, 8, 264)]
+# whole rounds of tiles over the chip and a rest behind them
+LARGE = (1500, 2048, 5504)
 
 
 def _np(t):
@@ -55,8 +60,29 @@ def _forward_bounds(x, wg, wu):
     return m, g, u, eg, eu, em + 2.0 ** -8 * (np.abs(m) + em) + 1e-38
 
 
+def _choice(rows, hidden, inter, which):
+    import ctypes
+
+    import torch  # noqa: F401  (its HIP runtime is loaded before the library asks for one)
+    f = _lib.lib().seg_glu_gemm_choice
+    f.restype, f.argtypes = None, [ctypes.c_int32] * 4 + [ctypes.c_void_p]
+    out = (ctypes.c_int32 * 4)()
+    f(rows, hidden, inter, which, out)
+    tile, parts, full, rest = out
+    return "whole" if not rest and parts == 1 else "parts" if not rest else ("rounds + " if full else "") + (
+        "halves" if parts == 1 else "parts of the rest")
+
+
+def test_every_way_of_cutting():
+    """The shapes above take, for the forward, dx and the weight gradients, every way that
+    their products are cut."""
+    got = {(w, _choice(*s, w)) for s in [*SHAPES, LARGE] for w in range(3)}
+    assert got >= {(0, "whole"), (0, "parts of the rest"), (0, "rounds + parts of the rest"), (1, "whole"), (1, "parts"),
+                   (1, "parts of the rest"), (2, "whole"), (2, "parts"), (2, "parts of the rest"), (2, "rounds + halves")}, got
+
+
 @pytest.mark.parametrize("keep", [False, True])
-@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("shape", [*SHAPES, LARGE], ids=lambda s: "x".join(map(str, s)))
 def test_forward(shape, keep):
     import torch
     rows, hidden, inter = shape
@@ -85,7 +111,7 @@ def _kept_of(g, u):
 
 
 @pytest.mark.parametrize("dw", ["bf16", "f32"])
-@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("shape", [*SHAPES, LARGE], ids=lambda s: "x".join(map(str, s)))
 def test_backward_from_kept_values(shape, dw):
     import torch
     rows, hidden, inter = shape
