@@ -186,6 +186,251 @@ __global__ void __launch_bounds__(256) k_finish_glu(const gemm::RestTiles<1> t, 
   }
 }
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// x and weights of a forward for few rows.
+struct RowsArgs {
+  const unsigned short *x, *wg, *wu;
+  long ldx;
+  int rows, hidden;
+};
+
+// Features of a block of the kernels for few rows: one block of the 8-bit format.
+constexpr int FEATURES = act8::BLOCK;
+constexpr int FEW = 8;      // rows that k_glu_few takes at most
+constexpr int ROWS = 64;    // and k_glu_rows
+constexpr int PARTS = 4;    // of K, k_glu_few; each four waves
+constexpr int ROWS_WAVES = 8;
+constexpr unsigned FEW_LDS = 64u << 10;
+
+// The forward for a handful of rows (at most T), where the weights' bytes are all
+// the work.  Measured, plain reads reach 6.7 TB/s when a load takes whole 128-byte
+// lines past the caches (__builtin_nontemporal_load), 6.0 through them, and 5.0 past
+// them in the half lines of a matrix product's operand layout.  So no matrix product: a
+// load takes 64 k of 8 features, a lane 8 k of one, and multiplies them with its k of
+// every row of x, which lies in LDS as all waves need it.  A block takes 32 features;
+// four waves of it 8 of them each, and four such groups a quarter of K each.  The
+// eight lanes of a feature add up by exchange, the quarters in LDS, in order.
+// 3,584 x 2 x 18,944, 1 / 4 / 8 rows: 46.9 / 49.1 / 59.2 us (5.8 / 5.5 / 4.6 TB/s;
+// the GEMM takes 62); 2,048 x 2 x 5,504: 11.1 / 11.6 / 13.8 (30).  With K in halves
+// 47 / 49 / 63 and 15.5 / 15.5 / 17.2; two steps in flight more registers, so fewer
+// blocks at once: 48 / 53 / 127.
+template <int T, Keep KEEP>
+__global__ void __launch_bounds__(256 * PARTS) k_glu_few(const RowsArgs a, const EpiGlu<KEEP> ep) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ float sums[PARTS][2][T][FEATURES];  // part of K, gate or up, row, feature
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int H = a.hidden, I = ep.features, f0 = blockIdx.x * FEATURES;
+  const int steps = (H + 63) / 64, per = (steps + PARTS - 1) / PARTS;  // of a part
+  bf16x8 *xs = reinterpret_cast<bf16x8 *>(lds);                        // [T][steps * 8]
+  const int part = wave % PARTS, grp = wave / PARTS, c = lane & 7;
+  const int f = min(f0 + 8 * grp + (lane >> 3), I - 1);  // past the end: the last, unused
+  const unsigned short *pg = a.wg + (long)f * H + 8 * c, *pu = a.wu + (long)f * H + 8 * c;
+  const int s0 = part * per, s1 = min(steps, s0 + per);
+  struct Step {
+    bf16x8 g, u;
+  };
+  auto load = [&](Step &w, int s) __attribute__((always_inline)) {
+    const bool in = s < s1 && s * 64 + 8 * c < H;
+    w.g = in ? __builtin_nontemporal_load(reinterpret_cast<const bf16x8 *>(pg + s * 64)) : bf16x8{};
+    w.u = in ? __builtin_nontemporal_load(reinterpret_cast<const bf16x8 *>(pu + s * 64)) : bf16x8{};
+  };
+  Step w0, w1;
+  load(w0, s0);
+  load(w1, s0 + 1);
+  for (int e = threadIdx.x; e < T * steps * 8; e += 256 * PARTS) {
+    const int t = e / (steps * 8), k = (e - t * steps * 8) * 8;
+    xs[e] = t < a.rows && k < H ? *reinterpret_cast<const bf16x8 *>(a.x + t * a.ldx + k) : bf16x8{};
+  }
+  __syncthreads();
+  float g[T], u[T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) g[t] = u[t] = 0.f;
+  auto products = [&](const Step &w, int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      const bf16x8 x = xs[(t * steps + s) * 8 + c];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x2 xj = bf16x2{x[2 * j], x[2 * j + 1]};
+        g[t] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w.g[2 * j], w.g[2 * j + 1]}, xj, g[t], false);
+        u[t] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w.u[2 * j], w.u[2 * j + 1]}, xj, u[t], false);
+      }
+    }
+  };
+  for (int s = s0; s < s1; s += 2) {
+    products(w0, s);
+    load(w0, s + 2);
+    if (s + 1 >= s1) break;
+    products(w1, s + 1);
+    load(w1, s + 3);
+  }
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+#pragma unroll
+    for (int o = 1; o <= 4; o *= 2) {
+      g[t] += __shfl_xor(g[t], o, 64);
+      u[t] += __shfl_xor(u[t], o, 64);
+    }
+    if (c == 0) {
+      sums[part][0][t][8 * grp + (lane >> 3)] = g[t];
+      sums[part][1][t][8 * grp + (lane >> 3)] = u[t];
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x >= FEATURES * T) return;
+  const int t = threadIdx.x / FEATURES, fi = threadIdx.x % FEATURES;
+  float gv = sums[0][0][t][fi], uv = sums[0][1][t][fi];
+#pragma unroll
+  for (int p = 1; p < PARTS; ++p) {
+    gv += sums[p][0][t][fi];
+    uv += sums[p][1][t][fi];
+  }
+  const bool in = t < a.rows && f0 + fi < I;
+  const long off = (long)t * I + f0 + fi;
+  if constexpr (KEEP == CODES) {
+    unsigned tg = in ? act8::mag(gv) : 0u, tu = in ? act8::mag(uv) : 0u;
+#pragma unroll
+    for (int o = 1; o <= 16; o *= 2) {
+      tg = max(tg, (unsigned)__shfl_xor((int)tg, o, 64));
+      tu = max(tu, (unsigned)__shfl_xor((int)tu, o, 64));
+    }
+    const int eg = act8::exp_byte(tg), eu = act8::exp_byte(tu);
+    if (in) {
+      const long at = (long)t * ((I + act8::BLOCK - 1) / act8::BLOCK) + blockIdx.x;
+      if (fi == 0) {
+        ep.k.g8.exp[at] = (uint8_t)eg;
+        ep.k.u8.exp[at] = (uint8_t)eu;
+      }
+      ep.k.g8.code[off] = (int8_t)act8::codes4(gv, 0.f, 0.f, 0.f, eg);
+      ep.k.u8.code[off] = (int8_t)act8::codes4(uv, 0.f, 0.f, 0.f, eu);
+    }
+  }
+  if (!in) return;
+  ep.m[off] = f2bf_bits(gv * sigmoidf_(gv) * uv);
+  if constexpr (KEEP == BF16) {
+    ep.k.g16[off] = f2bf_bits(gv);
+    ep.k.u16[off] = f2bf_bits(uv);
+  }
+}
+
+// The forward for some tens of rows (16 NB at most): a block takes 32 features and
+// reads their rows of wg and wu from memory to registers in the layout of the
+// products' operands (16 rows x 32 k); its eight waves take every eighth step of 32 of
+// K and add up their sums in LDS, in order.  The next step's loads are under way
+// during a step's products.  Lanes past the last feature or row read the last one,
+// and their sums go nowhere; what lies past K reads as zeros on both sides.  2,048 x
+// 2 x 5,504, 16 / 32 / 64 rows: 15.9 / 17.6 / 21.6 us (the GEMM: 30); 3,584 x 2 x
+// 18,944: 71 / 80 / 104 (62 to 66, so the GEMM serves there).  Longer steps need more
+// registers, and then not all blocks fit at once: steps of 128 in four waves 74 / 113 /
+// 372; past the caches, in half lines, 82 at 16 rows.
+template <int NB, Keep KEEP>
+__global__ void __launch_bounds__(64 * ROWS_WAVES) k_glu_rows(const RowsArgs a, const EpiGlu<KEEP> ep) {
+  __shared__ f32x4 sums[ROWS_WAVES][4 * NB][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, grp = lane >> 4;
+  const int f0 = blockIdx.x * FEATURES, I = ep.features, H = a.hidden;
+  const unsigned short *pw[4], *px[NB];
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+    pw[b] = (b < 2 ? a.wg : a.wu) + (long)min(f0 + 16 * (b & 1) + r, I - 1) * H + 8 * grp;
+#pragma unroll
+  for (int n = 0; n < NB; ++n) px[n] = a.x + (long)min(16 * n + r, a.rows - 1) * a.ldx + 8 * grp;
+  struct Step {
+    bf16x8 w[4], x[NB];
+  };
+  auto load = [&](Step &c, int k) __attribute__((always_inline)) {
+    const bool in = k + 8 * grp < H;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) c.w[b] = in ? *reinterpret_cast<const bf16x8 *>(pw[b] + k) : bf16x8{};
+#pragma unroll
+    for (int n = 0; n < NB; ++n) c.x[n] = in ? *reinterpret_cast<const bf16x8 *>(px[n] + k) : bf16x8{};
+  };
+  f32x4 acc[4][NB];
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int n = 0; n < NB; ++n) acc[b][n] = f32x4{};
+  // features of block b against rows of block n: a lane holds row 16 n + lane % 16,
+  // features 4 (lane / 16) .. + 3
+  auto products = [&](const Step &c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[b][n] = mfma16(c.w[b], c.x[n], acc[b][n]);
+  };
+  constexpr int ST = 32 * ROWS_WAVES;
+  Step c0, c1;
+  int k = wave * 32;
+  if (k < H) load(c0, k);
+  while (k < H) {
+    if (k + ST < H) load(c1, k + ST);
+    products(c0);
+    k += ST;
+    if (k >= H) break;
+    if (k + ST < H) load(c0, k + ST);
+    products(c1);
+    k += ST;
+  }
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int n = 0; n < NB; ++n) sums[wave][b * NB + n][lane] = acc[b][n];
+  __syncthreads();
+  if (wave >= NB) return;
+  const int row = 16 * wave + r;
+  f32x4 v[4];  // gate of features 4 grp .. and 16 + 4 grp .., up of the same
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    v[b] = sums[0][b * NB + wave][lane];
+#pragma unroll
+    for (int w = 1; w < ROWS_WAVES; ++w) v[b] += sums[w][b * NB + wave][lane];
+  }
+  int eg = 0, eu = 0;
+  if constexpr (KEEP == CODES) {
+    unsigned tg = 0, tu = 0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      if (f0 + 16 * b + 4 * grp >= I) continue;  // I is a multiple of 8
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        tg = max(tg, act8::mag(v[b][j]));
+        tu = max(tu, act8::mag(v[2 + b][j]));
+      }
+    }
+#pragma unroll
+    for (int o = 16; o <= 32; o *= 2) {
+      tg = max(tg, (unsigned)__shfl_xor((int)tg, o, 64));
+      tu = max(tu, (unsigned)__shfl_xor((int)tu, o, 64));
+    }
+    eg = act8::exp_byte(tg);
+    eu = act8::exp_byte(tu);
+    const long at = (long)row * ((I + act8::BLOCK - 1) / act8::BLOCK) + blockIdx.x;
+    if (row < a.rows && grp == 0) ep.k.g8.exp[at] = (uint8_t)eg;
+    if (row < a.rows && grp == 1) ep.k.u8.exp[at] = (uint8_t)eu;
+  }
+  if (row >= a.rows) return;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int f = f0 + 16 * b + 4 * grp;
+    if (f >= I) continue;
+    const f32x4 g = v[b], u = v[2 + b];
+    float m[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m[j] = g[j] * sigmoidf_(g[j]) * u[j];
+    const long off = (long)row * I + f;
+    *reinterpret_cast<gemm::u32x2 *>(ep.m + off) = gemm::u32x2{gemm::pack2(m[0], m[1]), gemm::pack2(m[2], m[3])};
+    if constexpr (KEEP == BF16) {
+      *reinterpret_cast<gemm::u32x2 *>(ep.k.g16 + off) = gemm::u32x2{gemm::pack2(g[0], g[1]), gemm::pack2(g[2], g[3])};
+      *reinterpret_cast<gemm::u32x2 *>(ep.k.u16 + off) = gemm::u32x2{gemm::pack2(u[0], u[1]), gemm::pack2(u[2], u[3])};
+    }
+    if constexpr (KEEP == CODES) {
+      *reinterpret_cast<unsigned *>(ep.k.g8.code + off) = act8::codes4(g[0], g[1], g[2], g[3], eg);
+      *reinterpret_cast<unsigned *>(ep.k.u8.code + off) = act8::codes4(u[0], u[1], u[2], u[3], eu);
+    }
+  }
+}
+
 // dg = dm * u * silu'(g), du = dm * silu(g), silu'(g) = s (1 + g (1 - s)),
 // s = sigmoid(g), and m = silu(g) * u; 8 features a thread.  A streaming kernel:
 // folded into the epilogue of the GEMM that makes dm its loads stall the one
@@ -228,20 +473,63 @@ __global__ void __launch_bounds__(256) k_glu_bwd(const glu::Kept k, const unsign
   }
 }
 
+unsigned few_lds(int rows, int hidden) { return (unsigned)((hidden + 63) / 64 * 128) * rows; }
+
+// Rows of x that the kernel for few rows is built for (1, 2, 4 or 8; 16, 32 or 64 for
+// k_glu_rows), or 0 where the GEMM serves: by the time that each is expected to take,
+// us, as measured (see the kernels).  A handful of rows reads the weights at the rate
+// of memory, if x fits the LDS; some tens do at 4.0, 3.5 and 2.7 TB/s and 4 us more,
+// against the GEMM's steps of 0.93 us on tiles of 128 x 256, one round where the
+// weights are as wide as the chip.
+int few_rows(int rows, int hidden, int inter, double gemm_us) {
+  for (int t = 1; t <= FEW; t *= 2)
+    if (rows <= t) {
+      if (few_lds(t, hidden) + PARTS * 2 * t * FEATURES * 4 <= FEW_LDS) return t;
+      break;
+    }
+  const double mb = 4e-6 * hidden * inter;
+  if (rows <= 16) return 4 + mb / 4.0 < gemm_us ? 16 : 0;
+  if (rows <= 32) return 4 + mb / 3.5 < gemm_us ? 32 : 0;
+  if (rows <= ROWS) return 4 + mb / 2.7 < gemm_us ? 64 : 0;
+  return 0;
+}
+
+template <class Epi>
+void launch_few(int t, const RowsArgs &a, const Epi &ep, hipStream_t st) {
+  const unsigned nb = (unsigned)act8::blocks_of(ep.features), lds = t <= FEW ? few_lds(t, a.hidden) : 0;
+  switch (t) {
+    case 1: k_glu_few<1><<<nb, 256 * PARTS, lds, st>>>(a, ep); break;
+    case 2: k_glu_few<2><<<nb, 256 * PARTS, lds, st>>>(a, ep); break;
+    case 4: k_glu_few<4><<<nb, 256 * PARTS, lds, st>>>(a, ep); break;
+    case 8: k_glu_few<8><<<nb, 256 * PARTS, lds, st>>>(a, ep); break;
+    case 16: k_glu_rows<1><<<nb, 64 * ROWS_WAVES, 0, st>>>(a, ep); break;
+    case 32: k_glu_rows<2><<<nb, 64 * ROWS_WAVES, 0, st>>>(a, ep); break;
+    default: k_glu_rows<4><<<nb, 64 * ROWS_WAVES, 0, st>>>(a, ep); break;
+  }
+  SEG_LAUNCH_CHECK();
+}
+
 int pair_columns(int inter) { return 2 * (int)act8::blocks_of(inter) * act8::BLOCK; }
 
-// How a forward of its own (not a chunk of a layer) is launched, with up to MAX_SUMS
-// partial sums.
-gemm::Choice choose_fwd(int rows, int hidden, int inter) {
+// How a forward of its own (not a chunk of a layer) is launched: few (few_rows), or a
+// GEMM with up to MAX_SUMS partial sums.
+struct Forward {
+  gemm::Choice c;
+  int few;
+};
+
+Forward choose_fwd(int rows, int hidden, int inter) {
   const int N = pair_columns(inter);
   const long steps = (hidden + gemm::BK - 1) / gemm::BK;
   const long t4 = gemm::tiles_of(rows, N, 4), t2 = gemm::tiles_of(rows, N, 2);
-  return gemm::choose_even(gemm::choose(t4, t2, steps, 1, 0), t4, steps, MAX_SUMS);
+  const gemm::Choice c = gemm::choose_even(gemm::choose(t4, t2, steps, 1, 0), t4, steps, MAX_SUMS);
+  return Forward{c, few_rows(rows, hidden, inter, c.us)};
 }
 
 size_t fwd_sums(int rows, int hidden, int inter) {
-  const gemm::Choice c = choose_fwd(rows, hidden, inter);
-  if (!c.rest || c.parts == 1) return 256;
+  const Forward f = choose_fwd(rows, hidden, inter);
+  const gemm::Choice &c = f.c;
+  if (f.few || !c.rest || c.parts == 1) return 256;
   return (size_t)c.parts * (gemm::tiles_of(rows, pair_columns(inter), 4) - c.full) * gemm::bm_of(4) * gemm::BN * 4;
 }
 
@@ -252,8 +540,13 @@ namespace glu {
 void forward(const unsigned short *x, long ldx, const unsigned short *wg, const unsigned short *wu, int rows,
              int hidden, int inter, unsigned short *m, const Kept &keep, float *sums, hipStream_t st) {
   const int N = pair_columns(inter);
-  const gemm::Choice c = sums ? choose_fwd(rows, hidden, inter) : gemm::Choice{4, 1, 0};
+  const Forward how = sums ? choose_fwd(rows, hidden, inter) : Forward{gemm::Choice{4, 1, 0}, 0};
+  const gemm::Choice &c = how.c;
   auto go = [&](auto ep) {
+    if (how.few) {
+      launch_few(how.few, RowsArgs{x, wg, wu, ldx, rows, hidden}, ep, st);
+      return;
+    }
     const auto g = gemm::one<false, false>(x, ldx, wg, hidden, rows, N, hidden, ep);
     if (!c.rest) {
       gemm::launch<false, false>(g, st);
@@ -348,12 +641,19 @@ using namespace seg;
 
 // For tests (not in seg.h; host only): how the forward (which = 0), dx (1) and the
 // weight gradients (2) are launched; out = {rows of a tile, parts of K, 256-row
-// tiles in whole rounds, whether there is a rest}.
+// tiles in whole rounds, whether there is a rest}, or {rows the kernel for few is
+// built for, 0, 0, 0}.
 extern "C" void seg_glu_gemm_choice(int32_t rows, int32_t hidden, int32_t inter, int32_t which, int32_t *out) {
   gemm::Choice c;
   const long sums = glu_ws(rows, hidden, inter, true).sum_elems;
   if (which == 0) {
-    c = choose_fwd(rows, hidden, inter);
+    const Forward f = choose_fwd(rows, hidden, inter);
+    if (f.few) {
+      out[0] = f.few;
+      out[1] = out[2] = out[3] = 0;
+      return;
+    }
+    c = f.c;
   } else if (which == 1) {
     const int K[2] = {inter, inter};
     c = gemm::choose_even_group(1, &rows, &hidden, 2, K, sums);

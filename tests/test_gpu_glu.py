@@ -26,7 +26,10 @@ pytestmark = pytest.mark.gpu
 SHAPES = [(1, 8, 8), (1, 64, 40), (3, 72, 104), (17, 328, 200), (64, 256, 256), (130, 264, 520), (300, 128, 1032),
           (257, 512, 72), (16, 1024, 2048), (33, 2048, 264),
           # each way a product is cut (test_every_way_of_cutting): parts of K and halves of tiles
-          (2, 1040, 8), (674, 8, 5512), (1, 24, 320), (1624, 8, 8), (2, 8, 2712), (1813, 8, 264)]
+          (70, 1040, 8), (674, 8, 5512), (1, 24, 320), (1624, 8, 8), (2, 8, 2712), (1813, 8, 264),
+          # each kernel for few rows, K that ends inside a step and parts of K that are empty
+          (2, 520, 264), (4, 1096, 96), (8, 200, 40), (5, 24, 1000), (9, 64, 256), (31, 512, 640), (50, 264, 1000), (64, 1032, 264),
+          (8, 4104, 64), (1, 16384, 40)]
 # whole rounds of tiles over the chip and a rest behind them
 LARGE = (1500, 2048, 5504)
 
@@ -69,6 +72,8 @@ def _choice(rows, hidden, inter, which):
     out = (ctypes.c_int32 * 4)()
     f(rows, hidden, inter, which, out)
     tile, parts, full, rest = out
+    if parts == 0:
+        return f"few {tile}"
     return "whole" if not rest and parts == 1 else "parts" if not rest else ("rounds + " if full else "") + (
         "halves" if parts == 1 else "parts of the rest")
 
@@ -77,6 +82,7 @@ def test_every_way_of_cutting():
     """The shapes above take, for the forward, dx and the weight gradients, every way that
     their products are cut."""
     got = {(w, _choice(*s, w)) for s in [*SHAPES, LARGE] for w in range(3)}
+    assert got >= {(0, f"few {n}") for n in (1, 2, 4, 8, 16, 32, 64)}, got
     assert got >= {(0, "whole"), (0, "parts of the rest"), (0, "rounds + parts of the rest"), (1, "whole"), (1, "parts"),
                    (1, "parts of the rest"), (2, "whole"), (2, "parts"), (2, "parts of the rest"), (2, "rounds + halves")}, got
 
