@@ -374,12 +374,12 @@ seg_status seg_layer_bwd(const seg_layout *L, const seg_sizes *sz, const seg_lay
  *   img_len = 0, has none; NULL where no step has one).
  *   pos [3, packed_tokens] int32: time, height and width; -1 in padding rows.
  * The run table is computed on the host and uploaded to `ws` (at least
- * seg_mrope_positions_workspace_bytes(p) bytes); the call waits on `stream`
+ * seg_mrope_positions_workspace_bytes(p, sz) bytes); the call waits on `stream`
  * once after that small upload, as seg_build_layout does.  Errors: SEG_ERR_ARG
  * (invalid problem, or a grid that is not its screenshot's tokens),
  * SEG_ERR_CAPACITY (a position past 2^31 - 1), SEG_ERR_WORKSPACE.
  */
-size_t seg_mrope_positions_workspace_bytes(const seg_problem *p); /* 0: invalid problem */
+size_t seg_mrope_positions_workspace_bytes(const seg_problem *p, const seg_sizes *sz);
 seg_status seg_mrope_positions(const seg_problem *p, const seg_sizes *sz, const int32_t *grid,
                                int32_t *pos, void *ws, size_t ws_bytes, hipStream_t stream);
 

@@ -185,7 +185,8 @@ def lib() -> ctypes.CDLL:
         i32, i64, size, dtype, act8 = (ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_int,
                                        ctypes.POINTER(SegAct8))
         L.seg_mrope_positions_workspace_bytes.restype = size
-        L.seg_mrope_positions_workspace_bytes.argtypes = [ctypes.POINTER(SegProblem)]
+        L.seg_mrope_positions_workspace_bytes.argtypes = [ctypes.POINTER(SegProblem),
+                                                          ctypes.POINTER(SegSizes)]
         L.seg_mrope_positions.restype = ctypes.c_int
         L.seg_mrope_positions.argtypes = [ctypes.POINTER(SegProblem), ctypes.POINTER(SegSizes), VP, VP,
                                           VP, size, VP]

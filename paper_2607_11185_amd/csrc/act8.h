@@ -64,6 +64,19 @@ __device__ __forceinline__ float value(unsigned codes, int j, float scale) {
   return (float)((int)(codes << (24 - 8 * j)) >> 24) * scale;
 }
 
+// The largest of a over aligned groups of 4 and of 8 lanes, by lane permutations inside
+// the vector unit (a general exchange goes through LDS).
+template <int CTRL>
+__device__ __forceinline__ unsigned max_dpp(unsigned a) {
+  return max(a, (unsigned)__builtin_amdgcn_mov_dpp((int)a, CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ unsigned max4(unsigned a) {
+  return max_dpp<0x4e>(max_dpp<0xb1>(a));  // lanes 1 0 3 2, then 2 3 0 1 of a quad
+}
+__device__ __forceinline__ unsigned max8(unsigned a) {
+  return max_dpp<0x141>(max4(a));  // lane 7 - i of a group of 8
+}
+
 // Eight codes of a chunk of columns, their block's scale with them.
 __device__ __forceinline__ void values8(const unsigned (&w)[2], float sc, float (&v)[8]) {
 #pragma unroll

@@ -2,8 +2,12 @@
 // act8.h), packed from and unpacked to rows of bf16 or fp32.
 //
 // Both kernels are bound by HBM: one pass, 3.03 (bf16) or 5.03 (fp32) bytes an
-// element.  A lane takes 8 columns (16-byte accesses for bf16), four lanes a
-// block, so the block's largest magnitude is two exchanges inside a quad.
+// element.  A lane takes 16 bytes of x, so four (bf16) or eight lanes a block, whose
+// largest magnitude is two or three lane permutations.  Rows may start anywhere:
+// global accesses of any width take any alignment of an element, and a row's last,
+// shorter chunk goes element by element.  Measured, pack / unpack: 137,895 x 3,584
+// bf16 ACTA; 100,000 x 2,147 bf16, rows on odd addresses, ACTB (a column a lane:
+// 395 / 333 us).
 #include <algorithm>
 
 #include "act8.h"
@@ -12,22 +16,42 @@
 namespace seg {
 namespace {
 
-constexpr int UNROLL = 4;  // chunks of a lane in flight
-
 struct ActArgs {
   void *x;
   long ldx;
   int8_t *code;
   uint8_t *exp;
-  long rows, chunks;  // chunks of 8 columns, whole blocks (four chunks) a row
-  int cols, per_row;  // per_row: chunks of a row
+  long rows;
+  int cols, per_row, blocks;   // of a row: chunks, and blocks of 32 columns
   int step_rows, step_chunks;  // 64 chunks further: rows and chunks
+  bool narrow;                 // all chunks count in 32 bits
 };
 
-// A lane's place in the chunks, which a wave takes 64 consecutive ones at a time.
+// accesses of a chunk, at the alignment of an element
+template <class T>
+struct Chunk;
+template <>
+struct Chunk<unsigned short> {
+  static constexpr int W = 8;
+  typedef unsigned short X __attribute__((ext_vector_type(8), aligned(2)));
+  typedef unsigned C __attribute__((ext_vector_type(2), aligned(1)));
+};
+template <>
+struct Chunk<float> {
+  static constexpr int W = 4;
+  typedef float X __attribute__((ext_vector_type(4), aligned(4)));
+  typedef unsigned C __attribute__((ext_vector_type(1), aligned(1)));
+};
+
+// A lane's chunk of columns; a wave takes 64 consecutive chunks at a time, a row
+// holding whole blocks of them.
 struct Walk {
   long row;
   int c;
+  __device__ __forceinline__ Walk(const ActArgs &a, long i) {
+    row = a.narrow ? (long)((unsigned)i / (unsigned)a.per_row) : i / a.per_row;
+    c = (int)(i - row * a.per_row);
+  }
   __device__ __forceinline__ void next(const ActArgs &a) {
     row += a.step_rows;
     c += a.step_chunks;
@@ -38,140 +62,110 @@ struct Walk {
   }
 };
 
-template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
-  if constexpr (VEC && sizeof(T) == 2) {
-    const u16x8 w = *reinterpret_cast<const u16x8 *>(p);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = bf_bits2f(w[j]);
-  } else if constexpr (VEC) {
-    const f32x4 lo = reinterpret_cast<const f32x4 *>(p)[0], hi = reinterpret_cast<const f32x4 *>(p)[1];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[j] = lo[j];
-      v[4 + j] = hi[j];
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[j] = 0.f;
-      if (j < n) {
-        if constexpr (sizeof(T) == 2) v[j] = bf_bits2f(p[j]);
-        else v[j] = p[j];
-      }
-    }
-  }
-}
-
-// VEC: cols a multiple of 8, x rows on 16-byte boundaries, codes on 8-byte ones
-template <class T, bool VEC>
-__global__ void __launch_bounds__(256) k_pack(const ActArgs a) {
-  const int lane = threadIdx.x & 63;
-  const long wave = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const long first = wave * (64 * UNROLL) + lane;
-  const T *x = static_cast<const T *>(a.x);
-  Walk w{first / a.per_row, 0};
-  w.c = (int)(first - w.row * a.per_row);
-  float v[UNROLL][8];
-  long row[UNROLL];
-  int col[UNROLL];
-#pragma unroll
-  for (int u = 0; u < UNROLL; ++u) {
-    row[u] = w.row;
-    col[u] = w.c * 8;
-    const int n = w.row < a.rows ? a.cols - col[u] : 0;
-    if (n > 0) load8<T, VEC>(x + w.row * a.ldx + col[u], n, v[u]);
-    else
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[u][j] = 0.f;
-    w.next(a);
-  }
-#pragma unroll
-  for (int u = 0; u < UNROLL; ++u) {
-    unsigned top = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, act8::mag(v[u][j]));
-    top = max(top, (unsigned)__shfl_xor((int)top, 1, 64));
-    top = max(top, (unsigned)__shfl_xor((int)top, 2, 64));
-    const int n = row[u] < a.rows ? a.cols - col[u] : 0;
-    if (n <= 0) continue;
-    const int e = act8::exp_byte(top);
-    if ((lane & 3) == 0) a.exp[row[u] * (a.per_row / 4) + col[u] / act8::BLOCK] = (uint8_t)e;
-    const unsigned lo = act8::codes4(v[u][0], v[u][1], v[u][2], v[u][3], e);
-    const unsigned hi = act8::codes4(v[u][4], v[u][5], v[u][6], v[u][7], e);
-    int8_t *d = a.code + row[u] * a.cols + col[u];
-    if constexpr (VEC) {
-      *reinterpret_cast<uint2 *>(d) = make_uint2(lo, hi);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < n) d[j] = (int8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
-    }
-  }
-}
-
 // bf16 bits of a value that bf16 holds: its upper half (the conversion
 // instruction makes zeros of subnormal numbers, and 2^-127 is one)
 __device__ __forceinline__ unsigned short bf_exact(float v) {
   return (unsigned short)(__builtin_bit_cast(unsigned, v) >> 16);
 }
+template <class T>
+__device__ __forceinline__ float to_float(T v) {
+  if constexpr (sizeof(T) == 2) return bf_bits2f(v);
+  else return v;
+}
+template <class T>
+__device__ __forceinline__ T of_exact(float v) {
+  if constexpr (sizeof(T) == 2) return bf_exact(v);
+  else return v;
+}
 
-template <class T, bool VEC>
-__global__ void __launch_bounds__(256) k_unpack(const ActArgs a) {
+// U chunks a lane
+template <class T, int U>
+__global__ void __launch_bounds__(256) k_pack(const ActArgs a) {
+  typedef Chunk<T> K;
+  constexpr int W = K::W;
   const int lane = threadIdx.x & 63;
-  const long wave = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const long first = wave * (64 * UNROLL) + lane;
-  T *x = static_cast<T *>(a.x);
-  Walk w{first / a.per_row, 0};
-  w.c = (int)(first - w.row * a.per_row);
-  unsigned cd[UNROLL][2];
-  int e[UNROLL], col[UNROLL];
-  long row[UNROLL];
+  Walk w(a, ((long)blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 * U) + lane);
+  typename K::X v[U];
+  long row[U];
+  int col[U];
 #pragma unroll
-  for (int u = 0; u < UNROLL; ++u) {
+  for (int u = 0; u < U; ++u) {
     row[u] = w.row;
-    col[u] = w.c * 8;
-    const int n = w.row < a.rows ? a.cols - col[u] : 0;
-    cd[u][0] = cd[u][1] = 0u;
-    e[u] = 0;
-    if (n > 0) {
-      e[u] = a.exp[w.row * (a.per_row / 4) + col[u] / act8::BLOCK];
-      const int8_t *s = a.code + w.row * a.cols + col[u];
-      if constexpr (VEC) {
-        const uint2 t = *reinterpret_cast<const uint2 *>(s);
-        cd[u][0] = t.x;
-        cd[u][1] = t.y;
-      } else {
+    col[u] = w.c * W;
+    const int n = row[u] < a.rows ? a.cols - col[u] : 0;
+    const T *p = static_cast<const T *>(a.x) + row[u] * a.ldx + col[u];
+    v[u] = typename K::X{};
+    if (n >= W) v[u] = *reinterpret_cast<const typename K::X *>(p);
+    else
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < n) cd[u][j / 4] |= (unsigned)(uint8_t)s[j] << (8 * (j & 3));
-      }
-    }
+      for (int j = 0; j < W - 1; ++j)
+        if (j < n) v[u][j] = p[j];
     w.next(a);
   }
 #pragma unroll
-  for (int u = 0; u < UNROLL; ++u) {
+  for (int u = 0; u < U; ++u) {
+    float f[W];
+    unsigned top = 0;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      f[j] = to_float<T>(v[u][j]);
+      top = max(top, act8::mag(f[j]));
+    }
+    top = W == 8 ? act8::max4(top) : act8::max8(top);
     const int n = row[u] < a.rows ? a.cols - col[u] : 0;
     if (n <= 0) continue;
-    float v[8];
-    act8::values8(cd[u], act8::scale(e[u]), v);
-    T *d = x + row[u] * a.ldx + col[u];
-    if constexpr (VEC && sizeof(T) == 2) {
-      u16x8 o;
+    const int e = act8::exp_byte(top);
+    if (col[u] % act8::BLOCK == 0) a.exp[row[u] * a.blocks + col[u] / act8::BLOCK] = (uint8_t)e;
+    typename K::C c;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = bf_exact(v[j]);
-      *reinterpret_cast<u16x8 *>(d) = o;
-    } else if constexpr (VEC) {
-      reinterpret_cast<f32x4 *>(d)[0] = f32x4{v[0], v[1], v[2], v[3]};
-      reinterpret_cast<f32x4 *>(d)[1] = f32x4{v[4], v[5], v[6], v[7]};
-    } else {
+    for (int q = 0; q < W / 4; ++q) c[q] = act8::codes4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3], e);
+    int8_t *d = a.code + row[u] * a.cols + col[u];
+    if (n >= W) *reinterpret_cast<typename K::C *>(d) = c;
+    else
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < n) {
-          if constexpr (sizeof(T) == 2) d[j] = bf_exact(v[j]);
-          else d[j] = v[j];
-        }
-    }
+      for (int j = 0; j < W - 1; ++j)
+        if (j < n) d[j] = (int8_t)(c[j / 4] >> (8 * (j & 3)));
+  }
+}
+
+template <class T, int U>
+__global__ void __launch_bounds__(256) k_unpack(const ActArgs a) {
+  typedef Chunk<T> K;
+  constexpr int W = K::W;
+  const int lane = threadIdx.x & 63;
+  Walk w(a, ((long)blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 * U) + lane);
+  typename K::C cd[U];
+  int e[U], col[U];
+  long row[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    row[u] = w.row;
+    col[u] = w.c * W;
+    const int n = row[u] < a.rows ? a.cols - col[u] : 0;
+    const int8_t *p = a.code + row[u] * a.cols + col[u];
+    e[u] = n > 0 ? a.exp[row[u] * a.blocks + col[u] / act8::BLOCK] : 0;
+    cd[u] = typename K::C{};
+    if (n >= W) cd[u] = *reinterpret_cast<const typename K::C *>(p);
+    else
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j)
+        if (j < n) cd[u][j / 4] |= (unsigned)(uint8_t)p[j] << (8 * (j & 3));
+    w.next(a);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int n = row[u] < a.rows ? a.cols - col[u] : 0;
+    if (n <= 0) continue;
+    const float sc = act8::scale(e[u]);
+    typename K::X o;
+#pragma unroll
+    for (int j = 0; j < W; ++j) o[j] = of_exact<T>(act8::value(cd[u][j / 4], j & 3, sc));
+    T *d = static_cast<T *>(a.x) + row[u] * a.ldx + col[u];
+    if (n >= W) *reinterpret_cast<typename K::X *>(d) = o;
+    else
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j)
+        if (j < n) d[j] = o[j];
   }
 }
 
@@ -192,26 +186,29 @@ bool act_args(int64_t rows, int32_t cols, seg_dtype dt, const void *x, int64_t l
   a.exp = p->exp;
   a.rows = rows;
   a.cols = cols;
-  a.per_row = (int)act8::blocks_of(cols) * (act8::BLOCK / 8);
-  a.chunks = rows * a.per_row;
-  a.step_rows = 64 / a.per_row;
-  a.step_chunks = 64 % a.per_row;
+  a.blocks = (int)act8::blocks_of(cols);
   return true;
 }
 
-// 16-byte accesses of x rows and 8-byte ones of code rows (both strides and both
-// pointers; otherwise element by element)
-bool vectors(const ActArgs &a, seg_dtype dt) {
-  const long e = dt == SEG_BF16 ? 2 : 4;
-  return a.cols % 8 == 0 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * e % 16 == 0 &&
-         reinterpret_cast<uintptr_t>(a.code) % 8 == 0;
-}
-
-unsigned act_blocks(const ActArgs &a) {
-  const long per = 256L * UNROLL;
-  const long n = (a.chunks + per - 1) / per;
-  SEG_CHECK(n <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "tensor too large for one launch");
-  return (unsigned)n;
+// Launches kernel(T, U): one chunk a lane until the chip is full, four in flight
+// beyond that.
+template <class F>
+void act_launch(ActArgs &a, seg_dtype dt, F &&kernel) {
+  a.per_row = a.blocks * (act8::BLOCK / (dt == SEG_BF16 ? Chunk<unsigned short>::W : Chunk<float>::W));
+  a.step_rows = 64 / a.per_row;
+  a.step_chunks = 64 % a.per_row;
+  const long n = a.rows * a.per_row;
+  const int unroll = n > 2048 * 256 ? 4 : 1;
+  const long nb = (n + 256 * unroll - 1) / (256 * unroll);
+  SEG_CHECK(nb <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "tensor too large for one launch");
+  a.narrow = nb * 256 * unroll <= 0xffffffffL;
+  auto go = [&](auto t) {
+    if (unroll == 1) kernel((unsigned)nb, t, std::integral_constant<int, 1>());
+    else kernel((unsigned)nb, t, std::integral_constant<int, 4>());
+  };
+  if (dt == SEG_BF16) go((unsigned short)0);
+  else go(0.f);
+  SEG_LAUNCH_CHECK();
 }
 
 }  // namespace
@@ -224,17 +221,10 @@ extern "C" seg_status seg_act_pack(int64_t rows, int32_t cols, seg_dtype dt, con
   return guarded([&] {
     ActArgs a{};
     if (!act_args(rows, cols, dt, x, ldx, out, a)) return;
-    const unsigned nb = act_blocks(a);
     ProfScope prof("act_pack", stream);
-    const bool v = vectors(a, dt);
-    if (dt == SEG_BF16) {
-      if (v) k_pack<unsigned short, true><<<nb, 256, 0, stream>>>(a);
-      else k_pack<unsigned short, false><<<nb, 256, 0, stream>>>(a);
-    } else {
-      if (v) k_pack<float, true><<<nb, 256, 0, stream>>>(a);
-      else k_pack<float, false><<<nb, 256, 0, stream>>>(a);
-    }
-    SEG_LAUNCH_CHECK();
+    act_launch(a, dt, [&](unsigned nb, auto t, auto u) {
+      k_pack<decltype(t), decltype(u)::value><<<nb, 256, 0, stream>>>(a);
+    });
   });
 }
 
@@ -243,16 +233,9 @@ extern "C" seg_status seg_act_unpack(int64_t rows, int32_t cols, seg_dtype dt, c
   return guarded([&] {
     ActArgs a{};
     if (!act_args(rows, cols, dt, x, ldx, in, a)) return;
-    const unsigned nb = act_blocks(a);
     ProfScope prof("act_unpack", stream);
-    const bool v = vectors(a, dt);
-    if (dt == SEG_BF16) {
-      if (v) k_unpack<unsigned short, true><<<nb, 256, 0, stream>>>(a);
-      else k_unpack<unsigned short, false><<<nb, 256, 0, stream>>>(a);
-    } else {
-      if (v) k_unpack<float, true><<<nb, 256, 0, stream>>>(a);
-      else k_unpack<float, false><<<nb, 256, 0, stream>>>(a);
-    }
-    SEG_LAUNCH_CHECK();
+    act_launch(a, dt, [&](unsigned nb, auto t, auto u) {
+      k_unpack<decltype(t), decltype(u)::value><<<nb, 256, 0, stream>>>(a);
+    });
   });
 }

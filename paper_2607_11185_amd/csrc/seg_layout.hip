@@ -559,15 +559,18 @@ struct Grid {
   int32_t t, h, w, e;
 };
 
+// Byte offsets of the positions' workspace: the runs, the grids and the last run at or
+// before each block's first row.
 struct PosWs {
-  size_t run, grid, total;
+  size_t run, grid, first, total;
 };
 
-PosWs pos_ws_layout(size_t pieces, size_t steps) {
+PosWs pos_ws_layout(const seg_sizes &sz, size_t pieces) {
   PosWs w{};
   w.run = 0;
-  w.grid = align_up(sizeof(PosRun) * std::max<size_t>(1, pieces));
-  w.total = w.grid + align_up(sizeof(Grid) * std::max<size_t>(1, steps));
+  w.grid = align_up(sizeof(PosRun) * (pieces + 1));
+  w.first = w.grid + align_up(sizeof(Grid) * std::max<size_t>(1, sz.num_steps));
+  w.total = w.first + align_up(4 * ((sz.packed_tokens + TOK_BLOCK - 1) / TOK_BLOCK + 1));
   return w;
 }
 
@@ -598,13 +601,16 @@ std::vector<PosRun> pos_runs(const seg_problem *p, const Plan &pl, const Grid *g
   return runs;
 }
 
-// pos[axis][row]: a block's rows lie in few runs, found once for the block.
-__global__ void __launch_bounds__(256) k_mrope_pos(const PosRun *__restrict__ runs, int n,
-                                                   const Grid *__restrict__ grid, int P,
+// pos[axis][row].  A few bytes a row are written and next to nothing is read, so
+// latency bounds it: a block's rows lie in few runs, which the host has found (a
+// search of all runs by every block took 13 us for 1.1M rows; now POSA).
+__global__ void __launch_bounds__(256) k_mrope_pos(const PosRun *__restrict__ runs,
+                                                   const Grid *__restrict__ grid,
+                                                   const int32_t *__restrict__ block_run, int P,
                                                    int32_t *__restrict__ pos) {
   const int first = blockIdx.x * TOK_BLOCK, rows = min(TOK_BLOCK, P - first);
-  const int r0 = max(0, upper_index(n, first, [&](int i) { return runs[i].row; }));
-  const int cnt = upper_index(n - r0, first + (rows - 1), [&](int i) { return runs[r0 + i].row; }) + 1;
+  // the runs of the block: those up to its end start no later than the next block's first
+  const int r0 = block_run[blockIdx.x], cnt = block_run[blockIdx.x + 1] - r0 + 1;
   for (int o = threadIdx.x; o < rows; o += 256) {
     const int r = first + o;
     const PosRun u = runs[r0 + max(0, upper_index(cnt, r, [&](int i) { return runs[r0 + i].row; }))];
@@ -631,13 +637,13 @@ __global__ void __launch_bounds__(256) k_mrope_pos(const PosRun *__restrict__ ru
 
 using namespace seg;
 
-extern "C" size_t seg_mrope_positions_workspace_bytes(const seg_problem *p) {
-  size_t n = 0;
-  (void)guarded([&] {
-    const Plan pl = make_plan(p);
-    n = pos_ws_layout(pl.pieces.size(), pl.sz.num_steps).total;
-  });
-  return n;
+extern "C" size_t seg_mrope_positions_workspace_bytes(const seg_problem *p, const seg_sizes *sz) {
+  if (!p || !sz || p->num_traj < 0 || (p->num_traj > 0 && !p->step_offsets)) return 0;
+  // a segment holds its prompt and at most two runs a turn
+  int64_t turns = 0;
+  for (int t = 0; t < p->num_traj; ++t)
+    turns = std::max<int64_t>(turns, (int64_t)p->step_offsets[t + 1] - p->step_offsets[t]);
+  return pos_ws_layout(*sz, (size_t)sz->num_segments * (2 * turns + 1)).total;
 }
 
 extern "C" seg_status seg_mrope_positions(const seg_problem *p, const seg_sizes *sz, const int32_t *grid,
@@ -653,30 +659,35 @@ extern "C" seg_status seg_mrope_positions(const seg_problem *p, const seg_sizes 
       SEG_CHECK(g, SEG_ERR_ARG, "grid is NULL, and step %d has a screenshot", s);
       SEG_CHECK(g[s].t >= 1 && g[s].h >= 1 && g[s].w >= 1 && g[s].e >= 0, SEG_ERR_ARG,
                 "grid of step %d: %d x %d x %d, time step %d", s, g[s].t, g[s].h, g[s].w, g[s].e);
-      // (t h may pass 63 bits only where t h w does not fit img_len either)
       const int64_t th = (int64_t)g[s].t * g[s].h;
       SEG_CHECK(th <= INT32_MAX && th * g[s].w == p->img_len[s], SEG_ERR_ARG,
                 "grid of step %d: %d x %d x %d is not its %d tokens", s, g[s].t, g[s].h, g[s].w,
                 p->img_len[s]);
     }
     const std::vector<PosRun> runs = pos_runs(p, pl, g);
-    const PosWs w = pos_ws_layout(pl.pieces.size(), sz->num_steps);
+    const PosWs w = pos_ws_layout(*sz, runs.size());
     SEG_CHECK(ws_bytes >= w.total, SEG_ERR_WORKSPACE, "workspace of %zu bytes < required %zu", ws_bytes,
               w.total);
     const int P = (int)sz->packed_tokens;
     if (P == 0) return;
     SEG_CHECK(pos && ws, SEG_ERR_ARG, "pos or ws is NULL");
+    const int blocks = (int)((P + (int64_t)TOK_BLOCK - 1) / TOK_BLOCK);
     std::vector<char> tab(w.total);
     std::memcpy(tab.data() + w.run, runs.data(), runs.size() * sizeof(PosRun));
     if (g) std::memcpy(tab.data() + w.grid, g, sz->num_steps * sizeof(Grid));
+    int32_t *first = reinterpret_cast<int32_t *>(tab.data() + w.first);
+    for (int b = 0, k = 0; b <= blocks; ++b) {
+      while (k + 1 < (int)runs.size() && runs[k + 1].row <= (int64_t)b * TOK_BLOCK) ++k;
+      first[b] = k;
+    }
     SEG_HIP(hipMemcpyAsync(ws, tab.data(), w.total, hipMemcpyHostToDevice, stream));
     // the host tables are locals of this call: wait until they have been read
     SEG_HIP(hipStreamSynchronize(stream));
     ProfScope prof("mrope_pos", stream);
     const char *base = static_cast<const char *>(ws);
-    k_mrope_pos<<<(unsigned)((P + (int64_t)TOK_BLOCK - 1) / TOK_BLOCK), 256, 0, stream>>>(
-        reinterpret_cast<const PosRun *>(base + w.run), (int)runs.size(),
-        reinterpret_cast<const Grid *>(base + w.grid), P, pos);
+    k_mrope_pos<<<(unsigned)blocks, 256, 0, stream>>>(
+        reinterpret_cast<const PosRun *>(base + w.run), reinterpret_cast<const Grid *>(base + w.grid),
+        reinterpret_cast<const int32_t *>(base + w.first), P, pos);
     SEG_LAUNCH_CHECK();
   });
 }

@@ -9,6 +9,7 @@ pointers plus torch's current stream to the library.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import dataclasses
 from typing import Optional
@@ -49,11 +50,12 @@ class Problem:
 
     def c(self) -> SegProblem:
         def ptr(a):
-            return a.ctypes.data_as(_lib.P32) if a.size else ctypes.cast(None, _lib.P32)
-        return SegProblem(len(self.prompt_len), ptr(self.step_offsets), ptr(self.prompt_len),
-                          ptr(self.img_len), ptr(self.text_len), ptr(self.action_len),
-                          self.window, self.seg_steps, self.max_seg_tokens, self.buffer_tokens,
-                          self.tile, self.mode)
+            return ctypes.cast(a.__array_interface__["data"][0] if a.size else None, _lib.P32)
+        arrays = (self.step_offsets, self.prompt_len, self.img_len, self.text_len, self.action_len)
+        p = SegProblem(len(self.prompt_len), *map(ptr, arrays), self.window, self.seg_steps,
+                       self.max_seg_tokens, self.buffer_tokens, self.tile, self.mode)
+        p.arrays = arrays  # alive as long as the struct
+        return p
 
 
 def seg_layout_query(problem: Problem) -> SegSizes:
@@ -375,6 +377,8 @@ def _device(*tensors):
 def _on(dev):
     """Calls are made with the tensors' GPU as the current one."""
     import torch
+    if torch.cuda.current_device() == dev.index:
+        return contextlib.nullcontext()
     return torch.cuda.device(dev)
 
 
@@ -407,7 +411,7 @@ def seg_mrope_positions(problem: Problem, lay: Layout, grid, pos=None, ws=None):
         pos = torch.empty((3, lay.sizes.packed_tokens), dtype=torch.int32, device=lay.device)
     assert pos.dtype == torch.int32 and pos.is_contiguous() and pos.shape == (3, lay.sizes.packed_tokens)
     if ws is None:
-        n = L.seg_mrope_positions_workspace_bytes(ctypes.byref(pc))
+        n = L.seg_mrope_positions_workspace_bytes(ctypes.byref(pc), ctypes.byref(lay.sizes))
         ws = torch.empty(max(n, 1), dtype=torch.uint8, device=lay.device)
     dev = _device(pos, ws)
     with _on(dev):

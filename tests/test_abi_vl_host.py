@@ -53,18 +53,28 @@ def test_positions_refuse_bad_calls():
     L = _lib_or_skip()
     pr = _prob()
     sz = S.seg_layout_query(pr)
-    need = L.seg_mrope_positions_workspace_bytes(ctypes.byref(pr.c()))
-    assert need > 0
+    assert L.seg_mrope_positions_workspace_bytes(ctypes.byref(pr.c()), ctypes.byref(sz)) > 0
     assert _positions(pr, None) == ARG and b"grid" in L.seg_last_error()
-    assert _positions(pr, GOOD, ws_bytes=need - 1) == WS
+    assert _positions(pr, GOOD, ws_bytes=255) == WS
     assert _positions(pr, GOOD) == ARG and b"NULL" in L.seg_last_error()       # pos and ws
     other = _lib.SegSizes.from_buffer_copy(sz)
     other.packed_tokens += 1
     assert _positions(pr, GOOD, sz=other) == ARG
     assert L.seg_mrope_positions(None, ctypes.byref(sz), None, None, None, 0, None) == ARG
     assert L.seg_mrope_positions(ctypes.byref(pr.c()), None, None, None, None, 0, None) == ARG
-    assert L.seg_mrope_positions_workspace_bytes(None) == 0
-    assert L.seg_mrope_positions_workspace_bytes(ctypes.byref(_prob(window=0).c())) == 0
+    assert L.seg_mrope_positions_workspace_bytes(None, ctypes.byref(sz)) == 0
+    assert L.seg_mrope_positions_workspace_bytes(ctypes.byref(pr.c()), None) == 0
+    # the size that is asked for is enough, for any problem
+    rng = np.random.default_rng(3)
+    for _ in range(20):
+        T = rng.integers(0, 30, size=3)
+        n = int(T.sum())
+        sp = WL.explicit_spans(T, rng.integers(1, 5, size=3), rng.integers(0, 2, size=n) * 6, rng.integers(0, 4, size=n), [0] * n)
+        many = S.Problem.from_spans(sp, int(rng.integers(1, 9)), int(rng.integers(1, 5)), 0, int(rng.choice([0, 4000])))
+        msz = S.seg_layout_query(many)
+        size = L.seg_mrope_positions_workspace_bytes(ctypes.byref(many.c()), ctypes.byref(msz))
+        grid = np.tile(np.array([1, 2, 3, 1], np.int32), (n, 1))
+        assert _positions(many, grid, ws_bytes=size) == (ARG if msz.packed_tokens else _lib.SEG_OK)   # pos is NULL
     # a problem without screenshots needs no grid, and one without trajectories no memory
     text = S.Problem.from_spans(WL.explicit_spans([2], [3], [0, 0], [4, 4], [1, 1]), 1, 1)
     assert _positions(text, None) == ARG and b"pos or ws" in L.seg_last_error()
