@@ -44,7 +44,9 @@ __device__ __forceinline__ float scale(int byte) {
 }
 
 // codes of four values of a block with exponent byte `byte`, lowest byte first
-// (zeros where the block is not finite)
+// (zeros where the block is not finite).  x 2^-s + 1.5 2^23 rounds to the nearest
+// integer, ties to even, in one operation (the product is exact), and holds that
+// integer in its low bits.
 __device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, int byte) {
   if (byte >= LAST) {  // rare: the largest numbers of fp32
     if (byte == NOT_FINITE) return 0u;
@@ -54,9 +56,12 @@ __device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, i
     c = fminf(fmaxf(c, -top), top);
     d = fminf(fmaxf(d, -top), top);
   }
-  const float inv = inv_scale(byte);
-  const int i = (int)rintf(a * inv), j = (int)rintf(b * inv), k = (int)rintf(c * inv), l = (int)rintf(d * inv);
-  return (unsigned)(i & 255) | (unsigned)(j & 255) << 8 | (unsigned)(k & 255) << 16 | (unsigned)(l & 255) << 24;
+  const float inv = inv_scale(byte), magic = 0x1.8p23f;
+  const unsigned i = __builtin_bit_cast(unsigned, fmaf(a, inv, magic)), j = __builtin_bit_cast(unsigned, fmaf(b, inv, magic));
+  const unsigned k = __builtin_bit_cast(unsigned, fmaf(c, inv, magic)), l = __builtin_bit_cast(unsigned, fmaf(d, inv, magic));
+  // the low bytes side by side
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(l, k, 0x0c0c0400u), __builtin_amdgcn_perm(j, i, 0x0c0c0400u),
+                               0x05040100u);
 }
 
 // value j of four codes
@@ -75,6 +80,15 @@ __device__ __forceinline__ unsigned max4(unsigned a) {
 }
 __device__ __forceinline__ unsigned max8(unsigned a) {
   return max_dpp<0x141>(max4(a));  // lane 7 - i of a group of 8
+}
+
+// The largest of a over lanes 16 and 32 apart (the four that share a row of a product's
+// result).
+__device__ __forceinline__ unsigned max_groups(unsigned a) {
+  const auto p = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  a = max(p[0], p[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+  return max(q[0], q[1]);
 }
 
 // Eight codes of a chunk of columns, their block's scale with them.

@@ -6,7 +6,7 @@
 // largest magnitude is two or three lane permutations.  Rows may start anywhere:
 // global accesses of any width take any alignment of an element, and a row's last,
 // shorter chunk goes element by element.  Measured, pack / unpack: 137,895 x 3,584
-// bf16 ACTA; 100,000 x 2,147 bf16, rows on odd addresses, ACTB (a column a lane:
+// bf16 ACTA; 100,000 x 2,147 bf16, rows on odd addresses, ACTB (with a column a lane
 // 395 / 333 us).
 #include <algorithm>
 
@@ -78,8 +78,20 @@ __device__ __forceinline__ T of_exact(float v) {
   else return v;
 }
 
-// U chunks a lane
-template <class T, int U>
+template <bool STREAM, class V, class P>
+__device__ __forceinline__ V load_piece(const P *p) {
+  const V *q = reinterpret_cast<const V *>(p);
+  return STREAM ? __builtin_nontemporal_load(q) : *q;
+}
+template <bool STREAM, class V, class P>
+__device__ __forceinline__ void store_piece(P *p, const V &x) {
+  V *q = reinterpret_cast<V *>(p);
+  if (STREAM) __builtin_nontemporal_store(x, q);
+  else *q = x;
+}
+
+// U chunks a lane; more than one: past the caches (STREAM_BYTES) or not
+template <class T, int U, bool STREAM>
 __global__ void __launch_bounds__(256) k_pack(const ActArgs a) {
   typedef Chunk<T> K;
   constexpr int W = K::W;
@@ -95,7 +107,7 @@ __global__ void __launch_bounds__(256) k_pack(const ActArgs a) {
     const int n = row[u] < a.rows ? a.cols - col[u] : 0;
     const T *p = static_cast<const T *>(a.x) + row[u] * a.ldx + col[u];
     v[u] = typename K::X{};
-    if (n >= W) v[u] = *reinterpret_cast<const typename K::X *>(p);
+    if (n >= W) v[u] = load_piece<STREAM, typename K::X>(p);
     else
 #pragma unroll
       for (int j = 0; j < W - 1; ++j)
@@ -120,7 +132,7 @@ __global__ void __launch_bounds__(256) k_pack(const ActArgs a) {
 #pragma unroll
     for (int q = 0; q < W / 4; ++q) c[q] = act8::codes4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3], e);
     int8_t *d = a.code + row[u] * a.cols + col[u];
-    if (n >= W) *reinterpret_cast<typename K::C *>(d) = c;
+    if (n >= W) store_piece<STREAM>(d, c);
     else
 #pragma unroll
       for (int j = 0; j < W - 1; ++j)
@@ -128,7 +140,7 @@ __global__ void __launch_bounds__(256) k_pack(const ActArgs a) {
   }
 }
 
-template <class T, int U>
+template <class T, int U, bool STREAM>
 __global__ void __launch_bounds__(256) k_unpack(const ActArgs a) {
   typedef Chunk<T> K;
   constexpr int W = K::W;
@@ -145,7 +157,7 @@ __global__ void __launch_bounds__(256) k_unpack(const ActArgs a) {
     const int8_t *p = a.code + row[u] * a.cols + col[u];
     e[u] = n > 0 ? a.exp[row[u] * a.blocks + col[u] / act8::BLOCK] : 0;
     cd[u] = typename K::C{};
-    if (n >= W) cd[u] = *reinterpret_cast<const typename K::C *>(p);
+    if (n >= W) cd[u] = load_piece<STREAM, typename K::C>(p);
     else
 #pragma unroll
       for (int j = 0; j < W - 1; ++j)
@@ -161,7 +173,7 @@ __global__ void __launch_bounds__(256) k_unpack(const ActArgs a) {
 #pragma unroll
     for (int j = 0; j < W; ++j) o[j] = of_exact<T>(act8::value(cd[u][j / 4], j & 3, sc));
     T *d = static_cast<T *>(a.x) + row[u] * a.ldx + col[u];
-    if (n >= W) *reinterpret_cast<typename K::X *>(d) = o;
+    if (n >= W) store_piece<STREAM>(d, o);
     else
 #pragma unroll
       for (int j = 0; j < W - 1; ++j)
@@ -190,8 +202,8 @@ bool act_args(int64_t rows, int32_t cols, seg_dtype dt, const void *x, int64_t l
   return true;
 }
 
-// Launches kernel(T, U): one chunk a lane until the chip is full, four in flight
-// beyond that.
+// Launches kernel(T, U, STREAM): one chunk a lane until the chip is full, four in
+// flight beyond that, past the caches where they cannot hold the tensors.
 template <class F>
 void act_launch(ActArgs &a, seg_dtype dt, F &&kernel) {
   a.per_row = a.blocks * (act8::BLOCK / (dt == SEG_BF16 ? Chunk<unsigned short>::W : Chunk<float>::W));
@@ -202,9 +214,11 @@ void act_launch(ActArgs &a, seg_dtype dt, F &&kernel) {
   const long nb = (n + 256 * unroll - 1) / (256 * unroll);
   SEG_CHECK(nb <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "tensor too large for one launch");
   a.narrow = nb * 256 * unroll <= 0xffffffffL;
+  const double bytes = (double)a.rows * a.cols * (dt == SEG_BF16 ? 3 : 5);
   auto go = [&](auto t) {
-    if (unroll == 1) kernel((unsigned)nb, t, std::integral_constant<int, 1>());
-    else kernel((unsigned)nb, t, std::integral_constant<int, 4>());
+    if (unroll == 1) kernel((unsigned)nb, t, std::integral_constant<int, 1>(), std::false_type());
+    else if (bytes <= STREAM_BYTES) kernel((unsigned)nb, t, std::integral_constant<int, 4>(), std::false_type());
+    else kernel((unsigned)nb, t, std::integral_constant<int, 4>(), std::true_type());
   };
   if (dt == SEG_BF16) go((unsigned short)0);
   else go(0.f);
@@ -222,8 +236,8 @@ extern "C" seg_status seg_act_pack(int64_t rows, int32_t cols, seg_dtype dt, con
     ActArgs a{};
     if (!act_args(rows, cols, dt, x, ldx, out, a)) return;
     ProfScope prof("act_pack", stream);
-    act_launch(a, dt, [&](unsigned nb, auto t, auto u) {
-      k_pack<decltype(t), decltype(u)::value><<<nb, 256, 0, stream>>>(a);
+    act_launch(a, dt, [&](unsigned nb, auto t, auto u, auto past) {
+      k_pack<decltype(t), decltype(u)::value, decltype(past)::value><<<nb, 256, 0, stream>>>(a);
     });
   });
 }
@@ -234,8 +248,8 @@ extern "C" seg_status seg_act_unpack(int64_t rows, int32_t cols, seg_dtype dt, c
     ActArgs a{};
     if (!act_args(rows, cols, dt, x, ldx, in, a)) return;
     ProfScope prof("act_unpack", stream);
-    act_launch(a, dt, [&](unsigned nb, auto t, auto u) {
-      k_unpack<decltype(t), decltype(u)::value><<<nb, 256, 0, stream>>>(a);
+    act_launch(a, dt, [&](unsigned nb, auto t, auto u, auto past) {
+      k_unpack<decltype(t), decltype(u)::value, decltype(past)::value><<<nb, 256, 0, stream>>>(a);
     });
   });
 }

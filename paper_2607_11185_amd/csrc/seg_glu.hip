@@ -67,13 +67,8 @@ struct EpiGlu {
               tg = max(tg, act8::mag(g[j][r]));
               tu = max(tu, act8::mag(u[j][r]));
             }
-#pragma unroll
-          for (int o = 16; o <= 32; o *= 2) {
-            tg = max(tg, (unsigned)__shfl_xor((int)tg, o, 64));
-            tu = max(tu, (unsigned)__shfl_xor((int)tu, o, 64));
-          }
-          eg = act8::exp_byte(tg);
-          eu = act8::exp_byte(tu);
+          eg = act8::exp_byte(act8::max_groups(tg));
+          eu = act8::exp_byte(act8::max_groups(tu));
           const int row = t.m0 + t.wr + bm * 32 + i * 16 + t.col;
           const long at = (long)row * ((I + act8::BLOCK - 1) / act8::BLOCK) + f0 / act8::BLOCK;
           if (row < t.M && t.grp == 0) k.g8.exp[at] = (uint8_t)eg;
@@ -149,13 +144,8 @@ __global__ void __launch_bounds__(256) k_finish_glu(const gemm::RestTiles<1> t, 
       tg = max(tg, act8::mag(g[j]));
       tu = max(tu, act8::mag(u[j]));
     }
-#pragma unroll
-    for (int o = 1; o <= 2; o *= 2) {
-      tg = max(tg, (unsigned)__shfl_xor((int)tg, o, 64));
-      tu = max(tu, (unsigned)__shfl_xor((int)tu, o, 64));
-    }
-    eg = act8::exp_byte(tg);
-    eu = act8::exp_byte(tu);
+    eg = act8::exp_byte(act8::max4(tg));
+    eu = act8::exp_byte(act8::max4(tu));
   }
   if (!in) return;
   const long off = (long)row * I + f;
@@ -398,13 +388,8 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES) k_glu_rows(const RowsArgs a, 
         tu = max(tu, act8::mag(v[2 + b][j]));
       }
     }
-#pragma unroll
-    for (int o = 16; o <= 32; o *= 2) {
-      tg = max(tg, (unsigned)__shfl_xor((int)tg, o, 64));
-      tu = max(tu, (unsigned)__shfl_xor((int)tu, o, 64));
-    }
-    eg = act8::exp_byte(tg);
-    eu = act8::exp_byte(tu);
+    eg = act8::exp_byte(act8::max_groups(tg));
+    eu = act8::exp_byte(act8::max_groups(tu));
     const long at = (long)row * ((I + act8::BLOCK - 1) / act8::BLOCK) + blockIdx.x;
     if (row < a.rows && grp == 0) ep.k.g8.exp[at] = (uint8_t)eg;
     if (row < a.rows && grp == 1) ep.k.u8.exp[at] = (uint8_t)eu;

@@ -19,27 +19,44 @@ namespace {
 constexpr int MAX_ROWS = 16;       // rows of a block
 constexpr int CS = 512;            // (cos, sin) pairs of a block
 
+// 16 bytes of a row
 template <class T>
-struct Eight;
+struct Piece;
 template <>
-struct Eight<unsigned short> {
+struct Piece<unsigned short> {
+  static constexpr int W = 8;
   u16x8 v;
   __device__ __forceinline__ float get(int j) const { return bf_bits2f(v[j]); }
   __device__ __forceinline__ void set(int j, float f) { v[j] = f2bf_bits(f); }
 };
 template <>
-struct Eight<float> {
-  f32x4 v[2];
-  __device__ __forceinline__ float get(int j) const { return v[j / 4][j & 3]; }
-  __device__ __forceinline__ void set(int j, float f) { v[j / 4][j & 3] = f; }
+struct Piece<float> {
+  static constexpr int W = 4;
+  f32x4 v;
+  __device__ __forceinline__ float get(int j) const { return v[j]; }
+  __device__ __forceinline__ void set(int j, float f) { v[j] = f; }
 };
+template <class T, bool STREAM>
+__device__ __forceinline__ Piece<T> load_piece(const T *p) {
+  const auto *q = reinterpret_cast<const decltype(Piece<T>::v) *>(p);
+  return Piece<T>{STREAM ? __builtin_nontemporal_load(q) : *q};
+}
+template <class T, bool STREAM>
+__device__ __forceinline__ void store_piece(T *p, const Piece<T> &x) {
+  auto *q = reinterpret_cast<decltype(Piece<T>::v) *>(p);
+  if (STREAM) __builtin_nontemporal_store(x.v, q);
+  else *q = x.v;
+}
 
-// rows_per rows a block; half_pow: d/2 rounded up to a power of two
-template <class T>
+// rows_per rows a block; half_pow: d/2 rounded up to a power of two; STREAM: more
+// than the caches hold is read and written, so accesses go past them
+template <class T, bool STREAM>
 __global__ void __launch_bounds__(256) k_mrope(const mrope::Args g, int rows_per, int half_pow) {
   __shared__ __attribute__((aligned(16))) float2 cs[CS];
   __shared__ int ok[MAX_ROWS];
-  const int half = g.d / 2, per = half / 8, chunks = (g.a.heads + g.b.heads) * per;
+  typedef Piece<T> E;
+  constexpr int W = E::W;
+  const int half = g.d / 2, per = half / W, chunks = (g.a.heads + g.b.heads) * per;
   const long row0 = (long)blockIdx.x * rows_per;
   const int rows = (int)min((long)rows_per, g.rows - row0);
   for (int e = threadIdx.x; e < rows * half_pow; e += 256) {
@@ -64,19 +81,19 @@ __global__ void __launch_bounds__(256) k_mrope(const mrope::Args g, int rows_per
   }
   __syncthreads();
   for (int e = threadIdx.x; e < rows * chunks; e += 256) {
-    const int r = e / chunks, q = e - r * chunks, h = q / per, i = (q - h * per) * 8;
+    const int r = e / chunks, q = e - r * chunks, h = q / per, i = (q - h * per) * W;
     const long row = row0 + r;
     const bool first = h < g.a.heads;
     const long lx = first ? g.a.ldx : g.b.ldx, ly = first ? g.a.ldy : g.b.ldy;
     const int hh = first ? h : h - g.a.heads;
     const T *x = static_cast<const T *>(first ? g.a.x : g.b.x) + row * lx + hh * g.d + i;
     T *y = static_cast<T *>(first ? g.a.y : g.b.y) + row * ly + hh * g.d + i;
-    typedef Eight<T> E;
-    E lo = *reinterpret_cast<const E *>(x), hi = *reinterpret_cast<const E *>(x + half), olo, ohi;
+    const E lo = load_piece<T, STREAM>(x), hi = load_piece<T, STREAM>(x + half);
+    E olo, ohi;
     if (ok[r]) {
       const f32x4 *t = reinterpret_cast<const f32x4 *>(cs + r * half + i);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < W; ++j) {
         const f32x4 w = t[j / 2];
         const float c = w[(j & 1) * 2], s = w[(j & 1) * 2 + 1];
         olo.set(j, lo.get(j) * c - hi.get(j) * s);
@@ -84,7 +101,7 @@ __global__ void __launch_bounds__(256) k_mrope(const mrope::Args g, int rows_per
       }
     } else if (g.inverse) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < W; ++j) {
         olo.set(j, 0.f);
         ohi.set(j, 0.f);
       }
@@ -93,8 +110,8 @@ __global__ void __launch_bounds__(256) k_mrope(const mrope::Args g, int rows_per
       olo = lo;
       ohi = hi;
     }
-    *reinterpret_cast<E *>(y) = olo;
-    *reinterpret_cast<E *>(y + half) = ohi;
+    store_piece<T, STREAM>(y, olo);
+    store_piece<T, STREAM>(y + half, ohi);
   }
   if (g.zero && g.inverse)
     for (int r = 0; r < rows; ++r)
@@ -123,15 +140,19 @@ void check_cfg(const seg_mrope_cfg *cfg, int32_t d) {
 
 void launch(seg_dtype dt, const Args &g, hipStream_t st) {
   if (g.rows == 0) return;
-  const int half = g.d / 2, chunks = (g.a.heads + g.b.heads) * (half / 8);
+  const int half = g.d / 2;
+  const int chunks = (g.a.heads + g.b.heads) * half / (dt == SEG_BF16 ? Piece<unsigned short>::W : Piece<float>::W);
   int hp = 8;
   while (hp < half) hp *= 2;
   const int want = (1024 + chunks - 1) / chunks;  // about four chunks a thread
   const int rows_per = std::max(1, std::min(std::min(want, MAX_ROWS), CS / hp));
   const long nb = (g.rows + rows_per - 1) / rows_per;
   SEG_CHECK(nb <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "too many rows for one launch");
-  if (dt == SEG_BF16) k_mrope<unsigned short><<<(unsigned)nb, 256, 0, st>>>(g, rows_per, hp);
-  else k_mrope<float><<<(unsigned)nb, 256, 0, st>>>(g, rows_per, hp);
+  const long bytes = g.rows * (g.a.heads + g.b.heads) * g.d * (dt == SEG_BF16 ? 2 : 4) * 2;
+  const bool stream = bytes > STREAM_BYTES;
+  auto go = [&](auto kernel) { kernel<<<(unsigned)nb, 256, 0, st>>>(g, rows_per, hp); };
+  if (dt == SEG_BF16) go(stream ? k_mrope<unsigned short, true> : k_mrope<unsigned short, false>);
+  else go(stream ? k_mrope<float, true> : k_mrope<float, false>);
   SEG_LAUNCH_CHECK();
 }
 

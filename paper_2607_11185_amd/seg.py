@@ -421,29 +421,38 @@ def seg_mrope_positions(problem: Problem, lay: Layout, grid, pos=None, ws=None):
     return pos
 
 
+def _heads(t, rows, d, dtype):
+    """Heads of t [rows, heads, d] (side by side in a row) and elements between rows."""
+    _, heads, last = t.shape
+    step, head, one = t.stride()
+    assert t.shape[0] == rows and last == d and t.dtype == dtype
+    assert one == 1 and (head == d or heads <= 1), "heads of a row must be adjacent"
+    return heads, step if rows > 1 else heads * d
+
+
 def _mrope(f, q, k, pos, cfg: MropeCfg, q_out, k_out):
     import torch
-    rows, hq, d = q.shape
-    hkv = 0 if k is None else k.shape[1]
-    dt = _dtype_code(q)
+    rows, _, d = q.shape
+    dt, dtype = _dtype_code(q), q.dtype
+    hq, ldq = _heads(q, rows, d, dtype)
+    hkv, ldk = (0, 0) if k is None else _heads(k, rows, d, dtype)
     if q_out is None:
-        q_out = torch.empty((rows, hq, d), dtype=q.dtype, device=q.device)
-    if k is not None and k_out is None:
-        k_out = torch.empty((rows, hkv, d), dtype=k.dtype, device=k.device)
-    for t, heads in ((q, hq), (k, hkv), (q_out, hq), (k_out, hkv)):
-        if t is not None:
-            # heads of a row side by side; rows at any distance
-            assert t.shape == (rows, heads, d) and t.dtype == q.dtype
-            assert t.stride(2) == 1 and (t.stride(1) == d or heads == 1), "heads of a row must be adjacent"
+        q_out, ldqo = torch.empty((rows, hq, d), dtype=dtype, device=q.device), hq * d
+    else:
+        heads, ldqo = _heads(q_out, rows, d, dtype)
+        assert heads == hq
+    if k is None:
+        k_out, ldko = None, 0
+    elif k_out is None:
+        k_out, ldko = torch.empty((rows, hkv, d), dtype=dtype, device=k.device), hkv * d
+    else:
+        heads, ldko = _heads(k_out, rows, d, dtype)
+        assert heads == hkv
     assert pos.shape == (3, rows) and pos.dtype == torch.int32 and pos.is_contiguous()
     dev = _device(q, k, q_out, k_out, pos)
-
-    def ld(t, heads):
-        return heads * d if rows <= 1 else t.stride(0)
     with _on(dev):
-        check(f(rows, dt, ctypes.byref(cfg.c()), hq, hkv, d, pos.data_ptr(), q.data_ptr(), ld(q, hq),
-                _ptr(k), 0 if k is None else ld(k, hkv), q_out.data_ptr(), ld(q_out, hq),
-                _ptr(k_out), 0 if k is None else ld(k_out, hkv), _stream(dev)))
+        check(f(rows, dt, ctypes.byref(cfg.c()), hq, hkv, d, pos.data_ptr(), q.data_ptr(), ldq,
+                _ptr(k), ldk, q_out.data_ptr(), ldqo, _ptr(k_out), ldko, _stream(dev)))
     return q_out, k_out
 
 
