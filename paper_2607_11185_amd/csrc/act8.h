@@ -43,25 +43,40 @@ __device__ __forceinline__ float scale(int byte) {
   return __builtin_bit_cast(float, byte == NOT_FINITE ? 0x7fc00000u : b);
 }
 
-// codes of four values of a block with exponent byte `byte`, lowest byte first
-// (zeros where the block is not finite).  x 2^-s + 1.5 2^23 rounds to the nearest
-// integer, ties to even, in one operation (the product is exact), and holds that
-// integer in its low bits.
-__device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, int byte) {
-  if (byte >= LAST) {  // rare: the largest numbers of fp32
-    if (byte == NOT_FINITE) return 0u;
-    const float top = 63.f * 0x1p122f;
-    a = fminf(fmaxf(a, -top), top);
-    b = fminf(fmaxf(b, -top), top);
-    c = fminf(fmaxf(c, -top), top);
-    d = fminf(fmaxf(d, -top), top);
+// Values as the codes hold them in the rare blocks of byte >= LAST: below 64 steps, or
+// zeros where the block is not finite (whose 2^-s then is 0 too).
+template <int N>
+__device__ __forceinline__ float rare(float (&v)[N], int byte) {
+  if (byte == NOT_FINITE) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = 0.f;
+    return 0.f;
   }
-  const float inv = inv_scale(byte), magic = 0x1.8p23f;
+  const float top = 63.f * 0x1p122f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) v[j] = fminf(fmaxf(v[j], -top), top);
+  return inv_scale(byte);
+}
+
+// codes of four values, lowest byte first; inv = 2^-s.  x 2^-s + 1.5 2^23 rounds to
+// the nearest integer, ties to even, in one operation (the product is exact), and
+// holds that integer in its low bits.
+__device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, float inv) {
+  const float magic = 0x1.8p23f;
   const unsigned i = __builtin_bit_cast(unsigned, fmaf(a, inv, magic)), j = __builtin_bit_cast(unsigned, fmaf(b, inv, magic));
   const unsigned k = __builtin_bit_cast(unsigned, fmaf(c, inv, magic)), l = __builtin_bit_cast(unsigned, fmaf(d, inv, magic));
   // the low bytes side by side
   return __builtin_amdgcn_perm(__builtin_amdgcn_perm(l, k, 0x0c0c0400u), __builtin_amdgcn_perm(j, i, 0x0c0c0400u),
                                0x05040100u);
+}
+
+// codes of the N values (a multiple of 4) that a lane has of a block
+template <int N>
+__device__ __forceinline__ void codes(float (&v)[N], int byte, unsigned (&c)[N / 4]) {
+  float inv = inv_scale(byte);
+  if (byte >= LAST) inv = rare(v, byte);
+#pragma unroll
+  for (int q = 0; q < N / 4; ++q) c[q] = codes4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], inv);
 }
 
 // value j of four codes

@@ -128,9 +128,11 @@ __global__ void __launch_bounds__(256) k_pack(const ActArgs a) {
     if (n <= 0) continue;
     const int e = act8::exp_byte(top);
     if (col[u] % act8::BLOCK == 0) a.exp[row[u] * a.blocks + col[u] / act8::BLOCK] = (uint8_t)e;
+    unsigned cw[W / 4];
+    act8::codes(f, e, cw);
     typename K::C c;
 #pragma unroll
-    for (int q = 0; q < W / 4; ++q) c[q] = act8::codes4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3], e);
+    for (int q = 0; q < W / 4; ++q) c[q] = cw[q];
     int8_t *d = a.code + row[u] * a.cols + col[u];
     if (n >= W) store_piece<STREAM>(d, c);
     else

@@ -57,18 +57,20 @@ struct EpiGlu {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const f32x4 *g = &acc[bm * 2 + i][0], *u = &acc[bm * 2 + i][2];
-        int eg = 0, eu = 0;
+        unsigned cg[2], cu[2];
         if constexpr (KEEP == CODES) {
           unsigned tg = 0, tu = 0;
+          float vg[8], vu[8];
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              tg = max(tg, act8::mag(g[j][r]));
-              tu = max(tu, act8::mag(u[j][r]));
-            }
-          eg = act8::exp_byte(act8::max_groups(tg));
-          eu = act8::exp_byte(act8::max_groups(tu));
+          for (int j = 0; j < 8; ++j) {
+            vg[j] = g[j / 4][j & 3];
+            vu[j] = u[j / 4][j & 3];
+            tg = max(tg, act8::mag(vg[j]));
+            tu = max(tu, act8::mag(vu[j]));
+          }
+          const int eg = act8::exp_byte(act8::max_groups(tg)), eu = act8::exp_byte(act8::max_groups(tu));
+          act8::codes(vg, eg, cg);
+          act8::codes(vu, eu, cu);
           const int row = t.m0 + t.wr + bm * 32 + i * 16 + t.col;
           const long at = (long)row * ((I + act8::BLOCK - 1) / act8::BLOCK) + f0 / act8::BLOCK;
           if (row < t.M && t.grp == 0) k.g8.exp[at] = (uint8_t)eg;
@@ -87,8 +89,8 @@ struct EpiGlu {
             w[512 + at] = gemm::u32x2{gemm::pack2(uv[0], uv[1]), gemm::pack2(uv[2], uv[3])};
           }
           if constexpr (KEEP == CODES) {
-            wc[at] = act8::codes4(gv[0], gv[1], gv[2], gv[3], eg);
-            wc[256 + at] = act8::codes4(uv[0], uv[1], uv[2], uv[3], eu);
+            wc[at] = cg[j];
+            wc[256 + at] = cu[j];
           }
         }
       }
@@ -169,10 +171,11 @@ __global__ void __launch_bounds__(256) k_finish_glu(const gemm::RestTiles<1> t, 
       ep.k.g8.exp[at] = (uint8_t)eg;
       ep.k.u8.exp[at] = (uint8_t)eu;
     }
-    *reinterpret_cast<uint2 *>(ep.k.g8.code + off) = make_uint2(act8::codes4(g[0], g[1], g[2], g[3], eg),
-                                                                 act8::codes4(g[4], g[5], g[6], g[7], eg));
-    *reinterpret_cast<uint2 *>(ep.k.u8.code + off) = make_uint2(act8::codes4(u[0], u[1], u[2], u[3], eu),
-                                                                 act8::codes4(u[4], u[5], u[6], u[7], eu));
+    unsigned cg[2], cu[2];
+    act8::codes(g, eg, cg);
+    act8::codes(u, eu, cu);
+    *reinterpret_cast<uint2 *>(ep.k.g8.code + off) = make_uint2(cg[0], cg[1]);
+    *reinterpret_cast<uint2 *>(ep.k.u8.code + off) = make_uint2(cu[0], cu[1]);
   }
 }
 
@@ -292,8 +295,12 @@ __global__ void __launch_bounds__(256 * PARTS) k_glu_few(const RowsArgs a, const
         ep.k.g8.exp[at] = (uint8_t)eg;
         ep.k.u8.exp[at] = (uint8_t)eu;
       }
-      ep.k.g8.code[off] = (int8_t)act8::codes4(gv, 0.f, 0.f, 0.f, eg);
-      ep.k.u8.code[off] = (int8_t)act8::codes4(uv, 0.f, 0.f, 0.f, eu);
+      float vg[4] = {gv, 0.f, 0.f, 0.f}, vu[4] = {uv, 0.f, 0.f, 0.f};
+      unsigned cg[1], cu[1];
+      act8::codes(vg, eg, cg);
+      act8::codes(vu, eu, cu);
+      ep.k.g8.code[off] = (int8_t)cg[0];
+      ep.k.u8.code[off] = (int8_t)cu[0];
     }
   }
   if (!in) return;
@@ -410,8 +417,12 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES) k_glu_rows(const RowsArgs a, 
       *reinterpret_cast<gemm::u32x2 *>(ep.k.u16 + off) = gemm::u32x2{gemm::pack2(u[0], u[1]), gemm::pack2(u[2], u[3])};
     }
     if constexpr (KEEP == CODES) {
-      *reinterpret_cast<unsigned *>(ep.k.g8.code + off) = act8::codes4(g[0], g[1], g[2], g[3], eg);
-      *reinterpret_cast<unsigned *>(ep.k.u8.code + off) = act8::codes4(u[0], u[1], u[2], u[3], eu);
+      float vg[4] = {g[0], g[1], g[2], g[3]}, vu[4] = {u[0], u[1], u[2], u[3]};
+      unsigned cg[1], cu[1];
+      act8::codes(vg, eg, cg);
+      act8::codes(vu, eu, cu);
+      *reinterpret_cast<unsigned *>(ep.k.g8.code + off) = cg[0];
+      *reinterpret_cast<unsigned *>(ep.k.u8.code + off) = cu[0];
     }
   }
 }

@@ -17,6 +17,7 @@ namespace seg {
 namespace {
 
 constexpr int MAX_ROWS = 16;       // rows of a block
+constexpr int ITEMS = 4;          // 16-byte pairs of pieces of a thread in flight
 constexpr int CS = 512;            // (cos, sin) pairs of a block
 
 // 16 bytes of a row
@@ -51,7 +52,7 @@ __device__ __forceinline__ void store_piece(T *p, const Piece<T> &x) {
 // rows_per rows a block; half_pow: d/2 rounded up to a power of two; STREAM: more
 // than the caches hold is read and written, so accesses go past them
 template <class T, bool STREAM>
-__global__ void __launch_bounds__(256) k_mrope(const mrope::Args g, int rows_per, int half_pow) {
+__global__ void __launch_bounds__(256, STREAM ? 1 : 5) k_mrope(const mrope::Args g, int rows_per, int half_pow) {
   __shared__ __attribute__((aligned(16))) float2 cs[CS];
   __shared__ int ok[MAX_ROWS];
   typedef Piece<T> E;
@@ -59,6 +60,29 @@ __global__ void __launch_bounds__(256) k_mrope(const mrope::Args g, int rows_per
   const int half = g.d / 2, per = half / W, chunks = (g.a.heads + g.b.heads) * per;
   const long row0 = (long)blockIdx.x * rows_per;
   const int rows = (int)min((long)rows_per, g.rows - row0);
+  // a thread's pieces: ITEMS at a time, the first ones under way during the angles
+  const int items = rows * chunks;
+  E lo[ITEMS], hi[ITEMS];
+  T *to[ITEMS];
+  int at[ITEMS];  // (row, pair) in cs; -1: none
+  auto load = [&](int base) __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < ITEMS; ++n) {
+      const int e = base + n * 256 + threadIdx.x;
+      at[n] = -1;
+      if (e >= items) continue;
+      const int r = e / chunks, q = e - r * chunks, h = q / per, i = (q - h * per) * W;
+      const long row = row0 + r;
+      const bool first = h < g.a.heads;
+      const int hh = first ? h : h - g.a.heads;
+      const T *x = static_cast<const T *>(first ? g.a.x : g.b.x) + row * (first ? g.a.ldx : g.b.ldx) + hh * g.d + i;
+      to[n] = static_cast<T *>(first ? g.a.y : g.b.y) + row * (first ? g.a.ldy : g.b.ldy) + hh * g.d + i;
+      at[n] = r * half + i;
+      lo[n] = load_piece<T, STREAM>(x);
+      hi[n] = load_piece<T, STREAM>(x + half);
+    }
+  };
+  load(0);
   for (int e = threadIdx.x; e < rows * half_pow; e += 256) {
     const int r = e / half_pow, i = e & (half_pow - 1);
     const long row = row0 + r;
@@ -80,38 +104,34 @@ __global__ void __launch_bounds__(256) k_mrope(const mrope::Args g, int rows_per
     }
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < rows * chunks; e += 256) {
-    const int r = e / chunks, q = e - r * chunks, h = q / per, i = (q - h * per) * W;
-    const long row = row0 + r;
-    const bool first = h < g.a.heads;
-    const long lx = first ? g.a.ldx : g.b.ldx, ly = first ? g.a.ldy : g.b.ldy;
-    const int hh = first ? h : h - g.a.heads;
-    const T *x = static_cast<const T *>(first ? g.a.x : g.b.x) + row * lx + hh * g.d + i;
-    T *y = static_cast<T *>(first ? g.a.y : g.b.y) + row * ly + hh * g.d + i;
-    const E lo = load_piece<T, STREAM>(x), hi = load_piece<T, STREAM>(x + half);
-    E olo, ohi;
-    if (ok[r]) {
-      const f32x4 *t = reinterpret_cast<const f32x4 *>(cs + r * half + i);
+  for (int base = 0; base < items; base += ITEMS * 256) {
+    if (base > 0) load(base);
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        const f32x4 w = t[j / 2];
-        const float c = w[(j & 1) * 2], s = w[(j & 1) * 2 + 1];
-        olo.set(j, lo.get(j) * c - hi.get(j) * s);
-        ohi.set(j, hi.get(j) * c + lo.get(j) * s);
-      }
-    } else if (g.inverse) {
+    for (int n = 0; n < ITEMS; ++n) {
+      if (at[n] < 0) continue;
+      E olo, ohi;
+      if (ok[at[n] / half]) {
+        const f32x4 *t = reinterpret_cast<const f32x4 *>(cs + at[n]);
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        olo.set(j, 0.f);
-        ohi.set(j, 0.f);
+        for (int j = 0; j < W; ++j) {
+          const f32x4 w = t[j / 2];
+          const float c = w[(j & 1) * 2], s = w[(j & 1) * 2 + 1];
+          olo.set(j, lo[n].get(j) * c - hi[n].get(j) * s);
+          ohi.set(j, hi[n].get(j) * c + lo[n].get(j) * s);
+        }
+      } else if (g.inverse) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          olo.set(j, 0.f);
+          ohi.set(j, 0.f);
+        }
+      } else {
+        olo = lo[n];
+        ohi = hi[n];
       }
-    } else {
-      if (y == x) continue;
-      olo = lo;
-      ohi = hi;
+      store_piece<T, STREAM>(to[n], olo);
+      store_piece<T, STREAM>(to[n] + half, ohi);
     }
-    store_piece<T, STREAM>(y, olo);
-    store_piece<T, STREAM>(y + half, ohi);
   }
   if (g.zero && g.inverse)
     for (int r = 0; r < rows; ++r)
@@ -144,7 +164,7 @@ void launch(seg_dtype dt, const Args &g, hipStream_t st) {
   const int chunks = (g.a.heads + g.b.heads) * half / (dt == SEG_BF16 ? Piece<unsigned short>::W : Piece<float>::W);
   int hp = 8;
   while (hp < half) hp *= 2;
-  const int want = (1024 + chunks - 1) / chunks;  // about four chunks a thread
+  const int want = (ITEMS * 256 + chunks - 1) / chunks;
   const int rows_per = std::max(1, std::min(std::min(want, MAX_ROWS), CS / hp));
   const long nb = (g.rows + rows_per - 1) / rows_per;
   SEG_CHECK(nb <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "too many rows for one launch");
