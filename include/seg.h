@@ -443,8 +443,10 @@ seg_status seg_act_unpack(int64_t rows, int32_t cols, seg_dtype dt, const seg_ac
  *   x [rows, hidden] (ldx elements between rows, a multiple of 8); wg, wu
  *   [inter, hidden]; m [rows, inter].  g8 and u8 (both or neither NULL): the
  *   values g and u [rows, inter] in 8 bits, formed from the fp32 sums.
- * Supported: hidden and inter multiples of 8, all sizes up to 2^20, tensors on
- * 16-byte boundaries and codes on 8-byte ones (SEG_ERR_UNSUPPORTED otherwise).
+ * Supported: hidden and inter multiples of 8, all sizes up to 2^20, tensors and
+ * workspace on 16-byte boundaries and codes on 8-byte ones
+ * (SEG_ERR_UNSUPPORTED otherwise).  A row's last bits may depend on the number of
+ * rows of the call.
  */
 seg_status seg_glu_fwd(int32_t rows, int32_t hidden, int32_t inter, const void *x, int64_t ldx,
                        const void *wg, const void *wu, void *m, const seg_act8 *g8,

@@ -607,6 +607,10 @@ void check_glu(int32_t rows, int32_t hidden, int32_t inter, int64_t ldx) {
             "hidden %d and inter %d must be positive multiples of 8", hidden, inter);
   SEG_CHECK(rows <= MAX_DIM && hidden <= MAX_DIM && inter <= MAX_DIM, SEG_ERR_UNSUPPORTED,
             "rows %d, hidden %d or inter %d above %d", rows, hidden, inter, MAX_DIM);
+  const long f = act8::blocks_of(inter);  // (a launch holds fewer than 2^32 threads)
+  SEG_CHECK(gemm::tiles_of(rows, 64 * f, 2) <= 1 << 22 && gemm::tiles_of(rows, hidden, 2) <= 1 << 22 &&
+                2 * gemm::tiles_of(inter, hidden, 2) <= 1 << 22,
+            SEG_ERR_CAPACITY, "rows %d, hidden %d and inter %d: too many tiles for one launch", rows, hidden, inter);
   SEG_CHECK(ldx >= hidden, SEG_ERR_ARG, "row stride %lld < hidden %d", (long long)ldx, hidden);
   SEG_CHECK(ldx % 8 == 0 && ldx <= MAX_DIM, SEG_ERR_UNSUPPORTED,
             "row stride %lld must be a multiple of 8 up to %d", (long long)ldx, MAX_DIM);

@@ -671,6 +671,8 @@ extern "C" seg_status seg_mrope_positions(const seg_problem *p, const seg_sizes 
     const int P = (int)sz->packed_tokens;
     if (P == 0) return;
     SEG_CHECK(pos && ws, SEG_ERR_ARG, "pos or ws is NULL");
+    SEG_CHECK(reinterpret_cast<uintptr_t>(ws) % 16 == 0, SEG_ERR_UNSUPPORTED,
+              "ws does not start on a 16-byte boundary");
     const int blocks = (int)((P + (int64_t)TOK_BLOCK - 1) / TOK_BLOCK);
     std::vector<char> tab(w.total);
     std::memcpy(tab.data() + w.run, runs.data(), runs.size() * sizeof(PosRun));

@@ -630,6 +630,7 @@ def _layer_ext(lay, cfg, rope, pos, saved8):
     e, tensors = _lib.SegLayerExt(), []
     if rope is not None:
         import torch
+        assert pos is not None, "rope needs pos"
         assert pos.shape == (3, P) and pos.dtype == torch.int32 and pos.is_contiguous()
         e.rope = ctypes.pointer(rope.c())
         e.pos = pos.data_ptr()

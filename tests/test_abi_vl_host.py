@@ -131,7 +131,8 @@ def test_packing_of_nothing():
 
 @pytest.mark.parametrize("kw,want", [
     (dict(rows=-1), ARG), (dict(rows=(1 << 20) + 1), UNS), (dict(hidden=60), UNS), (dict(inter=100), UNS), (dict(hidden=0), UNS),
-    (dict(inter=(1 << 20) + 8), UNS), (dict(ldx=56), ARG), (dict(ldx=68), UNS), (dict(x=None), ARG), (dict(wu=None), ARG),
+    (dict(inter=(1 << 20) + 8), UNS), (dict(rows=1 << 20, inter=1 << 19), CAP), (dict(hidden=1 << 19, ldx=1 << 19, inter=1 << 20), CAP),
+    (dict(ldx=56), ARG), (dict(ldx=68), UNS), (dict(x=None), ARG), (dict(wu=None), ARG),
     (dict(x=8), UNS), (dict(wg=24), UNS), (dict(u8=False), ARG), (dict(g8=False), ARG), (dict(code=None), ARG), (dict(code=4), UNS)])
 def test_gated_block_refuses(kw, want):
     L = _lib_or_skip()
