@@ -318,9 +318,9 @@ __global__ void __launch_bounds__(256 * PARTS) k_glu_few(const RowsArgs a, const
 // during a step's products.  Lanes past the last feature or row read the last one,
 // and their sums go nowhere; what lies past K reads as zeros on both sides.  2,048 x
 // 2 x 5,504, 16 / 32 / 64 rows: 15.9 / 17.6 / 21.6 us (the GEMM: 30); 3,584 x 2 x
-// 18,944: 71 / 80 / 104 (62 to 66, so the GEMM serves there).  Longer steps need more
-// registers, and then not all blocks fit at once: steps of 128 in four waves 74 / 113 /
-// 372; past the caches, in half lines, 82 at 16 rows.
+// 18,944: 71 / 82 / 103 (62 to 66, so the GEMM serves there).  Steps of 128 in four
+// waves take 74 / 113 / 372; held to six waves a SIMD 98 at 16 rows; past the
+// caches, in half lines, 82 there.
 template <int NB, Keep KEEP>
 __global__ void __launch_bounds__(64 * ROWS_WAVES) k_glu_rows(const RowsArgs a, const EpiGlu<KEEP> ep) {
   __shared__ f32x4 sums[ROWS_WAVES][4 * NB][64];
@@ -378,11 +378,11 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES) k_glu_rows(const RowsArgs a, 
   const int row = 16 * wave + r;
   f32x4 v[4];  // gate of features 4 grp .. and 16 + 4 grp .., up of the same
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    v[b] = sums[0][b * NB + wave][lane];
+  for (int b = 0; b < 4; ++b) v[b] = sums[0][b * NB + wave][lane];
+#pragma unroll 1  // (unrolled, these reads take more registers than the products)
+  for (int w = 1; w < ROWS_WAVES; ++w)
 #pragma unroll
-    for (int w = 1; w < ROWS_WAVES; ++w) v[b] += sums[w][b * NB + wave][lane];
-  }
+    for (int b = 0; b < 4; ++b) v[b] += sums[w][b * NB + wave][lane];
   int eg = 0, eu = 0;
   if constexpr (KEEP == CODES) {
     unsigned tg = 0, tu = 0;
