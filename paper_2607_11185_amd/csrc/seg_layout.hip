@@ -559,6 +559,8 @@ struct Grid {
   int32_t t, h, w, e;
 };
 
+constexpr int POS_BLOCK = 1024;  // rows of a block
+
 // Byte offsets of the positions' workspace: the runs, the grids and the last run at or
 // before each block's first row.
 struct PosWs {
@@ -570,7 +572,7 @@ PosWs pos_ws_layout(const seg_sizes &sz, size_t pieces) {
   w.run = 0;
   w.grid = align_up(sizeof(PosRun) * (pieces + 1));
   w.first = w.grid + align_up(sizeof(Grid) * std::max<size_t>(1, sz.num_steps));
-  w.total = w.first + align_up(4 * ((sz.packed_tokens + TOK_BLOCK - 1) / TOK_BLOCK + 1));
+  w.total = w.first + align_up(4 * ((sz.packed_tokens + POS_BLOCK - 1) / POS_BLOCK + 1));
   return w;
 }
 
@@ -601,34 +603,83 @@ std::vector<PosRun> pos_runs(const seg_problem *p, const Plan &pl, const Grid *g
   return runs;
 }
 
-// pos[axis][row].  A few bytes a row are written and next to nothing is read, so
-// latency bounds it: a block's rows lie in few runs, which the host has found (a
-// search of all runs by every block took 13 us for 1.1M rows; now POSA).
+// pos[axis][row].  Twelve bytes a row are written and next to nothing is read, so
+// latency and index arithmetic bound it.  The host finds the runs of a block's rows (a
+// search of all runs by every block took 13 us for 1.1M rows), a block brings them to
+// LDS in one read (only where they are many, as they are short, it uses them where
+// they are), and a lane takes four rows: one search and one division, then it
+// counts on (with a row a lane 9.6 us, and 20 for 5.2M rows; now 8.4 and 17).
 __global__ void __launch_bounds__(256) k_mrope_pos(const PosRun *__restrict__ runs,
                                                    const Grid *__restrict__ grid,
                                                    const int32_t *__restrict__ block_run, int P,
                                                    int32_t *__restrict__ pos) {
-  const int first = blockIdx.x * TOK_BLOCK, rows = min(TOK_BLOCK, P - first);
-  // the runs of the block: those up to its end start no later than the next block's first
+  constexpr int CAP = 128, ROWS = 4;
+  typedef int Out __attribute__((ext_vector_type(ROWS), aligned(4)));
+  __shared__ PosRun run_lds[CAP];
+  __shared__ Grid grid_lds[CAP];
+  const int first = blockIdx.x * POS_BLOCK, rows = min(POS_BLOCK, P - first);
   const int r0 = block_run[blockIdx.x], cnt = block_run[blockIdx.x + 1] - r0 + 1;
-  for (int o = threadIdx.x; o < rows; o += 256) {
-    const int r = first + o;
-    const PosRun u = runs[r0 + max(0, upper_index(cnt, r, [&](int i) { return runs[r0 + i].row; }))];
-    const int at = r - u.row;
-    int t = -1, h = -1, w = -1;
-    if (at >= 0 && at < u.len) {
-      t = h = w = u.start + at;
-      if (u.step >= 0) {
-        const Grid g = grid[u.step];
-        const int f = at / (g.h * g.w), in = at - f * (g.h * g.w), y = in / g.w;
-        t = u.start + g.e * f;
-        h = u.start + y;
-        w = u.start + (in - y * g.w);
-      }
+  const bool few = cnt <= CAP;
+  if (few) {
+    if (threadIdx.x < cnt) {
+      const PosRun u = runs[r0 + threadIdx.x];
+      run_lds[threadIdx.x] = u;
+      if (u.step >= 0) grid_lds[threadIdx.x] = grid[u.step];
     }
-    pos[r] = t;
-    pos[(long)P + r] = h;
-    pos[2L * P + r] = w;
+    __syncthreads();
+  }
+  auto run_row = [&](int i) { return few ? run_lds[i].row : runs[r0 + i].row; };
+  for (int o = threadIdx.x * ROWS; o < rows; o += 256 * ROWS) {
+    const int n = min(ROWS, rows - o);
+    PosRun u{};
+    Grid g{};
+    int i = max(0, upper_index(cnt, first + o, run_row)) - 1, at = 0, f = 0, y = 0, x = 0;
+    Out t{}, h{}, w{};
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      const int r = first + (o + min(k, n - 1));
+      if (k == 0 || (i + 1 < cnt && run_row(i + 1) <= r && k < n)) {  // the row's run, or a new one
+        ++i;
+        u = few ? run_lds[i] : runs[r0 + i];
+        g = Grid{1, 1, 1, 0};
+        if (u.step >= 0) g = few ? grid_lds[i] : grid[u.step];
+        at = r - u.row;
+        f = y = x = 0;
+        if (k == 0 && u.step >= 0) {
+          const unsigned hw = g.h * g.w;
+          f = (unsigned)at / hw;
+          y = ((unsigned)at - f * hw) / (unsigned)g.w;
+          x = at - f * hw - y * g.w;
+        }
+      } else {
+        ++at;
+        if (++x == g.w) {
+          x = 0;
+          if (++y == g.h) {
+            y = 0;
+            ++f;
+          }
+        }
+      }
+      const bool in = at >= 0 && at < u.len, image = u.step >= 0;
+      t[k] = !in ? -1 : u.start + (image ? g.e * f : at);
+      h[k] = !in ? -1 : u.start + (image ? y : at);
+      w[k] = !in ? -1 : u.start + (image ? x : at);
+    }
+    const long r = first + o;
+    if (n == ROWS) {
+      *reinterpret_cast<Out *>(pos + r) = t;
+      *reinterpret_cast<Out *>(pos + P + r) = h;
+      *reinterpret_cast<Out *>(pos + 2L * P + r) = w;
+    } else {
+#pragma unroll
+      for (int k = 0; k < ROWS - 1; ++k)
+        if (k < n) {
+          pos[r + k] = t[k];
+          pos[P + r + k] = h[k];
+          pos[2L * P + r + k] = w[k];
+        }
+    }
   }
 }
 
@@ -673,13 +724,13 @@ extern "C" seg_status seg_mrope_positions(const seg_problem *p, const seg_sizes 
     SEG_CHECK(pos && ws, SEG_ERR_ARG, "pos or ws is NULL");
     SEG_CHECK(reinterpret_cast<uintptr_t>(ws) % 16 == 0, SEG_ERR_UNSUPPORTED,
               "ws does not start on a 16-byte boundary");
-    const int blocks = (int)((P + (int64_t)TOK_BLOCK - 1) / TOK_BLOCK);
+    const int blocks = (int)((P + (int64_t)POS_BLOCK - 1) / POS_BLOCK);
     std::vector<char> tab(w.total);
     std::memcpy(tab.data() + w.run, runs.data(), runs.size() * sizeof(PosRun));
     if (g) std::memcpy(tab.data() + w.grid, g, sz->num_steps * sizeof(Grid));
     int32_t *first = reinterpret_cast<int32_t *>(tab.data() + w.first);
     for (int b = 0, k = 0; b <= blocks; ++b) {
-      while (k + 1 < (int)runs.size() && runs[k + 1].row <= (int64_t)b * TOK_BLOCK) ++k;
+      while (k + 1 < (int)runs.size() && runs[k + 1].row <= (int64_t)b * POS_BLOCK) ++k;
       first[b] = k;
     }
     SEG_HIP(hipMemcpyAsync(ws, tab.data(), w.total, hipMemcpyHostToDevice, stream));

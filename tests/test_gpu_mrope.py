@@ -62,6 +62,15 @@ def test_positions(name, kw):
     _check_positions(sp, kw["W"], kw["L"], kw.get("buf", 0), kw.get("mode", "sliding"))
 
 
+def test_positions_of_many_short_runs():
+    """Runs of one to three rows, many to a block of rows, with screenshots and without."""
+    rng = np.random.default_rng(9)
+    n = 900
+    sp = WL.explicit_spans([n], [1], rng.choice([0, 1, 2, 3], n), rng.integers(1, 3, n), [0] * n)
+    _check_positions(sp, n, n)
+    _check_positions(sp, 40, 300, buf=4096)
+
+
 @pytest.mark.parametrize("seed", range(6))
 def test_positions_random(seed):
     rng = np.random.default_rng(100 + seed)
