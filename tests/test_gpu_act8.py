@@ -98,3 +98,19 @@ def test_empty():
     import torch
     x = torch.empty(0, 40, device="cuda")
     assert S.seg_act_unpack(S.seg_act_pack(x), torch.float32).shape == (0, 40)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 31), (7, 100), (33, 1001), (301, 3584)])
+def test_nothing_is_written_past_the_end(rows, cols):
+    import torch
+    x = torch.randn(rows, cols, device="cuda")
+    code = torch.full((rows * cols + 999,), 77, dtype=torch.int8, device="cuda")
+    nb = -(-cols // 32)
+    exp = torch.full((rows * nb + 999,), 77, dtype=torch.uint8, device="cuda")
+    out = S.Act8(code[:rows * cols].view(rows, cols), exp[:rows * nb].view(rows, nb))
+    S.seg_act_pack(x, out)
+    assert bool((code[rows * cols:] == 77).all()) and bool((exp[rows * nb:] == 77).all())
+    for dt in (torch.bfloat16, torch.float32):
+        v = torch.full((rows * cols + 999,), 77, dtype=dt, device="cuda")
+        S.seg_act_unpack(out, x=v[:rows * cols].view(rows, cols))
+        assert bool((v[rows * cols:] == 77).all())

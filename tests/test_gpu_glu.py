@@ -148,7 +148,8 @@ def test_backward_from_kept_values(shape, dw):
     _within(_np(out["m"]), m, h * np.abs(m) * (1 + 1e-5) + np.abs(m) * (np.abs(gv) + 8) * 2.0 ** -22 + 1e-38, "m")
 
 
-@pytest.mark.parametrize("shape", [(17, 328, 200), (300, 128, 1032)], ids=str)
+# (a kernel for few rows, for some tens, the GEMM whole and in parts: each in its bf16 form)
+@pytest.mark.parametrize("shape", [(17, 328, 200), (300, 128, 1032), (3, 520, 136), (70, 1040, 40), (7, 256, 264)], ids=str)
 def test_backward_without_kept_values(shape):
     """Gate and up values computed again, in bf16: their rounding (2^-8) moves dg and du
     by a few times that, independently, so 2^-6 bounds the relative Frobenius error."""
@@ -203,3 +204,36 @@ def test_no_rows_give_zero_weight_gradients():
         nan = {n: torch.full((72, 64), float("nan"), dtype=dt, device="cuda") for n in ("dwg", "dwu")}
         S.seg_glu_bwd(x[:0], wg, wu, dm[:0], None, out=dict(nan, dx=x[:0].contiguous(), m=None))
         assert not nan["dwg"].any() and not nan["dwu"].any()
+
+
+@pytest.mark.parametrize("shape", [(1, 64, 40), (3, 72, 104), (17, 328, 200), (130, 264, 520), (257, 512, 72), (70, 1040, 8),
+                                   LARGE], ids=str)
+def test_nothing_is_written_past_the_end(shape):
+    """Outputs as the first part of larger buffers, workspaces of exactly the size that is asked
+    for: what lies behind stays as it was."""
+    import torch
+    rows, hidden, inter = shape
+    x, wg, wu, dm = _inputs(*shape, seed=6)
+
+    def room(shape, dtype):
+        n = int(np.prod(shape))
+        flat = torch.full((n + 4096,), 77, dtype=dtype, device="cuda")
+        return flat[:n].view(shape), flat[n:]
+    bf, nb = torch.bfloat16, -(-inter // 32)
+    m, m_end = room((rows, inter), bf)
+    codes = [room((rows, inter), torch.int8) for _ in range(2)]
+    exps = [room((rows, nb), torch.uint8) for _ in range(2)]
+    kept = tuple(S.Act8(c[0], e[0]) for c, e in zip(codes, exps))
+    ends = [m_end, *(c[1] for c in codes), *(e[1] for e in exps)]
+    ws, end = room((S.glu_workspace(*shape, False, False, "cuda").numel(),), torch.uint8)
+    S.seg_glu_fwd(x, wg, wu, keep=kept, m=m, ws=ws)
+    ends.append(end)
+    for k in (kept, None):
+        for dt in (bf, torch.float32):
+            out = {n: room(s, t) for n, s, t in (("dx", (rows, hidden), bf), ("dwg", (inter, hidden), dt),
+                                                 ("dwu", (inter, hidden), dt), ("m", (rows, inter), bf))}
+            ws, end = room((S.glu_workspace(*shape, True, k is not None, "cuda").numel(),), torch.uint8)
+            S.seg_glu_bwd(x, wg, wu, dm, k, out={n: t[0] for n, t in out.items()}, ws=ws)
+            ends += [end, *(t[1] for t in out.values())]
+    for i, e in enumerate(ends):
+        assert bool((e == 77).all()), i

@@ -188,6 +188,23 @@ def test_chunking_leaves_what_is_kept_unchanged():
             assert torch.equal(_rows(pad, getattr(kept[0][1][n], f)), _rows(pad, getattr(kept[1][1][n], f))), (n, f)
 
 
+@pytest.mark.parametrize("keep_gate", [False, True])
+def test_workspaces_of_the_size_asked_for(keep_gate):
+    """Nothing is read or written behind a workspace of exactly that size."""
+    import torch
+    lr = ExtRun(*CASES["d64_gqa4_buffers"])
+    res = []
+    for fill in (0, 255):
+        s8 = S.layer_saved8(lr.lay, lr.lc, keep_gate)
+        sizes = [S.layer_ext_workspace(lr.lay, lr.lc, True, b).numel() for b in (False, True)]
+        ws = [torch.full((n + 65536,), fill, dtype=torch.uint8, device=lr.dev) for n in sizes]
+        y, _ = S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, lr.rope, lr.pos, saved8=s8, ws=ws[0][:sizes[0]])
+        dx, g = S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, lr.dy, lr.rope, lr.pos, saved8=s8, ws=ws[1][:sizes[1]])
+        assert all(bool((w[n:] == fill).all()) for w, n in zip(ws, sizes))
+        res.append([_rows(lr.pad, y), dx, *g.values()])
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
 def test_capture_and_replay_of_the_operators_together():
     """Rotation, packing, the gated block and the extended layer in one graph, replayed
     between eager work: every replay equals the eager run."""

@@ -39,8 +39,11 @@ def _check_positions(sp, W, L, buf=0, mode="sliding", cap=0, seed=0):
     grid = _grid(sp.img_len, rng)
     pr = S.Problem.from_spans(sp, W, L, cap, buf, 128, mode)
     lay = S.seg_build_layout(pr)
-    pos = torch.full((3, lay.sizes.packed_tokens), 12345, dtype=torch.int32, device="cuda")
+    n = 3 * lay.sizes.packed_tokens
+    flat = torch.full((n + 999,), 12345, dtype=torch.int32, device="cuda")
+    pos = flat[:n].view(3, -1)
     S.seg_mrope_positions(pr, lay, grid, pos)
+    assert bool((flat[n:] == 12345).all())
     ref = OL.build(sp, W, L, 128, cap=cap, buffer_tokens=buf, with_tiles=False, mode=mode)
     want = OM.positions(ref, sp, grid, ref.packed_tokens)
     say(f"positions: {lay.sizes.packed_tokens} rows, {lay.sizes.num_segments} segments")
@@ -128,8 +131,9 @@ def test_rotation(case, dtype):
     k = _rows(rows, hkv, d, dt, hkv + 1, 1, gen) if hkv else None
     pn = pos.cpu().numpy()
     for f, inverse in ((S.seg_mrope_fwd, False), (S.seg_mrope_bwd, True)):
-        qo = torch.full((rows, hq + 1, d), 7.0, dtype=dt, device="cuda")
-        got = f(q, k, pos, cfg, qo[:, :hq])
+        qo = torch.full((rows + 3, hq + 1, d), 7.0, dtype=dt, device="cuda")
+        got = f(q, k, pos, cfg, qo[:rows, :hq])
+        assert bool((qo[rows:] == 7.0).all())
         for x, y in zip((q, k), got):
             if x is None:
                 assert y is None
@@ -142,7 +146,7 @@ def test_rotation(case, dtype):
             over = err - _bound(xn, ref, dt) - far
             worst = float(over.max())
             assert worst <= 0, (case, dtype, inverse, worst)
-        assert bool((qo[:, hq] == 7.0).all())    # what lies between the rows is left alone
+        assert bool((qo[:, hq] == 7.0).all())    # what lies between the rows and behind them is left alone
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
