@@ -429,8 +429,7 @@ typedef struct {
 } seg_act8;
 
 /* x [rows, cols] (dtype dt, ldx >= cols elements between rows) to 8 bits and
- * back.  Any cols >= 1; 16-byte accesses where cols is a multiple of 8 and x's
- * rows (codes: 8-byte) are aligned. */
+ * back.  Any cols >= 1, rows at any alignment of an element. */
 seg_status seg_act_pack(int64_t rows, int32_t cols, seg_dtype dt, const void *x, int64_t ldx,
                         const seg_act8 *out, hipStream_t stream);
 seg_status seg_act_unpack(int64_t rows, int32_t cols, seg_dtype dt, const seg_act8 *in, void *x,

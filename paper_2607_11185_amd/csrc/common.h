@@ -79,9 +79,9 @@ inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 // Bytes read and written from which on a single pass over memory goes past the
 // caches: what it leaves there would be evicted before anybody reads it, and the
 // lines of others with it.  Measured in turns over three sets of tensors, us through
-// the caches / past them: rotation of 64 MB 13.1 / 15.4, 128 MB 28.9 / 26.7, 1 GB 191 /
-// 180; unpacking of 64 MB 11.4 / 14.6, 128 MB 26.7 / 24.1, 1 GB 179 / 168; packing
-// of 1 GB 182 / 162.
+// the caches / past them: a rotation of 64 MB 13.1 / 15.4, of 128 MB 28.9 / 26.7, of 1 GB
+// 191 / 180; unpacking of 64 MB 11.4 / 14.6, of 128 MB 26.7 / 24.1, of 1 GB 179 / 168;
+// packing of 1 GB 182 / 162.
 constexpr long STREAM_BYTES = 96L << 20;
 
 // Carves aligned sub-buffers out of a caller workspace.

@@ -374,6 +374,13 @@ def _device(*tensors):
     return dev
 
 
+def _current(dev) -> int:
+    """The handle of the GPU's current stream (as _stream, without the 2 us of making a
+    Stream object of it)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(dev.index)
+
+
 def _on(dev):
     """Calls are made with the tensors' GPU as the current one."""
     import torch
@@ -417,7 +424,7 @@ def seg_mrope_positions(problem: Problem, lay: Layout, grid, pos=None, ws=None):
     with _on(dev):
         check(L.seg_mrope_positions(ctypes.byref(pc), ctypes.byref(lay.sizes),
                                     None if grid is None else grid.ctypes.data, pos.data_ptr(),
-                                    ws.data_ptr(), ws.numel(), _stream(dev)))
+                                    ws.data_ptr(), ws.numel(), _current(dev)))
     return pos
 
 
@@ -437,14 +444,14 @@ def _mrope(f, q, k, pos, cfg: MropeCfg, q_out, k_out):
     hq, ldq = _heads(q, rows, d, dtype)
     hkv, ldk = (0, 0) if k is None else _heads(k, rows, d, dtype)
     if q_out is None:
-        q_out, ldqo = torch.empty((rows, hq, d), dtype=dtype, device=q.device), hq * d
+        q_out, ldqo = q.new_empty((rows, hq, d)), hq * d
     else:
         heads, ldqo = _heads(q_out, rows, d, dtype)
         assert heads == hq
     if k is None:
         k_out, ldko = None, 0
     elif k_out is None:
-        k_out, ldko = torch.empty((rows, hkv, d), dtype=dtype, device=k.device), hkv * d
+        k_out, ldko = k.new_empty((rows, hkv, d)), hkv * d
     else:
         heads, ldko = _heads(k_out, rows, d, dtype)
         assert heads == hkv
@@ -452,7 +459,7 @@ def _mrope(f, q, k, pos, cfg: MropeCfg, q_out, k_out):
     dev = _device(q, k, q_out, k_out, pos)
     with _on(dev):
         check(f(rows, dt, ctypes.byref(cfg.c()), hq, hkv, d, pos.data_ptr(), q.data_ptr(), ldq,
-                _ptr(k), ldk, q_out.data_ptr(), ldqo, _ptr(k_out), ldko, _stream(dev)))
+                _ptr(k), ldk, q_out.data_ptr(), ldqo, _ptr(k_out), ldko, _current(dev)))
     return q_out, k_out
 
 
@@ -502,12 +509,14 @@ def seg_act_pack(x, out: Optional[Act8] = None) -> Act8:
     rows, cols = x.shape
     dt = _dtype_code(x)
     if out is None:
-        out = Act8.empty(rows, cols, x.device)
+        import torch
+        out = Act8(x.new_empty((rows, cols), dtype=torch.int8),
+                   x.new_empty((rows, -(-cols // 32)), dtype=torch.uint8))
     assert out.code.shape == (rows, cols)
     dev = _device(x, out.code, out.exp)
     with _on(dev):
         check(_lib.lib().seg_act_pack(rows, cols, dt, x.data_ptr(), _rows(x), ctypes.byref(out.c()),
-                                      _stream(dev)))
+                                      _current(dev)))
     return out
 
 
@@ -521,7 +530,7 @@ def seg_act_unpack(act: Act8, dtype=None, x=None):
     dev = _device(x, act.code, act.exp)
     with _on(dev):
         check(_lib.lib().seg_act_unpack(rows, cols, _dtype_code(x), ctypes.byref(act.c()),
-                                        x.data_ptr(), _rows(x), _stream(dev)))
+                                        x.data_ptr(), _rows(x), _current(dev)))
     return x
 
 
@@ -557,7 +566,7 @@ def seg_glu_fwd(x, wg, wu, keep=False, m=None, ws=None):
     import torch
     rows, hidden, inter = _glu_args(x, wg, wu)
     if m is None:
-        m = torch.empty((rows, inter), dtype=torch.bfloat16, device=x.device)
+        m = x.new_empty((rows, inter))
     assert m.shape == (rows, inter) and m.dtype == torch.bfloat16 and m.is_contiguous()
     if keep is True:
         keep = (Act8.empty(rows, inter, x.device), Act8.empty(rows, inter, x.device))
@@ -569,7 +578,7 @@ def seg_glu_fwd(x, wg, wu, keep=False, m=None, ws=None):
     with _on(dev):
         check(_lib.lib().seg_glu_fwd(rows, hidden, inter, x.data_ptr(), _rows(x), wg.data_ptr(),
                                      wu.data_ptr(), m.data_ptr(), *c, ws.data_ptr(), ws.numel(),
-                                     _stream(dev)))
+                                     _current(dev)))
     return m, kept
 
 
@@ -602,7 +611,7 @@ def seg_glu_bwd(x, wg, wu, dm, kept=None, dw_dtype=None, want_m=True, out=None, 
                                      wu.data_ptr(), *c, dm.data_ptr(), _ptr(out.get("m")),
                                      out["dx"].data_ptr(), _dtype_code(out["dwg"]),
                                      out["dwg"].data_ptr(), out["dwu"].data_ptr(), ws.data_ptr(),
-                                     ws.numel(), _stream(dev)))
+                                     ws.numel(), _current(dev)))
     return out
 
 
@@ -713,7 +722,7 @@ def seg_layer_fwd_ext(lay: Layout, cfg: LayerCfg, w: dict, x, rope: Optional[Mro
         check(_lib.lib().seg_layer_fwd_ext(
             ctypes.byref(lay.c), ctypes.byref(lay.sizes), ctypes.byref(cfg.c()), ctypes.byref(e),
             ctypes.byref(_layer_weights(w)), x.data_ptr(), y.data_ptr(), sv, ws.data_ptr(),
-            ws.numel(), _stream(dev)))
+            ws.numel(), _current(dev)))
     return y, saved if saved8 is None else saved8
 
 
@@ -747,5 +756,5 @@ def seg_layer_bwd_ext(lay: Layout, cfg: LayerCfg, w: dict, dy, rope: Optional[Mr
         check(_lib.lib().seg_layer_bwd_ext(
             ctypes.byref(lay.c), ctypes.byref(lay.sizes), ctypes.byref(cfg.c()), ctypes.byref(e),
             ctypes.byref(_layer_weights(w)), None if saved8 is not None else x.data_ptr(), sv,
-            dy.data_ptr(), dx.data_ptr(), ctypes.byref(g), ws.data_ptr(), ws.numel(), _stream(dev)))
+            dy.data_ptr(), dx.data_ptr(), ctypes.byref(g), ws.data_ptr(), ws.numel(), _current(dev)))
     return dx, grads
