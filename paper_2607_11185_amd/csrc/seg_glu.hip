@@ -22,7 +22,15 @@ using gemm::ST;
 constexpr int MAX_DIM = 1 << 20;  // GEMM rows are addressed with 32-bit offsets
 constexpr long MAX_SUMS = 64L << 20;  // fp32 partial sums of a launch at most (256 MB)
 
-__device__ __forceinline__ float sigmoidf_(float g) { return 1.f / (1.f + __expf(-g)); }
+// 1 / (1 + exp(-g)): the reciprocal and one step towards 1 / x, which has the bits of
+// the division 1.f / x at every float x in [1, 2^126) (all tried); the fixup makes inf
+// 0 and keeps NaN.  Past 2^126 (g < -87.3) the result is 0, off by less than 2^-126.
+// Half the instructions of the division: 1555 -> 1531 us for the gate and up product
+// of 8192 x 3584 x 18944, 66.9 -> 65.1 us for 1500 x 2048 x 5504.
+__device__ __forceinline__ float sigmoidf_(float g) {
+  const float x = 1.f + __expf(-g), r = __builtin_amdgcn_rcpf(x);
+  return __builtin_amdgcn_div_fixupf(fmaf(fmaf(-x, r, 1.f), r, r), x, 1.f);
+}
 
 enum Keep { NONE, BF16, CODES };
 

@@ -196,6 +196,39 @@ def test_extremes():
     assert torch.equal(kept2[0].code[rows], kept[0].code[rows])
 
 
+@pytest.mark.parametrize("rows", [1, 22, 300])
+def test_gates_over_the_whole_range(rows):
+    """g = x[:, 0] and u = 1 exactly, down to where exp(-g) leaves fp32: there the sigmoid
+    may be off by 2^-126, elsewhere by the exponential's and four more roundings."""
+    import torch
+    steps = [0, 2.0 ** -120, 1e-3, 1, 1.28125, 5, 20, 80, 87, 87.5, 88, 88.5, 89, 104, 1e4, 3e38]
+    v = torch.tensor([s * t for t in steps for s in (1, -1)]).to(torch.bfloat16)
+    for v in v.split(1) if rows == 1 else [v.repeat(-(-rows // len(v)))[-rows:]]:
+        x = torch.zeros(len(v), 64, dtype=torch.bfloat16)
+        x[:, 0], x[:, 1] = v, 1
+        wg, wu = torch.zeros(2, 64, 64, dtype=torch.bfloat16)
+        wg[:, 0] = wu[:, 1] = 1
+        x, wg, wu = x.cuda(), wg.cuda(), wu.cuda()
+        m, kept = S.seg_glu_fwd(x, wg, wu, keep=True)
+        g = v.double().numpy()
+        for g, name in ((g, "m"), (_np(S.seg_act_unpack(kept[0], torch.float32))[:, 0], "dx")):
+            with np.errstate(over="ignore"):
+                s, c = OG.sigmoid(g), np.minimum(np.abs(g), 110)  # past 110 the sigmoid is 0 or 1
+            es = s * ((1 - s) * (c + 8) + 2) * 2.0 ** -23 + (g < -87.3) * 2.0 ** -126
+            em = c * es + 2.0 ** -8 * np.abs(g * s) + 2.0 ** -133
+            if name == "m":
+                _within(_np(m), (g * s)[:, None], em[:, None] * 1.01, name)
+                continue
+            # from the kept g (8 bits: not x's own); 64 equal terms, their sum rounded again
+            dx = _np(S.seg_glu_bwd(x, wg, wu, torch.ones_like(m), kept)["dx"])
+            d = s * (1 + g * (1 - s))
+            ed = es * (1 + 2 * c) + s * (1 + c * (1 - s)) * 2.0 ** -22 + 2.0 ** -8 * np.abs(d) + 2.0 ** -133
+            for at, ref, e in ((0, d, ed), (1, g * s, em)):
+                fits = np.abs(ref) < 4e36
+                got = np.where(fits, dx[:, at], 64 * ref)
+                _within(got, 64 * ref, 64 * 1.01 * (e + 2.0 ** -8 * np.abs(ref)), at)
+
+
 def test_no_rows_give_zero_weight_gradients():
     import torch
     x, wg, wu, dm = _inputs(4, 64, 72)
