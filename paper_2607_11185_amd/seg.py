@@ -634,11 +634,12 @@ def layer_saved8(lay: Layout, cfg: LayerCfg, keep_gate=False) -> dict:
 
 
 def _layer_ext(lay, cfg, rope, pos, saved8):
-    """The C struct, and the tensors it points to."""
+    """The C struct, and the tensors that have to be on the layer's GPU with it."""
+    import torch
     P = lay.sizes.packed_tokens
-    e, tensors = _lib.SegLayerExt(), []
+    e, tensors = _lib.SegLayerExt(), [lay.tok_meta]
+    assert rope is not None or pos is None, "pos needs rope"
     if rope is not None:
-        import torch
         assert pos is not None, "rope needs pos"
         assert pos.shape == (3, P) and pos.dtype == torch.int32 and pos.is_contiguous()
         e.rope = ctypes.pointer(rope.c())
@@ -657,7 +658,7 @@ def _layer_ext(lay, cfg, rope, pos, saved8):
             tensors += [a.code, a.exp]
         for n, size in (("lse", cfg.hq * P), ("rstd1", P), ("rstd2", P)):
             t = saved8[n]
-            assert t.numel() == size and t.is_contiguous() and t.element_size() == 4, n
+            assert t.numel() == size and t.is_contiguous() and t.dtype == torch.float32, n
             setattr(s, n, t.data_ptr())
             tensors.append(t)
         e.saved8 = ctypes.pointer(s)

@@ -212,3 +212,23 @@ def test_extended_layer_refuses():
     both(ext(sections=None, gate=False), WS, n=size(1, 0) - 1)
     both(None, ARG, saved=None)              # nothing to save into
     both(_lib.SegLayerExt(), ARG, x=None)
+
+
+def test_layer_binding_refuses():
+    """Positions without their sections and base, saved vectors of another type, a layout
+    on another device than the tensors."""
+    import torch
+    _lib_or_skip()
+    sz = S.seg_layout_query(_prob())
+    lay, cfg = S.Layout(sz, torch.device("cpu")), S.LayerCfg(256, 512, 4, 2, 64)
+    P = sz.packed_tokens
+    pos = torch.zeros(3, P, dtype=torch.int32)
+    s8 = S.layer_saved8(lay, cfg)
+    S._layer_ext(lay, cfg, S.MropeCfg((8, 12, 12)), pos, s8)
+    for rope, p, saved in ((None, pos, None), (S.MropeCfg((8, 12, 12)), None, None),
+                           (None, None, dict(s8, lse=s8["lse"].int())),
+                           (None, None, dict(s8, rstd1=s8["rstd1"][:-1])),
+                           (None, None, {n: v for n, v in s8.items() if n != "y1"})):
+        with pytest.raises(AssertionError):
+            S._layer_ext(lay, cfg, rope, p, saved)
+    assert any(t is lay.tok_meta for t in S._layer_ext(lay, cfg, None, None, None)[1])
