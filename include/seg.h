@@ -444,8 +444,9 @@ seg_status seg_act_unpack(int64_t rows, int32_t cols, seg_dtype dt, const seg_ac
  *   values g and u [rows, inter] in 8 bits, formed from the fp32 sums.
  * Supported: hidden and inter multiples of 8, all sizes up to 2^20, tensors and
  * workspace on 16-byte boundaries and codes on 8-byte ones
- * (SEG_ERR_UNSUPPORTED otherwise).  A row's last bits may depend on the number of
- * rows of the call.
+ * (SEG_ERR_UNSUPPORTED otherwise).  Outputs and workspace overlap neither an
+ * input nor each other (SEG_ERR_ARG; here and in the backward).  A row's last bits
+ * may depend on the number of rows of the call.
  */
 seg_status seg_glu_fwd(int32_t rows, int32_t hidden, int32_t inter, const void *x, int64_t ldx,
                        const void *wg, const void *wu, void *m, const seg_act8 *g8,

@@ -639,6 +639,24 @@ bool check_kept(const seg_act8 *g, const seg_act8 *u) {
   return true;
 }
 
+struct Span {
+  const void *p;
+  size_t bytes;
+};
+
+// what a call writes shares no byte with what it reads, nor one output with another
+void check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  auto meet = [](const Span &a, const Span &b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+  };
+  for (const Span *o = outs.begin(); o != outs.end(); ++o) {
+    for (const Span &i : ins) SEG_CHECK(!meet(*o, i), SEG_ERR_ARG, "an output or the workspace overlaps an input");
+    for (const Span *q = outs.begin(); q != o; ++q)
+      SEG_CHECK(!meet(*o, *q), SEG_ERR_ARG, "an output overlaps another or the workspace");
+  }
+}
+
 #define US(p) reinterpret_cast<unsigned short *>(p)
 #define CUS(p) reinterpret_cast<const unsigned short *>(p)
 
@@ -692,6 +710,9 @@ extern "C" seg_status seg_glu_fwd(int32_t rows, int32_t hidden, int32_t inter, c
       keep.g8 = *g8;
       keep.u8 = *u8;
     }
+    const size_t R = rows, H = hidden, I = inter, W = I * H * 2, E = R * act8::blocks_of(inter);
+    check_apart({{m, R * I * 2}, {ws, need}, {keep.g8.code, R * I}, {keep.g8.exp, E}, {keep.u8.code, R * I}, {keep.u8.exp, E}},
+                {{x, ((R - 1) * ldx + H) * 2}, {wg, W}, {wu, W}});
     ProfScope prof("glu_fwd", stream);
     glu::forward(CUS(x), ldx, CUS(wg), CUS(wu), rows, hidden, inter, US(m), keep, static_cast<float *>(ws), stream);
   });
@@ -724,6 +745,11 @@ extern "C" seg_status seg_glu_bwd(int32_t rows, int32_t hidden, int32_t inter, c
     SEG_CHECK(ws_bytes >= W.total, SEG_ERR_WORKSPACE, "workspace of %zu bytes < required %zu", ws_bytes, W.total);
     SEG_CHECK(ws, SEG_ERR_ARG, "ws is NULL");
     check_aligned({ws}, 16);
+    const seg_act8 none{}, &gk = has ? *g8 : none, &uk = has ? *u8 : none;
+    const size_t R = rows, H = hidden, I = inter, E = R * act8::blocks_of(inter), D = I * H * (dw_dt == SEG_BF16 ? 2 : 4);
+    check_apart({{m, R * I * 2}, {dx, R * H * 2}, {dwg, D}, {dwu, D}, {ws, W.total}},
+                {{x, ((R - 1) * ldx + H) * 2}, {wg, I * H * 2}, {wu, I * H * 2}, {dm, R * I * 2}, {gk.code, R * I},
+                 {gk.exp, E}, {uk.code, R * I}, {uk.exp, E}});
     char *base = static_cast<char *>(ws);
     unsigned short *dg = US(base + W.dg), *du = US(base + W.du);
     const gemm::Scratch sums{reinterpret_cast<float *>(base + W.sums), W.sum_elems};

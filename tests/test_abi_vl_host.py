@@ -168,6 +168,35 @@ def test_gated_block_backward_refuses():
     assert L.seg_glu_fwd(0, 64, 96, None, 64, None, None, None, None, None, None, 0, None) == _lib.SEG_OK
 
 
+def test_gated_block_refuses_overlapping_tensors():
+    """An output or the workspace on an input, or on another output: dx over x for one,
+    which the weight gradients read afterwards."""
+    L = _lib_or_skip()
+    R, H, I = 4, 64, 96
+    size = {"x": R * H * 2, "wg": I * H * 2, "wu": I * H * 2, "m": R * I * 2, "dm": R * I * 2, "dx": R * H * 2,
+            "dwg": I * H * 4, "dwu": I * H * 4, "gc": R * I, "ge": R * 3, "uc": R * I, "ue": R * 3}
+    need = {0: L.seg_glu_workspace_bytes(R, H, I, 0, 0), 1: L.seg_glu_workspace_bytes(R, H, I, 1, 1)}
+    at, names = {}, {0: ["x", "wg", "wu", "m", "gc", "ge", "uc", "ue", "ws"],
+                     1: ["x", "wg", "wu", "m", "gc", "ge", "uc", "ue", "dm", "dx", "dwg", "dwu", "ws"]}
+    for i, n in enumerate([*size, "ws"]):
+        at[n] = (i + 1) << 20
+
+    def call(bwd, p):
+        g8, u8 = ctypes.byref(_lib.SegAct8(p["gc"], p["ge"])), ctypes.byref(_lib.SegAct8(p["uc"], p["ue"]))
+        if bwd:
+            return L.seg_glu_bwd(R, H, I, p["x"], H, p["wg"], p["wu"], g8, u8, p["dm"], p["m"], p["dx"], 1, p["dwg"],
+                                 p["dwu"], p["ws"], need[1], None)
+        return L.seg_glu_fwd(R, H, I, p["x"], H, p["wg"], p["wu"], p["m"], g8, u8, p["ws"], need[0], None)
+    for bwd in (0, 1):
+        size["ws"] = need[bwd]
+        outs = {"ws", "m", "dx", "dwg", "dwu"} if bwd else {"ws", "m", "gc", "ge", "uc", "ue"}
+        for a in names[bwd]:
+            for b in names[bwd]:
+                if a != b and a in outs:
+                    assert call(bwd, dict(at, **{a: at[b]})) == ARG, (bwd, a, b)
+                    assert call(bwd, dict(at, **{a: at[b] + (size[b] - 1) // 16 * 16})) == ARG, (bwd, a, b)
+
+
 def test_extended_layer_refuses():
     L = _lib_or_skip()
     sz = S.seg_layout_query(_prob())
