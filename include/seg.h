@@ -397,7 +397,7 @@ typedef struct {
  * in fp64; fp32 tensors are rotated in fp32.  ldq, ldk, ldqo, ldko: elements
  * between rows (at least heads * d), so q and k may be parts of one
  * projection's rows; an output may be its input (same pointer and stride), and
- * must not overlap an input otherwise.  Rows with a negative position on any
+ * must not overlap an input otherwise (SEG_ERR_ARG).  Rows with a negative position on any
  * axis are padding: seg_mrope_fwd copies them, and seg_mrope_bwd, which turns
  * dq and dk back (the transpose: gradients of the unrotated q and k), writes
  * zeros there.  Supported: d a multiple of 16 up to 256, rows on 16-byte
@@ -429,7 +429,8 @@ typedef struct {
 } seg_act8;
 
 /* x [rows, cols] (dtype dt, ldx >= cols elements between rows) to 8 bits and
- * back.  Any cols >= 1, rows at any alignment of an element. */
+ * back.  Any cols >= 1, rows at any alignment of an element; the three arrays share
+ * no memory (SEG_ERR_ARG). */
 seg_status seg_act_pack(int64_t rows, int32_t cols, seg_dtype dt, const void *x, int64_t ldx,
                         const seg_act8 *out, hipStream_t stream);
 seg_status seg_act_unpack(int64_t rows, int32_t cols, seg_dtype dt, const seg_act8 *in, void *x,

@@ -5,6 +5,7 @@
 
 #include <cstdint>
 #include <cstdio>
+#include <initializer_list>
 #include <string>
 
 #include "seg.h"
@@ -83,6 +84,24 @@ inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 // 191 / 180; unpacking of 64 MB 11.4 / 14.6, of 128 MB 26.7 / 24.1, of 1 GB 179 / 168;
 // packing of 1 GB 182 / 162.
 constexpr long STREAM_BYTES = 96L << 20;
+
+struct Span {
+  const void *p;
+  size_t bytes;
+};
+
+// what a call writes shares no byte with what it reads, nor one output with another
+inline void check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  auto meet = [](const Span &a, const Span &b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+  };
+  for (const Span *o = outs.begin(); o != outs.end(); ++o) {
+    for (const Span &i : ins) SEG_CHECK(!meet(*o, i), SEG_ERR_ARG, "an output or the workspace overlaps an input");
+    for (const Span *q = outs.begin(); q != o; ++q)
+      SEG_CHECK(!meet(*o, *q), SEG_ERR_ARG, "an output overlaps another or the workspace");
+  }
+}
 
 // Carves aligned sub-buffers out of a caller workspace.
 struct Carver {

@@ -215,6 +215,8 @@ void act_launch(ActArgs &a, seg_dtype dt, F &&kernel) {
   const int unroll = n > 2048 * 256 ? 4 : 1;
   const long nb = (n + 256 * unroll - 1) / (256 * unroll);
   SEG_CHECK(nb <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "tensor too large for one launch");
+  check_apart({{a.code, (size_t)a.rows * a.cols}, {a.exp, (size_t)a.rows * a.blocks}},
+              {{a.x, ((size_t)(a.rows - 1) * a.ldx + a.cols) * (dt == SEG_BF16 ? 2 : 4)}});
   a.narrow = nb * 256 * unroll <= 0xffffffffL;
   const double bytes = (double)a.rows * a.cols * (dt == SEG_BF16 ? 3 : 5);
   auto go = [&](auto t) {

@@ -639,24 +639,6 @@ bool check_kept(const seg_act8 *g, const seg_act8 *u) {
   return true;
 }
 
-struct Span {
-  const void *p;
-  size_t bytes;
-};
-
-// what a call writes shares no byte with what it reads, nor one output with another
-void check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
-  auto meet = [](const Span &a, const Span &b) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-    return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
-  };
-  for (const Span *o = outs.begin(); o != outs.end(); ++o) {
-    for (const Span &i : ins) SEG_CHECK(!meet(*o, i), SEG_ERR_ARG, "an output or the workspace overlaps an input");
-    for (const Span *q = outs.begin(); q != o; ++q)
-      SEG_CHECK(!meet(*o, *q), SEG_ERR_ARG, "an output overlaps another or the workspace");
-  }
-}
-
 #define US(p) reinterpret_cast<unsigned short *>(p)
 #define CUS(p) reinterpret_cast<const unsigned short *>(p)
 

@@ -185,6 +185,22 @@ void launch(seg_dtype dt, const Args &g, hipStream_t st) {
 
 namespace {
 
+// rows of `width` bytes, `ld` bytes apart
+struct Rows {
+  const void *p;
+  int64_t ld, width;
+};
+
+// Whether they share a byte.  At one stride they may be parts of the same wide
+// rows: then the columns decide.
+bool meet(const Rows &a, const Rows &b, int64_t rows) {
+  const __int128 x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);  // strides up to 2^42
+  if (x >= y + (__int128)(rows - 1) * b.ld + b.width || y >= x + (__int128)(rows - 1) * a.ld + a.width) return false;
+  if (rows == 1 || a.ld != b.ld) return true;
+  const int64_t at = (int64_t)(((y - x) % a.ld + a.ld) % a.ld);
+  return at < a.width || at + b.width > a.ld;
+}
+
 seg_status rotate(int64_t rows, seg_dtype dt, const seg_mrope_cfg *cfg, int32_t hq, int32_t hkv, int32_t d,
                   const int32_t *pos, const void *q, int64_t ldq, const void *k, int64_t ldk, void *qo,
                   int64_t ldqo, void *ko, int64_t ldko, int inverse, hipStream_t stream) {
@@ -207,6 +223,14 @@ seg_status rotate(int64_t rows, seg_dtype dt, const seg_mrope_cfg *cfg, int32_t 
       SEG_CHECK(reinterpret_cast<uintptr_t>(ptr[i]) % 16 == 0 && ld[i] * e % 16 == 0, SEG_ERR_UNSUPPORTED,
                 "rows must start on 16-byte boundaries");
     }
+    Rows t[4];
+    for (int i = 0; i < 4; ++i) t[i] = Rows{ptr[i], ld[i] * e, (i & 1 ? hkv : hq) * (int64_t)d * e};
+    for (int o = 2; o < 4; ++o)
+      for (int i = 0; i < o; ++i) {
+        const bool itself = i == o - 2 && t[i].p == t[o].p && t[i].ld == t[o].ld;
+        SEG_CHECK(!t[i].width || !t[o].width || itself || !meet(t[i], t[o], rows), SEG_ERR_ARG,
+                  "an output overlaps an input that is not its own, or another output");
+      }
     mrope::Args g{};
     g.a = mrope::Heads{q, qo, ldq, ldqo, hq};
     g.b = mrope::Heads{k, ko, ldk, ldko, hkv};

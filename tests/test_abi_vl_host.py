@@ -104,6 +104,17 @@ def test_rotation_refuses(kw, want):
     assert _rope(**kw) == want
 
 
+@pytest.mark.parametrize("kw", [
+    dict(qo=1 << 20, ldqo=136), dict(qo=(1 << 20) + 16), dict(qo=(1 << 20) + 256), dict(qo=(1 << 20) - 16), dict(ko=2 << 20, ldko=72),
+    dict(ko=1 << 20), dict(qo=2 << 20), dict(qo=4 << 20), dict(ko=(3 << 20) + 3 * 256 + 240),
+    # parts of one wide row: the next one's columns, its own of another row, its last columns
+    dict(ldq=256, ldqo=256, qo=(1 << 20) + 240), dict(ldq=256, ldqo=256, qo=(1 << 20) + 512),
+    dict(ldq=256, ldqo=256, qo=(1 << 20) + 272), dict(rows=1, qo=(1 << 20) + 240)])
+def test_rotation_refuses_overlapping_tensors(kw):
+    """An output on an input that is not its own, or at another stride or offset of its own."""
+    assert _rope(**dict(dict(q=1 << 20, k=2 << 20, qo=3 << 20, ko=4 << 20), **kw)) == ARG
+
+
 def test_rotation_of_nothing():
     assert _rope(rows=0, pos=None, q=None, k=None, qo=None, ko=None) == _lib.SEG_OK
 
@@ -120,6 +131,14 @@ def test_packing_refuses(kw, want):
     p = ctypes.byref(s) if a["p"] else None
     assert L.seg_act_pack(a["rows"], a["cols"], a["dt"], a["x"], a["ldx"], p, None) == want
     assert L.seg_act_unpack(a["rows"], a["cols"], a["dt"], p, a["x"], a["ldx"], None) == want
+
+
+@pytest.mark.parametrize("x,code,exp", [(16, 16, 1 << 20), (16, 1 << 20, 16 + 510), (1 << 20, 16, 16 + 255), (256, 1, 1 << 20)])
+def test_packing_refuses_overlapping_arrays(x, code, exp):
+    L = _lib_or_skip()
+    s = _lib.SegAct8(code, exp)
+    assert L.seg_act_pack(4, 64, 0, x, 64, ctypes.byref(s), None) == ARG
+    assert L.seg_act_unpack(4, 64, 0, ctypes.byref(s), x, 64, None) == ARG
 
 
 def test_packing_of_nothing():
