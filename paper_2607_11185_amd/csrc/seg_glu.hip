@@ -7,6 +7,7 @@
 // into dg and du, and two GEMM launches give dx = dg Wg + du Wu (one sum over
 // both contractions) and both weight gradients.
 #include <algorithm>
+#include <cmath>
 
 #include "act8.h"
 #include "common.h"
@@ -198,10 +199,9 @@ struct RowsArgs {
 
 // Features of a block of the kernels for few rows: one block of the 8-bit format.
 constexpr int FEATURES = act8::BLOCK;
-constexpr int FEW = 8;      // rows that k_glu_few takes at most
+constexpr int FEW = 2;      // rows that k_glu_few takes at most
 constexpr int ROWS = 64;    // and k_glu_rows
 constexpr int PARTS = 4;    // of K, k_glu_few; each four waves
-constexpr int ROWS_WAVES = 8;
 constexpr unsigned FEW_LDS = 64u << 10;
 
 // The forward for a handful of rows (at most T), where the weights' bytes are all
@@ -212,10 +212,9 @@ constexpr unsigned FEW_LDS = 64u << 10;
 // every row of x, which lies in LDS as all waves need it.  A block takes 32 features;
 // four waves of it 8 of them each, and four such groups a quarter of K each.  The
 // eight lanes of a feature add up by exchange, the quarters in LDS, in order.
-// 3,584 x 2 x 18,944, 1 / 4 / 8 rows: 46.9 / 49.1 / 59.2 us (5.8 / 5.5 / 4.6 TB/s;
-// the GEMM takes 62); 2,048 x 2 x 5,504: 11.1 / 11.6 / 13.8 (30).  With K in halves
-// 47 / 49 / 63 and 15.5 / 15.5 / 17.2; two steps in flight more registers, so fewer
-// blocks at once: 48 / 53 / 127.
+// 3,584 x 2 x 18,944, 1 / 2 / 4 rows: 46.7 / 47.1 / 49.0 us (5.8 / 5.8 / 5.5 TB/s;
+// k_glu_rows takes 47.1 / 47.1 / 47.3); 2,048 x 2 x 5,504: 10.9 / 11.3 / 11.5 (11.7);
+// 896 x 2 x 4,864: 6.0 / 6.0 / 7.1 (6.4).  With K in halves 47 us and 15.5.
 template <int T, Keep KEEP>
 __global__ void __launch_bounds__(256 * PARTS) k_glu_few(const RowsArgs a, const EpiGlu<KEEP> ep) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -319,64 +318,83 @@ __global__ void __launch_bounds__(256 * PARTS) k_glu_few(const RowsArgs a, const
   }
 }
 
-// The forward for some tens of rows (16 NB at most): a block takes 32 features and
-// reads their rows of wg and wu from memory to registers in the layout of the
-// products' operands (16 rows x 32 k); its eight waves take every eighth step of 32 of
-// K and add up their sums in LDS, in order.  The next step's loads are under way
-// during a step's products.  Lanes past the last feature or row read the last one,
-// and their sums go nowhere; what lies past K reads as zeros on both sides.  2,048 x
-// 2 x 5,504, 16 / 32 / 64 rows: 15.9 / 17.6 / 21.6 us (the GEMM: 30); 3,584 x 2 x
-// 18,944: 71 / 82 / 103 (62 to 66, so the GEMM serves there).  Steps of 128 in four
-// waves take 74 / 113 / 372; held to six waves a SIMD 98 at 16 rows; past the
-// caches, in half lines, 82 there.
-template <int NB, Keep KEEP>
-__global__ void __launch_bounds__(64 * ROWS_WAVES) k_glu_rows(const RowsArgs a, const EpiGlu<KEEP> ep) {
-  __shared__ f32x4 sums[ROWS_WAVES][4 * NB][64];
+// The forward for some tens of rows (16 NB at most): a block takes 32 features, its
+// waves every WAVES-th step of 64 of K, and their sums are added up in LDS, in order.
+// The weights' bytes are the work, and memory gives them fastest in whole 128-byte lines
+// (k_glu_few), which are not the layout of a matrix product's operand: there a load
+// takes 64 bytes of 16 rows.  So a lane's 16 bytes, 8 rows to a load, go through the
+// wave's own 8 KB of LDS (chunk c of row r in slot c ^ (r & 7): no conflicts), first
+// those of x, then the weights', while the loads of the wave's next step are under
+// way; no wave waits for another.  Lanes past the last feature or row read the last
+// one, and their sums go nowhere; what lies past K reads as zeros.  16 / 32 / 64 rows:
+// 3,584 x 2 x 18,944 48.7 / 54.8 / 66 us (5.6 / 5.0 / 4.1 TB/s; the GEMM 62 to 66; both
+// operands from memory in their layout 71 / 82 / 103, x alone 50 / 58 / 76); 2,048 x 2 x
+// 5,504 11.5 / 13.7 / 18.0 (30).  x a step later, which saves its second set of registers,
+// takes 53 / 62 / 82; four waves for 16 rows 51 and 13.0, eight for 64 rows 83 and 18.7.
+template <int NB, int WAVES, Keep KEEP>
+__global__ void __launch_bounds__(64 * WAVES, NB < 4 ? 4 : 2) k_glu_rows(const RowsArgs a, const EpiGlu<KEEP> ep) {
+  // [wave][64 weight rows: 32 of wg, 32 of wu][8 chunks], then the waves' sums
+  constexpr int STAGE = WAVES * 64 * 8, SUMS = WAVES * 4 * NB * 64;
+  __shared__ __attribute__((aligned(1024))) f32x4 lds[STAGE > SUMS ? STAGE : SUMS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = lane & 15, grp = lane >> 4;
+  const int r = lane & 15, grp = lane >> 4, lr = lane >> 3, lc = lane & 7;
   const int f0 = blockIdx.x * FEATURES, I = ep.features, H = a.hidden;
-  const unsigned short *pw[4], *px[NB];
+  const unsigned short *wg = a.wg + (long)f0 * H, *wu = a.wu + (long)f0 * H;
+  unsigned off[4];
 #pragma unroll
-  for (int b = 0; b < 4; ++b)
-    pw[b] = (b < 2 ? a.wg : a.wu) + (long)min(f0 + 16 * (b & 1) + r, I - 1) * H + 8 * grp;
+  for (int i = 0; i < 4; ++i) off[i] = (unsigned)min(8 * i + lr, I - 1 - f0) * (unsigned)H + 8 * lc;
+  unsigned xoff[2 * NB];
 #pragma unroll
-  for (int n = 0; n < NB; ++n) px[n] = a.x + (long)min(16 * n + r, a.rows - 1) * a.ldx + 8 * grp;
-  struct Step {
-    bf16x8 w[4], x[NB];
-  };
-  auto load = [&](Step &c, int k) __attribute__((always_inline)) {
-    const bool in = k + 8 * grp < H;
+  for (int i = 0; i < 2 * NB; ++i) xoff[i] = (unsigned)min(8 * i + lr, a.rows - 1) * (unsigned)a.ldx + 8 * lc;
+  bf16x8 w[8], x[2 * NB];
+  auto load = [&](int k) __attribute__((always_inline)) {
+    const bool in = k + 8 * lc < H;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) c.w[b] = in ? *reinterpret_cast<const bf16x8 *>(pw[b] + k) : bf16x8{};
+    for (int i = 0; i < 8; ++i) {
+      const unsigned short *p = (i < 4 ? wg : wu) + k + off[i & 3];
+      w[i] = in ? __builtin_nontemporal_load(reinterpret_cast<const bf16x8 *>(p)) : bf16x8{};
+    }
 #pragma unroll
-    for (int n = 0; n < NB; ++n) c.x[n] = in ? *reinterpret_cast<const bf16x8 *>(px[n] + k) : bf16x8{};
+    for (int i = 0; i < 2 * NB; ++i) x[i] = in ? *reinterpret_cast<const bf16x8 *>(a.x + k + xoff[i]) : bf16x8{};
   };
   f32x4 acc[4][NB];
 #pragma unroll
   for (int b = 0; b < 4; ++b)
 #pragma unroll
     for (int n = 0; n < NB; ++n) acc[b][n] = f32x4{};
-  // features of block b against rows of block n: a lane holds row 16 n + lane % 16,
-  // features 4 (lane / 16) .. + 3
-  auto products = [&](const Step &c) __attribute__((always_inline)) {
+  bf16x8 *stage = reinterpret_cast<bf16x8 *>(lds) + wave * (64 * 8);
+  bf16x8 *to = stage + lr * 8 + (lc ^ lr);
+  const bf16x8 *from = stage + r * 8;
+  int k = wave * 64;
+  load(k);
+  for (; k < H; k += 64 * WAVES) {
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int i = 0; i < 2 * NB; ++i) to[64 * i] = x[i];
+    __builtin_amdgcn_wave_barrier();
+    bf16x8 cx[2][NB];
 #pragma unroll
-      for (int n = 0; n < NB; ++n) acc[b][n] = mfma16(c.w[b], c.x[n], acc[b][n]);
-  };
-  constexpr int ST = 32 * ROWS_WAVES;
-  Step c0, c1;
-  int k = wave * 32;
-  if (k < H) load(c0, k);
-  while (k < H) {
-    if (k + ST < H) load(c1, k + ST);
-    products(c0);
-    k += ST;
-    if (k >= H) break;
-    if (k + ST < H) load(c0, k + ST);
-    products(c1);
-    k += ST;
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int n = 0; n < NB; ++n) cx[h][n] = from[n * 128 + ((4 * h + grp) ^ (r & 7))];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) to[64 * i] = w[i];
+    __builtin_amdgcn_wave_barrier();
+    load(k + 64 * WAVES);
+    // features of block b against rows of block n: a lane holds row 16 n + lane % 16,
+    // features 4 (lane / 16) .. + 3
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const bf16x8 cw = from[b * 128 + ((4 * h + grp) ^ (r & 7))];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[b][n] = mfma16(cw, cx[h][n], acc[b][n]);
+      }
+    __builtin_amdgcn_wave_barrier();
   }
+  f32x4(*sums)[4 * NB][64] = reinterpret_cast<f32x4(*)[4 * NB][64]>(lds);
+  __syncthreads();
 #pragma unroll
   for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -388,9 +406,9 @@ __global__ void __launch_bounds__(64 * ROWS_WAVES) k_glu_rows(const RowsArgs a, 
 #pragma unroll
   for (int b = 0; b < 4; ++b) v[b] = sums[0][b * NB + wave][lane];
 #pragma unroll 1  // (unrolled, these reads take more registers than the products)
-  for (int w = 1; w < ROWS_WAVES; ++w)
+  for (int q = 1; q < WAVES; ++q)
 #pragma unroll
-    for (int b = 0; b < 4; ++b) v[b] += sums[w][b * NB + wave][lane];
+    for (int b = 0; b < 4; ++b) v[b] += sums[q][b * NB + wave][lane];
   int eg = 0, eu = 0;
   if constexpr (KEEP == CODES) {
     unsigned tg = 0, tu = 0;
@@ -479,23 +497,23 @@ __global__ void __launch_bounds__(256) k_glu_bwd(const glu::Kept k, const unsign
 
 unsigned few_lds(int rows, int hidden) { return (unsigned)((hidden + 63) / 64 * 128) * rows; }
 
-// Rows of x that the kernel for few rows is built for (1, 2, 4 or 8; 16, 32 or 64 for
-// k_glu_rows), or 0 where the GEMM serves: by the time that each is expected to take,
-// us, as measured (see the kernels).  A handful of rows reads the weights at the rate
-// of memory, if x fits the LDS; some tens do at 4.0, 3.5 and 2.7 TB/s and 4 us more,
-// against the GEMM's steps of 0.93 us on tiles of 128 x 256, one round where the
-// weights are as wide as the chip.
+// Rows of x that the kernel for few rows is built for (1 or 2; 16, 32 or 64 for
+// k_glu_rows), or 0 where the GEMM serves.  One or two rows go to k_glu_few if x fits its
+// LDS.  Beyond, the time of each is that of the weights' bytes, or of its steps where
+// there are few blocks, as measured: k_glu_rows 5.3, 4.9 and 4.3 TB/s, and 2.0, 2.3 and
+// 1.55 us for a wave's step of 64; the GEMM's tiles take 1.12 of what choose() expects
+// when the weights come from memory, which give 5.4 TB/s at most.  Measured, 16 / 32 / 64
+// rows, k_glu_rows / GEMM: 8,192 x 2 x 28,672 182 / 191 / 200 and 176 / 171 / 172 us;
+// 4,096 x 2 x 14,336 43 / 47 / 52 and 69; 8,192 x 2 x 4,096 36 / 41 / 53 and 45 / 46 / 47;
+// 512 x 2 x 18,944 10 / 14 / 14 and 15 / 14 / 14; 16,384 x 2 x 2,048 54 / 62 / 88 and 45.
 int few_rows(int rows, int hidden, int inter, double gemm_us) {
-  for (int t = 1; t <= FEW; t *= 2)
-    if (rows <= t) {
-      if (few_lds(t, hidden) + PARTS * 2 * t * FEATURES * 4 <= FEW_LDS) return t;
-      break;
-    }
-  const double mb = 4e-6 * hidden * inter;
-  if (rows <= 16) return 4 + mb / 4.0 < gemm_us ? 16 : 0;
-  if (rows <= 32) return 4 + mb / 3.5 < gemm_us ? 32 : 0;
-  if (rows <= ROWS) return 4 + mb / 2.7 < gemm_us ? 64 : 0;
-  return 0;
+  if (rows <= FEW && few_lds(rows, hidden) + PARTS * 2 * rows * FEATURES * 4 <= FEW_LDS) return rows;
+  if (rows > ROWS) return 0;
+  const int n = rows <= 16 ? 0 : rows <= 32 ? 1 : 2;
+  constexpr double RATE[3] = {5.3, 4.9, 4.3}, STEP[3] = {2.0, 2.3, 1.55};
+  const double mb = 4e-6 * hidden * inter, steps = (hidden + 63) / 64;
+  const double us = 4 + std::max(mb / RATE[n], STEP[n] * std::ceil(steps / (n < 2 ? 8 : 4)));
+  return us < std::max(1.12 * gemm_us, 4 + mb / 5.4) ? 16 << n : 0;
 }
 
 template <class Epi>
@@ -504,11 +522,9 @@ void launch_few(int t, const RowsArgs &a, const Epi &ep, hipStream_t st) {
   switch (t) {
     case 1: k_glu_few<1><<<nb, 256 * PARTS, lds, st>>>(a, ep); break;
     case 2: k_glu_few<2><<<nb, 256 * PARTS, lds, st>>>(a, ep); break;
-    case 4: k_glu_few<4><<<nb, 256 * PARTS, lds, st>>>(a, ep); break;
-    case 8: k_glu_few<8><<<nb, 256 * PARTS, lds, st>>>(a, ep); break;
-    case 16: k_glu_rows<1><<<nb, 64 * ROWS_WAVES, 0, st>>>(a, ep); break;
-    case 32: k_glu_rows<2><<<nb, 64 * ROWS_WAVES, 0, st>>>(a, ep); break;
-    default: k_glu_rows<4><<<nb, 64 * ROWS_WAVES, 0, st>>>(a, ep); break;
+    case 16: k_glu_rows<1, 8><<<nb, 64 * 8, 0, st>>>(a, ep); break;
+    case 32: k_glu_rows<2, 8><<<nb, 64 * 8, 0, st>>>(a, ep); break;
+    default: k_glu_rows<4, 4><<<nb, 64 * 4, 0, st>>>(a, ep); break;
   }
   SEG_LAUNCH_CHECK();
 }
