@@ -196,6 +196,23 @@ def test_extremes():
     assert torch.equal(kept2[0].code[rows], kept[0].code[rows])
 
 
+@pytest.mark.parametrize("shape", [(2, 328, 104), (5, 328, 104), (16, 1096, 40), (30, 1096, 104), (50, 328, 72), (300, 328, 104)],
+                         ids=str)
+def test_infinities_stay_in_their_row_and_feature(shape):
+    """An infinite row of x and a NaN in a weight reach that row's and that feature's values
+    only, though rows and features share loads, LDS and matrix operands."""
+    import torch
+    rows, hidden, inter = shape
+    x, wg, wu, _ = _inputs(*shape, seed=6)
+    m = S.seg_glu_fwd(x, wg, wu)[0]
+    x2, w2 = x.clone(), wu.clone()
+    x2[rows - 1, hidden - 3] = float("inf")
+    w2[inter - 2, 7] = float("nan")
+    m2 = S.seg_glu_fwd(x2, wg, w2)[0]
+    assert torch.equal(m2[:-1, :-2], m[:-1, :-2]) and torch.equal(m2[:-1, -1], m[:-1, -1])
+    assert bool(m2[:, -2].isnan().all()) and not bool(m2[-1].isfinite().all())
+
+
 @pytest.mark.parametrize("rows", [1, 22, 300])
 def test_gates_over_the_whole_range(rows):
     """g = x[:, 0] and u = 1 exactly, down to where exp(-g) leaves fp32: there the sigmoid
