@@ -488,7 +488,8 @@ seg_status seg_glu_bwd(int32_t rows, int32_t hidden, int32_t inter, const void *
  *   read back (seg_act_unpack) and lse, rstd1 and rstd2 of the forward.  With
  *   codes for g and u (both or none) the gate and up values are kept too, and
  *   the backward does not compute the two projections again.  y is the same,
- *   bit for bit, with saved8 or without.
+ *   bit for bit, with saved8 or without; with it y may be x, and dx may be dy
+ *   (the same pointers).
  */
 typedef struct {
   seg_act8 x, y1;       /* [P, H] */

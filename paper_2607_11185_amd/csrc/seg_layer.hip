@@ -524,6 +524,10 @@ void layer_fwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cf
     ProfScope prof("ly_misc", st);
     positions(L, sz, P, pos, st);
   }
+  if (ext.packed) {  // before y, which may be x, is written
+    ProfScope prof("ly_act8", st);
+    pack(P, H, x, ext.packed->x, st);
+  }
   for (long r0 = 0; r0 < P; r0 += m.C) {
     const int cr = (int)std::min<long>(m.C, P - r0);
     {
@@ -568,7 +572,6 @@ void layer_fwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cf
   if (ext.packed) {
     const seg_layer_saved8 &s8 = *ext.packed;
     ProfScope prof("ly_act8", st);
-    pack(P, H, x, s8.x, st);
     pack(P, m.QD, q, s8.q, st);
     pack(P, m.KD, k, s8.k, st);
     pack(P, m.KD, v, s8.v, st);

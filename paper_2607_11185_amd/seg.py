@@ -702,8 +702,8 @@ def _layer_args(lay, cfg, w, x):
 def seg_layer_fwd_ext(lay: Layout, cfg: LayerCfg, w: dict, x, rope: Optional[MropeCfg] = None,
                       pos=None, saved8=None, y=None, saved=None, ws=None):
     """seg_layer_fwd with positions on three axes (rope, pos [3, P] int32) and 8-bit
-    saved activations (saved8: layer_saved8's dict, filled here).  Returns (y,
-    saved8), or (y, saved) without saved8."""
+    saved activations (saved8: layer_saved8's dict, filled here; y may then be x).
+    Returns (y, saved8), or (y, saved) without saved8."""
     import torch
     P, H = x.shape
     weights = _layer_args(lay, cfg, w, x)
@@ -729,8 +729,8 @@ def seg_layer_fwd_ext(lay: Layout, cfg: LayerCfg, w: dict, x, rope: Optional[Mro
 
 def seg_layer_bwd_ext(lay: Layout, cfg: LayerCfg, w: dict, dy, rope: Optional[MropeCfg] = None,
                       pos=None, saved8=None, x=None, saved=None, dx=None, grads=None, ws=None):
-    """seg_layer_bwd with rope and pos of the forward, from saved8 alone or from x and
-    saved: returns (dx, grads) with fp32 weight gradients by name."""
+    """seg_layer_bwd with rope and pos of the forward, from saved8 alone (dx may then be
+    dy) or from x and saved: returns (dx, grads) with fp32 weight gradients by name."""
     import torch
     weights = _layer_args(lay, cfg, w, dy)
     dev, (P, H) = dy.device, dy.shape

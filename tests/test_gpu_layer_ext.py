@@ -251,3 +251,23 @@ def test_capture_and_replay_of_the_operators_together():
                 e = eager[n]
             assert torch.equal(t, e), (rep, n)
         say("replay", rep)
+
+
+@pytest.mark.parametrize("keep_gate", [False, True])
+@pytest.mark.parametrize("name", ["d128_chunked", "d64_gqa4_buffers"])
+def test_output_in_place_of_the_input(name, keep_gate):
+    """With 8-bit saved activations y may be x and dx may be dy: what is kept, both outputs and
+    all gradients are those of separate tensors, bit for bit."""
+    import torch
+    say(name, keep_gate)
+    lr = ExtRun(*CASES[name])
+    res = []
+    for inplace in (False, True):
+        x, dy, s8 = lr.x.clone(), lr.dy.clone(), S.layer_saved8(lr.lay, lr.lc, keep_gate)
+        y, _ = S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, x, lr.rope, lr.pos, saved8=s8, y=x if inplace else None)
+        dx, g = S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, dy, lr.rope, lr.pos, saved8=s8, dx=dy if inplace else None)
+        assert (y is x) == inplace and (dx is dy) == inplace
+        kept = {n + " " + f: _rows(lr.pad, getattr(s8[n], f)) for n in _lib.SAVED8 if n in s8 for f in ("code", "exp")}
+        res.append({"y": _rows(lr.pad, y), "dx": dx, **kept, **{"d" + n: t for n, t in g.items()}})
+    for n in res[0]:
+        assert torch.equal(res[0][n], res[1][n]), n
