@@ -489,7 +489,8 @@ seg_status seg_glu_bwd(int32_t rows, int32_t hidden, int32_t inter, const void *
  *   codes for g and u (both or none) the gate and up values are kept too, and
  *   the backward does not compute the two projections again.  y is the same,
  *   bit for bit, with saved8 or without; with it y may be x, and dx may be dy
- *   (the same pointers).
+ *   (the same pointers), and otherwise the outputs, what is kept and the workspace
+ *   share no memory with x, dy, pos or the weights, nor with each other (SEG_ERR_ARG).
  */
 typedef struct {
   seg_act8 x, y1;       /* [P, H] */

@@ -20,6 +20,9 @@ constexpr int NOT_FINITE = 255;
 
 inline long blocks_of(long cols) { return (cols + BLOCK - 1) / BLOCK; }
 
+// refuses what one launch of seg_act_pack or seg_act_unpack does not hold
+void check_launch(long rows, long cols, seg_dtype dt);
+
 // Magnitudes compare as their bits do, infinities and NaN above all numbers.
 __device__ __forceinline__ unsigned mag(float x) { return __builtin_bit_cast(unsigned, x) & 0x7fffffffu; }
 

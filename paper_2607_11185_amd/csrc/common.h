@@ -91,16 +91,20 @@ struct Span {
 };
 
 // what a call writes shares no byte with what it reads, nor one output with another
-inline void check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+inline void check_apart(const Span *outs, size_t n_outs, const Span *ins, size_t n_ins) {
   auto meet = [](const Span &a, const Span &b) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
     return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
   };
-  for (const Span *o = outs.begin(); o != outs.end(); ++o) {
-    for (const Span &i : ins) SEG_CHECK(!meet(*o, i), SEG_ERR_ARG, "an output or the workspace overlaps an input");
-    for (const Span *q = outs.begin(); q != o; ++q)
-      SEG_CHECK(!meet(*o, *q), SEG_ERR_ARG, "an output overlaps another or the workspace");
+  for (size_t o = 0; o < n_outs; ++o) {
+    for (size_t i = 0; i < n_ins; ++i)
+      SEG_CHECK(!meet(outs[o], ins[i]), SEG_ERR_ARG, "an output or the workspace overlaps an input");
+    for (size_t q = 0; q < o; ++q)
+      SEG_CHECK(!meet(outs[o], outs[q]), SEG_ERR_ARG, "an output overlaps another or the workspace");
   }
+}
+inline void check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  check_apart(outs.begin(), outs.size(), ins.begin(), ins.size());
 }
 
 // Carves aligned sub-buffers out of a caller workspace.

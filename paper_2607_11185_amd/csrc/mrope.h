@@ -42,6 +42,8 @@ struct Args {
 
 // sections, base, head counts and head size as seg_mrope_fwd takes them
 void check_cfg(const seg_mrope_cfg *cfg, int32_t d);
+// refuses what one launch does not hold (heads: of q and k together)
+void check_launch(seg_dtype dt, long rows, int heads, int d);
 void launch(seg_dtype dt, const Args &g, hipStream_t st);
 
 }  // namespace mrope

@@ -204,17 +204,29 @@ bool act_args(int64_t rows, int32_t cols, seg_dtype dt, const void *x, int64_t l
   return true;
 }
 
-// Launches kernel(T, U, STREAM): one chunk a lane until the chip is full, four in
-// flight beyond that, past the caches where they cannot hold the tensors.
+// chunks of a row, whole blocks of them
+long chunks_of(long cols, seg_dtype dt) {
+  return act8::blocks_of(cols) * (act8::BLOCK / (dt == SEG_BF16 ? Chunk<unsigned short>::W : Chunk<float>::W));
+}
+
+// Chunks a lane: one until the chip is full, four in flight beyond that.
+struct Grid {
+  int unroll;
+  long blocks;
+  explicit Grid(long chunks) : unroll(chunks > 2048 * 256 ? 4 : 1), blocks((chunks + 256 * unroll - 1) / (256 * unroll)) {}
+};
+
+// Launches kernel(T, U, STREAM): U chunks a lane, past the caches where they cannot
+// hold the tensors.
 template <class F>
 void act_launch(ActArgs &a, seg_dtype dt, F &&kernel) {
-  a.per_row = a.blocks * (act8::BLOCK / (dt == SEG_BF16 ? Chunk<unsigned short>::W : Chunk<float>::W));
+  act8::check_launch(a.rows, a.cols, dt);
+  a.per_row = (int)chunks_of(a.cols, dt);
   a.step_rows = 64 / a.per_row;
   a.step_chunks = 64 % a.per_row;
-  const long n = a.rows * a.per_row;
-  const int unroll = n > 2048 * 256 ? 4 : 1;
-  const long nb = (n + 256 * unroll - 1) / (256 * unroll);
-  SEG_CHECK(nb <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "tensor too large for one launch");
+  const Grid grid(a.rows * a.per_row);
+  const int unroll = grid.unroll;
+  const long nb = grid.blocks;
   check_apart({{a.code, (size_t)a.rows * a.cols}, {a.exp, (size_t)a.rows * a.blocks}},
               {{a.x, ((size_t)(a.rows - 1) * a.ldx + a.cols) * (dt == SEG_BF16 ? 2 : 4)}});
   a.narrow = nb * 256 * unroll <= 0xffffffffL;
@@ -230,6 +242,12 @@ void act_launch(ActArgs &a, seg_dtype dt, F &&kernel) {
 }
 
 }  // namespace
+
+void act8::check_launch(long rows, long cols, seg_dtype dt) {
+  SEG_CHECK(Grid(rows * chunks_of(cols, dt)).blocks <= 0x7fffffffL / 256, SEG_ERR_CAPACITY,
+            "tensor too large for one launch");
+}
+
 }  // namespace seg
 
 using namespace seg;

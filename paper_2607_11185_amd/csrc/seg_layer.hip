@@ -10,7 +10,9 @@
 // the weight's rows, a weight gradient over the chunk's rows.
 // Weight gradients are summed chunk after chunk and the norm-weight gradients
 // through fixed-order partial sums, so results are bitwise reproducible.
+#include <algorithm>
 #include <cmath>
+#include <vector>
 
 #include "act8.h"
 #include "common.h"
@@ -733,12 +735,13 @@ extern "C" size_t seg_layer_ext_workspace_bytes(const seg_sizes *sz, const seg_l
 
 namespace {
 
-Ext check_ext(const seg_layer_ext *e, const seg_layer_cfg &c) {
+Ext check_ext(const seg_layer_ext *e, const seg_sizes &sz, const seg_layer_cfg &c) {
   Ext x{};
   if (!e) return x;
   if (e->rope) {
     mrope::check_cfg(e->rope, c.d);
     SEG_CHECK(e->pos, SEG_ERR_ARG, "rope without pos");
+    mrope::check_launch(SEG_BF16, sz.packed_tokens, c.hq + c.hkv, c.d);
   }
   if (e->saved8) {
     const seg_act8 *a[] = {&e->saved8->x, &e->saved8->q, &e->saved8->k,
@@ -750,11 +753,51 @@ Ext check_ext(const seg_layer_ext *e, const seg_layer_cfg &c) {
     SEG_CHECK((reinterpret_cast<uintptr_t>(g.code) | reinterpret_cast<uintptr_t>(u.code)) % 8 == 0,
               SEG_ERR_UNSUPPORTED, "the gate's and up values' codes must start on 8-byte boundaries");
     SEG_CHECK(e->saved8->lse && e->saved8->rstd1 && e->saved8->rstd2, SEG_ERR_ARG, "a saved vector is NULL");
+    act8::check_launch(sz.packed_tokens, std::max(c.hidden, c.hq * c.d), SEG_BF16);
   }
   x.rope = e->rope;
   x.pos = e->pos;
   x.packed = e->saved8;
   return x;
+}
+
+// With 8-bit saved activations: a forward's outputs (grads NULL) or a backward's, and the
+// workspace, share no memory with its inputs or each other, but y may be x and dx may be dy
+// (in: x or dy, out: y or dx).
+void check_ext_apart(const Ext &ext, const seg_sizes &sz, const seg_layer_cfg &c, const seg_layer_weights &w,
+                     const void *in, const void *out, const seg_layer_grads *grads, const void *ws, size_t ws_bytes) {
+  if (!ext.packed) return;
+  const size_t P = sz.packed_tokens, H = c.hidden, I = c.inter, QD = (size_t)c.hq * c.d, KD = (size_t)c.hkv * c.d;
+  const seg_layer_saved8 &s = *ext.packed;
+  std::vector<Span> kept, outs{{out, P * H * 2}, {ws, ws_bytes}}, ins;
+  auto act = [&](const seg_act8 &a, size_t cols) {
+    if (!a.code) return;
+    kept.push_back({a.code, P * cols});
+    kept.push_back({a.exp, P * act8::blocks_of(cols)});
+  };
+  act(s.x, H);
+  act(s.y1, H);
+  act(s.q, QD);
+  act(s.o, QD);
+  act(s.k, KD);
+  act(s.v, KD);
+  act(s.g, I);
+  act(s.u, I);
+  kept.push_back({s.lse, c.hq * P * 4});
+  kept.push_back({s.rstd1, P * 4});
+  kept.push_back({s.rstd2, P * 4});
+  std::vector<Span> &to = grads ? ins : outs;
+  to.insert(to.end(), kept.begin(), kept.end());
+  if (in != out) ins.push_back({in, P * H * 2});
+  if (ext.rope) ins.push_back({ext.pos, 3 * P * 4});
+  const void *wp[9] = {w.g1, w.wq, w.wk, w.wv, w.wo, w.g2, w.wg, w.wu, w.wd};
+  const size_t n[9] = {H, QD * H, KD * H, KD * H, H * QD, H, I * H, I * H, H * I};
+  for (int i = 0; i < 9; ++i) ins.push_back({wp[i], n[i] * 2});
+  if (grads) {
+    const void *gp[9] = {grads->g1, grads->wq, grads->wk, grads->wv, grads->wo, grads->g2, grads->wg, grads->wu, grads->wd};
+    for (int i = 0; i < 9; ++i) outs.push_back({gp[i], n[i] * 4});
+  }
+  check_apart(outs.data(), outs.size(), ins.data(), ins.size());
 }
 
 // bf16 saved activations as the caller's struct says, or those of the workspace with
@@ -780,12 +823,13 @@ extern "C" seg_status seg_layer_fwd_ext(const seg_layout *L, const seg_sizes *sz
                                         hipStream_t stream) {
   return guarded([&] {
     check_layer(L, sz, cfg, w);
-    const Ext e = check_ext(ext, *cfg);
+    const Ext e = check_ext(ext, *sz, *cfg);
     const LayerWs W = layer_ws(*sz, *cfg, 0, e.packed != nullptr);
     SEG_CHECK(ws_bytes >= W.total, SEG_ERR_WORKSPACE, "workspace of %zu bytes < required %zu",
               ws_bytes, W.total);
     if (sz->packed_tokens == 0) return;
     SEG_CHECK(x && y && ws, SEG_ERR_ARG, "x, y or ws is NULL");
+    check_ext_apart(e, *sz, *cfg, *w, x, y, nullptr, ws, W.total);
     char *base = static_cast<char *>(ws);
     layer_fwd_impl(L, sz, *cfg, e, *w, CUS(x), US(y), saved_of(e, saved, base, W), base, W, ws_bytes,
                    stream);
@@ -807,7 +851,7 @@ extern "C" seg_status seg_layer_bwd_ext(const seg_layout *L, const seg_sizes *sz
                                         hipStream_t stream) {
   return guarded([&] {
     check_layer(L, sz, cfg, w);
-    const Ext e = check_ext(ext, *cfg);
+    const Ext e = check_ext(ext, *sz, *cfg);
     const LayerWs W = layer_ws(*sz, *cfg, 1, e.packed != nullptr);
     SEG_CHECK(ws_bytes >= W.total, SEG_ERR_WORKSPACE, "workspace of %zu bytes < required %zu",
               ws_bytes, W.total);
@@ -818,6 +862,7 @@ extern "C" seg_status seg_layer_bwd_ext(const seg_layout *L, const seg_sizes *sz
       return;
     }
     SEG_CHECK((x || e.packed) && dy && dx && ws, SEG_ERR_ARG, "x, dy, dx or ws is NULL");
+    check_ext_apart(e, *sz, *cfg, *w, dy, dx, g, ws, W.total);
     char *base = static_cast<char *>(ws);
     const unsigned short *xs = e.packed ? CUS(base + W.x) : CUS(x);
     layer_bwd_impl(L, sz, *cfg, e, *w, xs, saved_of(e, saved, base, W), CUS(dy), US(dx), *g, base, W,

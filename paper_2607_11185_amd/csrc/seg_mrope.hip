@@ -163,19 +163,36 @@ void check_cfg(const seg_mrope_cfg *cfg, int32_t d) {
   SEG_CHECK(std::isfinite(cfg->base) && cfg->base > 1.f, SEG_ERR_ARG, "the rotary base must be > 1");
 }
 
-void launch(seg_dtype dt, const Args &g, hipStream_t st) {
-  if (g.rows == 0) return;
-  const int half = g.d / 2;
-  const int chunks = (g.a.heads + g.b.heads) * half / (dt == SEG_BF16 ? Piece<unsigned short>::W : Piece<float>::W);
+namespace {
+
+// rows of a block, d/2 rounded up to a power of two, blocks
+struct Grid {
+  int rows_per, half_pow;
+  long blocks;
+};
+
+Grid grid_of(seg_dtype dt, long rows, int heads, int d) {
+  const int half = d / 2, chunks = heads * half / (dt == SEG_BF16 ? Piece<unsigned short>::W : Piece<float>::W);
   int hp = 8;
   while (hp < half) hp *= 2;
   const int want = (ITEMS * 256 + chunks - 1) / chunks;
   const int rows_per = std::max(1, std::min(std::min(want, MAX_ROWS), CS / hp));
-  const long nb = (g.rows + rows_per - 1) / rows_per;
-  SEG_CHECK(nb <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "too many rows for one launch");
+  return Grid{rows_per, hp, (rows + rows_per - 1) / rows_per};
+}
+
+}  // namespace
+
+void check_launch(seg_dtype dt, long rows, int heads, int d) {
+  SEG_CHECK(grid_of(dt, rows, heads, d).blocks <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "too many rows for one launch");
+}
+
+void launch(seg_dtype dt, const Args &g, hipStream_t st) {
+  if (g.rows == 0) return;
+  check_launch(dt, g.rows, g.a.heads + g.b.heads, g.d);
+  const Grid grid = grid_of(dt, g.rows, g.a.heads + g.b.heads, g.d);
   const long bytes = g.rows * (g.a.heads + g.b.heads) * g.d * (dt == SEG_BF16 ? 2 : 4) * 2;
   const bool stream = bytes > STREAM_BYTES;
-  auto go = [&](auto kernel) { kernel<<<(unsigned)nb, 256, 0, st>>>(g, rows_per, hp); };
+  auto go = [&](auto kernel) { kernel<<<(unsigned)grid.blocks, 256, 0, st>>>(g, grid.rows_per, grid.half_pow); };
   if (dt == SEG_BF16) go(stream ? k_mrope<unsigned short, true> : k_mrope<unsigned short, false>);
   else go(stream ? k_mrope<float, true> : k_mrope<float, false>);
   SEG_LAUNCH_CHECK();

@@ -280,3 +280,52 @@ def test_layer_binding_refuses():
         with pytest.raises(AssertionError):
             S._layer_ext(lay, cfg, rope, p, saved)
     assert any(t is lay.tok_meta for t in S._layer_ext(lay, cfg, None, None, None)[1])
+
+
+def test_extended_layer_refuses_overlapping_tensors():
+    """With 8-bit saved activations an output, what is kept or the workspace on an input or on
+    another of them is refused before any launch; y over x by an offset among them."""
+    L = _lib_or_skip()
+    sz = S.seg_layout_query(_prob())
+    lay = _lib.SegLayout()
+    lay.tile, lay.window = 128, 2
+    H, I, hq, hkv, d, P = 256, 512, 4, 2, 64, sz.packed_tokens
+    cfg = S.LayerCfg(H, I, hq, hkv, d).c()
+    QD, KD = hq * d, hkv * d
+    cols = {"x": H, "y1": H, "q": QD, "o": QD, "k": KD, "v": KD, "g": I, "u": I}
+    kept = {f"{n}.{f}": P * (c if f == "code" else -(-c // 32)) for n, c in cols.items() for f in ("code", "exp")}
+    kept.update(lse=hq * P * 4, rstd1=P * 4, rstd2=P * 4)
+    weights = dict(zip(_lib.LAYER_WEIGHTS, (H, QD * H, KD * H, KD * H, H * QD, H, I * H, I * H, H * I)))
+    acts = {"x": P * H * 2, "y": P * H * 2, "pos": 12 * P}
+    size = {**kept, **{"w " + n: 2 * c for n, c in weights.items()}, **{"d " + n: 4 * c for n, c in weights.items()}, **acts}
+    ws = [L.seg_layer_ext_workspace_bytes(ctypes.byref(sz), ctypes.byref(cfg), 1, b) for b in (0, 1)]
+    at = {n: (i + 1) << 26 for i, n in enumerate(size)}
+    at["ws"] = (len(at) + 1) << 26
+
+    def call(bwd, p):
+        e, s = _lib.SegLayerExt(), _lib.SegLayerSaved8()
+        for n in cols:
+            setattr(s, n, _lib.SegAct8(p[n + ".code"], p[n + ".exp"]))
+        s.lse, s.rstd1, s.rstd2 = p["lse"], p["rstd1"], p["rstd2"]
+        e.rope = ctypes.pointer(_lib.SegMropeCfg((ctypes.c_int32 * 3)(8, 12, 12), 1e4))
+        e.pos, e.saved8 = p["pos"], ctypes.pointer(s)
+        w = _lib.SegLayerWeights(*[p["w " + n] for n in _lib.LAYER_WEIGHTS])
+        g = _lib.SegLayerGrads(*[p["d " + n] for n in _lib.LAYER_WEIGHTS])
+        head = (ctypes.byref(lay), ctypes.byref(sz), ctypes.byref(cfg), ctypes.byref(e), ctypes.byref(w))
+        if bwd:
+            return L.seg_layer_bwd_ext(*head, None, None, p["x"], p["y"], ctypes.byref(g), p["ws"], ws[1], None)
+        return L.seg_layer_fwd_ext(*head, p["x"], p["y"], None, p["ws"], ws[0], None)
+    ins = [n for n in at if n.startswith("w ")] + ["x", "pos"]
+    for bwd in (0, 1):
+        size["ws"] = ws[bwd]
+        outs = ["y", "ws", *([n for n in at if n.startswith("d ")] if bwd else kept)]
+        others = ins + outs + (list(kept) if bwd else [])
+        for a in outs:
+            for b in others:
+                if a == b or {a, b} == {"x", "y"}:
+                    continue
+                assert call(bwd, dict(at, **{a: at[b]})) == ARG, (bwd, a, b)
+                assert call(bwd, dict(at, **{a: at[b] + size[b] - 1 if size[b] < 64 else at[b] + (size[b] - 1) // 16 * 16})) in (
+                    (ARG, UNS) if a in ("g.code", "u.code") else (ARG,)), (bwd, a, b)
+        for by in (16, H * 2, P * H * 2 - 16):
+            assert call(bwd, dict(at, y=at["x"] + by)) == ARG and call(bwd, dict(at, y=at["x"] - by)) == ARG
