@@ -737,6 +737,7 @@ def seg_layer_bwd_ext(lay: Layout, cfg: LayerCfg, w: dict, dy, rope: Optional[Mr
     e, tensors = _layer_ext(lay, cfg, rope, pos, saved8)
     sv = None
     if saved8 is None:
+        assert x is not None and saved is not None, "the backward needs saved8, or x and saved"
         assert x.shape == dy.shape and x.dtype == dy.dtype and x.is_contiguous()
         saved, c = _layer_saved(saved, cfg, P, H, dev)
         sv = ctypes.byref(c)

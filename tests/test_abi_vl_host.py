@@ -329,3 +329,20 @@ def test_extended_layer_refuses_overlapping_tensors():
                     (ARG, UNS) if a in ("g.code", "u.code") else (ARG,)), (bwd, a, b)
         for by in (16, H * 2, P * H * 2 - 16):
             assert call(bwd, dict(at, y=at["x"] + by)) == ARG and call(bwd, dict(at, y=at["x"] - by)) == ARG
+
+
+def test_layer_backward_needs_what_the_forward_saved():
+    """Without saved8 and without `saved` the binding allocates nothing to read from."""
+    import torch
+    _lib_or_skip()
+    sz = S.seg_layout_query(_prob())
+    lay, cfg = S.Layout(sz, torch.device("cpu")), S.LayerCfg(256, 512, 4, 2, 64)
+    bf = dict(dtype=torch.bfloat16)
+    shapes = dict(zip(_lib.LAYER_WEIGHTS, ((256,), (256, 256), (128, 256), (128, 256), (256, 256), (256,), (512, 256), (512, 256),
+                                           (256, 512))))
+    w = {n: torch.zeros(s, **bf) for n, s in shapes.items()}
+    x = torch.zeros(sz.packed_tokens, 256, **bf)
+    saved, _ = S._layer_saved(None, cfg, sz.packed_tokens, 256, x.device)
+    for kw in (dict(x=x), dict(saved=saved), dict()):
+        with pytest.raises(AssertionError, match="saved"):
+            S.seg_layer_bwd_ext(lay, cfg, w, x, **kw)
