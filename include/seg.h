@@ -397,7 +397,7 @@ typedef struct {
  * in fp64; fp32 tensors are rotated in fp32.  ldq, ldk, ldqo, ldko: elements
  * between rows (at least heads * d), so q and k may be parts of one
  * projection's rows; an output may be its input (same pointer and stride), and
- * must not overlap an input otherwise (SEG_ERR_ARG).  Rows with a negative position on any
+ * must not overlap an input otherwise, pos among them (SEG_ERR_ARG).  Rows with a negative position on any
  * axis are padding: seg_mrope_fwd copies them, and seg_mrope_bwd, which turns
  * dq and dk back (the transpose: gradients of the unrotated q and k), writes
  * zeros there.  Supported: d a multiple of 16 up to 256, rows on 16-byte

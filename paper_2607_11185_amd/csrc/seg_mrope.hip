@@ -218,6 +218,13 @@ bool meet(const Rows &a, const Rows &b, int64_t rows) {
   return at < a.width || at + b.width > a.ld;
 }
 
+// Whether rows share a byte with the n bytes from p on.
+bool meet(const Rows &a, int64_t rows, const void *p, int64_t n) {
+  const __int128 x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(p);
+  const __int128 r = y < x + a.width ? 0 : (y - x - a.width) / a.ld + 1;  // the first row that ends behind p
+  return r < rows && x + r * a.ld < y + n;
+}
+
 seg_status rotate(int64_t rows, seg_dtype dt, const seg_mrope_cfg *cfg, int32_t hq, int32_t hkv, int32_t d,
                   const int32_t *pos, const void *q, int64_t ldq, const void *k, int64_t ldk, void *qo,
                   int64_t ldqo, void *ko, int64_t ldko, int inverse, hipStream_t stream) {
@@ -242,12 +249,14 @@ seg_status rotate(int64_t rows, seg_dtype dt, const seg_mrope_cfg *cfg, int32_t 
     }
     Rows t[4];
     for (int i = 0; i < 4; ++i) t[i] = Rows{ptr[i], ld[i] * e, (i & 1 ? hkv : hq) * (int64_t)d * e};
-    for (int o = 2; o < 4; ++o)
+    for (int o = 2; o < 4; ++o) {
+      SEG_CHECK(!t[o].width || !meet(t[o], rows, pos, 12 * rows), SEG_ERR_ARG, "an output overlaps pos");
       for (int i = 0; i < o; ++i) {
         const bool itself = i == o - 2 && t[i].p == t[o].p && t[i].ld == t[o].ld;
         SEG_CHECK(!t[i].width || !t[o].width || itself || !meet(t[i], t[o], rows), SEG_ERR_ARG,
                   "an output overlaps an input that is not its own, or another output");
       }
+    }
     mrope::Args g{};
     g.a = mrope::Heads{q, qo, ldq, ldqo, hq};
     g.b = mrope::Heads{k, ko, ldk, ldko, hkv};

@@ -346,3 +346,15 @@ def test_layer_backward_needs_what_the_forward_saved():
     for kw in (dict(x=x), dict(saved=saved), dict()):
         with pytest.raises(AssertionError, match="saved"):
             S.seg_layer_bwd_ext(lay, cfg, w, x, **kw)
+
+
+@pytest.mark.parametrize("row", [0, 1, 3])
+@pytest.mark.parametrize("out,width", [("qo", 256), ("ko", 128)])
+def test_rotation_refuses_outputs_on_the_positions(out, width, row):
+    """4 rows of `width` bytes, 512 bytes apart, and 48 bytes of positions that reach into a row's
+    first or last byte or lie inside it."""
+    base = 3 << 20
+    kw = dict(q=1 << 20, k=2 << 20, qo=4 << 20, ko=5 << 20, ldqo=256, ldko=256)
+    for at in (-47, -1, 0, 16, width - 1):
+        assert _rope(**dict(kw, **{out: base, "pos": base + 512 * row + at})) == ARG
+        assert b"pos" in _lib.lib().seg_last_error()

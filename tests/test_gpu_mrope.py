@@ -207,3 +207,18 @@ def test_rotation_refuses_unaligned_rows_before_any_launch():
     assert e.value.status == _lib.SEG_ERR_UNSUPPORTED
     with pytest.raises(AssertionError):
         S.seg_mrope_fwd(x.cpu(), None, pos, S.MropeCfg((32, 0, 0)))
+
+
+def test_rotation_with_positions_between_the_rows():
+    """Positions that lie in the gap behind an output's first or last row share nothing with it."""
+    import torch
+    q = torch.randn(4, 2, 64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(8))
+    pos = torch.randint(0, 1000, (3, 4), device="cuda", dtype=torch.int32, generator=torch.Generator(device="cuda").manual_seed(9))
+    cfg = S.MropeCfg((8, 12, 12))
+    want = S.seg_mrope_fwd(q, None, pos, cfg)[0]
+    for row in (0, 3):
+        buf = torch.zeros(4, 256, device="cuda")
+        here = buf[row, 128:140].view(torch.int32).view(3, 4)
+        here.copy_(pos)
+        got = S.seg_mrope_fwd(q, None, here, cfg, buf[:, :128].view(4, 2, 64))[0]
+        assert torch.equal(got, want) and torch.equal(here, pos)
