@@ -376,7 +376,7 @@ seg_status seg_layer_bwd(const seg_layout *L, const seg_sizes *sz, const seg_lay
  * The run table is computed on the host and uploaded to `ws` (at least
  * seg_mrope_positions_workspace_bytes(p, sz) bytes); the call waits on `stream`
  * once after that small upload, as seg_build_layout does.  Errors: SEG_ERR_ARG
- * (invalid problem, or a grid that is not its screenshot's tokens),
+ * (invalid problem, a grid that is not its screenshot's tokens, or pos on ws),
  * SEG_ERR_CAPACITY (a position past 2^31 - 1), SEG_ERR_WORKSPACE.
  */
 size_t seg_mrope_positions_workspace_bytes(const seg_problem *p, const seg_sizes *sz);

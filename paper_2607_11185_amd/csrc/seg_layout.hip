@@ -724,6 +724,7 @@ extern "C" seg_status seg_mrope_positions(const seg_problem *p, const seg_sizes 
     SEG_CHECK(pos && ws, SEG_ERR_ARG, "pos or ws is NULL");
     SEG_CHECK(reinterpret_cast<uintptr_t>(ws) % 16 == 0, SEG_ERR_UNSUPPORTED,
               "ws does not start on a 16-byte boundary");
+    check_apart({{pos, (size_t)P * 12}, {ws, w.total}}, {});
     const int blocks = (int)((P + (int64_t)POS_BLOCK - 1) / POS_BLOCK);
     std::vector<char> tab(w.total);
     std::memcpy(tab.data() + w.run, runs.data(), runs.size() * sizeof(PosRun));

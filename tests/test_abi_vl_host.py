@@ -358,3 +358,8 @@ def test_rotation_refuses_outputs_on_the_positions(out, width, row):
     for at in (-47, -1, 0, 16, width - 1):
         assert _rope(**dict(kw, **{out: base, "pos": base + 512 * row + at})) == ARG
         assert b"pos" in _lib.lib().seg_last_error()
+
+
+def test_positions_refuse_their_workspace():
+    for pos, ws in ((1 << 20, 1 << 20), ((1 << 20) + 16, 1 << 20), (1 << 20, (1 << 20) + 16)):
+        assert _positions(_prob(), GOOD, pos=pos, ws=ws) == ARG
