@@ -23,14 +23,27 @@ using gemm::ST;
 constexpr int MAX_DIM = 1 << 20;  // GEMM rows are addressed with 32-bit offsets
 constexpr long MAX_SUMS = 64L << 20;  // fp32 partial sums of a launch at most (256 MB)
 
-// 1 / (1 + exp(-g)): the reciprocal and one step towards 1 / x, which has the bits of
-// the division 1.f / x at every float x in [1, 2^126) (all tried); the fixup makes inf
-// 0 and keeps NaN.  Past 2^126 (g < -87.3) the result is 0, off by less than 2^-126.
-// Half the instructions of the division: 1555 -> 1531 us for the gate and up product
-// of 8192 x 3584 x 18944, 66.9 -> 65.1 us for 1500 x 2048 x 5504.
-__device__ __forceinline__ float sigmoidf_(float g) {
-  const float x = 1.f + __expf(-g), r = __builtin_amdgcn_rcpf(x);
-  return __builtin_amdgcn_div_fixupf(fmaf(fmaf(-x, r, 1.f), r, r), x, 1.f);
+// s = 1 / (1 + exp(-g)): the reciprocal and one step towards 1 / x, which has the bits of
+// the division 1.f / x at every float x in [1, 2^126) (found on this card by trying them
+// all, which no test repeats); the fixup makes inf 0 and keeps NaN.  Beyond (g < -87.3) 1 / x
+// is a subnormal number, which the reciprocal does not give: there, for all N together as
+// it is rare, the division itself.  Against divisions throughout: 8192 x 3584 x 2 x 18944 with
+// kept values read back 1779 -> 1760 us, 1500 x 2048 x 2 x 5504 82.4 -> 81.1 (without the rare
+// branch, and zeros beyond, 1757 and 81.1).
+template <int N>
+__device__ __forceinline__ void sigmoids(const float (&g)[N], float (&s)[N]) {
+  float x[N], top = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    x[j] = 1.f + __expf(-g[j]);
+    top = fmaxf(top, x[j]);
+    const float r = __builtin_amdgcn_rcpf(x[j]);
+    s[j] = __builtin_amdgcn_div_fixupf(fmaf(fmaf(-x[j], r, 1.f), r, r), x[j], 1.f);
+  }
+  if (top >= 0x1p126f) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) s[j] = 1.f / x[j];
+  }
 }
 
 enum Keep { NONE, BF16, CODES };
@@ -88,9 +101,11 @@ struct EpiGlu {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const f32x4 gv = g[j], uv = u[j];
-          float mv[4];
+          const float ga[4] = {gv[0], gv[1], gv[2], gv[3]};
+          float sg[4], mv[4];
+          sigmoids(ga, sg);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) mv[r] = gv[r] * sigmoidf_(gv[r]) * uv[r];
+          for (int r = 0; r < 4; ++r) mv[r] = gv[r] * sg[r] * uv[r];
           const int at = (i * 16 + t.col) * 8 + ((j * 4 + t.grp) ^ (t.col & 6));
           w[at] = gemm::u32x2{gemm::pack2(mv[0], mv[1]), gemm::pack2(mv[2], mv[3])};
           if constexpr (KEEP == BF16) {
@@ -161,8 +176,10 @@ __global__ void __launch_bounds__(256) k_finish_glu(const gemm::RestTiles<1> t, 
   if (!in) return;
   const long off = (long)row * I + f;
   u16x8 m;
+  float sg[8];
+  sigmoids(g, sg);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) m[j] = f2bf_bits(g[j] * sigmoidf_(g[j]) * u[j]);
+  for (int j = 0; j < 8; ++j) m[j] = f2bf_bits(g[j] * sg[j] * u[j]);
   *reinterpret_cast<u16x8 *>(ep.m + off) = m;
   if constexpr (KEEP == BF16) {
     u16x8 a, b;
@@ -311,7 +328,10 @@ __global__ void __launch_bounds__(256 * PARTS) k_glu_few(const RowsArgs a, const
     }
   }
   if (!in) return;
-  ep.m[off] = f2bf_bits(gv * sigmoidf_(gv) * uv);
+  const float ga[1] = {gv};
+  float sg[1];
+  sigmoids(ga, sg);
+  ep.m[off] = f2bf_bits(gv * sg[0] * uv);
   if constexpr (KEEP == BF16) {
     ep.k.g16[off] = f2bf_bits(gv);
     ep.k.u16[off] = f2bf_bits(uv);
@@ -433,9 +453,11 @@ __global__ void __launch_bounds__(64 * WAVES, NB < 4 ? 4 : 2) k_glu_rows(const R
     const int f = f0 + 16 * b + 4 * grp;
     if (f >= I) continue;
     const f32x4 g = v[b], u = v[2 + b];
-    float m[4];
+    const float ga[4] = {g[0], g[1], g[2], g[3]};
+    float sg[4], m[4];
+    sigmoids(ga, sg);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) m[j] = g[j] * sigmoidf_(g[j]) * u[j];
+    for (int j = 0; j < 4; ++j) m[j] = g[j] * sg[j] * u[j];
     const long off = (long)row * I + f;
     *reinterpret_cast<gemm::u32x2 *>(ep.m + off) = gemm::u32x2{gemm::pack2(m[0], m[1]), gemm::pack2(m[2], m[3])};
     if constexpr (KEEP == BF16) {
@@ -482,9 +504,11 @@ __global__ void __launch_bounds__(256) k_glu_bwd(const glu::Kept k, const unsign
     }
     const u16x8 mv = *reinterpret_cast<const u16x8 *>(dm + c * 8);
     u16x8 og, ou, om;
+    float sg[8];
+    sigmoids(g, sg);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float d = bf_bits2f(mv[j]), s = sigmoidf_(g[j]);
+      const float d = bf_bits2f(mv[j]), s = sg[j];
       og[j] = f2bf_bits(d * u[j] * s * (1.f + g[j] * (1.f - s)));
       ou[j] = f2bf_bits(d * g[j] * s);
       om[j] = f2bf_bits(g[j] * s * u[j]);

@@ -287,3 +287,35 @@ def test_nothing_is_written_past_the_end(shape):
             ends += [end, *(t[1] for t in out.values())]
     for i, e in enumerate(ends):
         assert bool((e == 77).all()), i
+
+
+@pytest.mark.parametrize("rows,hidden,inter", [(1, 64, 40), (22, 64, 64), (300, 64, 64), (70, 1040, 8)],
+                         ids=["few", "rows", "product", "product in parts"])
+def test_sigmoid_where_it_is_subnormal(rows, hidden, inter):
+    """Gates of -87.4 to -88.5: the sigmoid is a subnormal number there (a step of 2^-149), and
+    times g an ordinary one.  g = -(88 + t) exactly, u = 1; the exponential is off by the
+    rounding of its argument and a few more (|g| + 8) 2^-23."""
+    import torch
+    t = (torch.arange(rows) * 37 % 72 - 38) / 64.0       # -38/64 .. 33/64
+    if rows == 1:
+        t[0] = 0.25
+    x = torch.zeros(rows, hidden)
+    x[:, 0], x[:, 1], x[:, 2] = -88, 1, -t
+    wg, wu = torch.zeros(2, inter, hidden)
+    wg[:, 0] = wg[:, 2] = wu[:, 1] = 1
+    x, wg, wu = (v.to(torch.bfloat16).cuda() for v in (x, wg, wu))
+    m, kept = S.seg_glu_fwd(x, wg, wu, keep=True)
+    g = -88 - t.double().numpy()
+    ref = g * OG.sigmoid(g)
+    tol = np.abs(ref) * ((np.abs(g) + 8) * 2.0 ** -23 + 2.0 ** -8) * 1.01 + np.abs(g) * 2.0 ** -149 + 2.0 ** -133
+    assert np.abs(ref).min() > 2 * tol.max()             # zeros would not pass
+    _within(_np(m), ref[:, None], tol[:, None], "m")
+    # backward: the kept g has steps of one, half a step off -88.52 .. -87.40: -87, -88 or -89
+    assert bool((S.seg_act_unpack(kept[0], torch.float32)[:, 0] + 88).abs().max() <= 1)
+    out = S.seg_glu_bwd(x, wg, wu, torch.ones_like(m), kept)
+    g = _np(S.seg_act_unpack(kept[0], torch.float32))[:, 0]
+    ok = g == -88
+    ref = (g * OG.sigmoid(g))[ok]
+    tol = np.abs(ref) * ((np.abs(g[ok]) + 8) * 2.0 ** -23 + 2.0 ** -8) * 1.01 + np.abs(g[ok]) * 2.0 ** -149 + 2.0 ** -133
+    assert ok.any()
+    _within(_np(out["m"])[ok], ref[:, None], tol[:, None], "m of the backward")
