@@ -10,7 +10,9 @@
 // for four: 383, 401), and keeps those in LDS.  An angle of a
 // far position needs more than fp32 (at position 10^6 its last place is 1/16
 // of a radian), so the turns are formed and reduced in fp64 and only the part
-// of a turn that is left goes to fp32.
+// of a turn that is left goes to fp32.  That rounding moves an angle by up to 9.4e-8: next
+// to nothing where results round to bf16, but more than the rest of an fp32 rotation, which
+// turns by the remainder too (to first order: its square is below 10^-14).
 #include <cmath>
 
 #include "mrope.h"
@@ -102,9 +104,15 @@ __global__ void __launch_bounds__(256, STREAM ? 1 : 5) k_mrope(const mrope::Args
       const int axis = i < g.s0 ? 0 : i < g.s01 ? 1 : 2;
       // turns = pos base^(-2i/d) / (2 pi)
       const double f = exp2(-(double)(2 * i) / g.d * g.log2_base) * 0.15915494309189535;
-      const double t = (double)g.pos[axis * g.rows + row] * f;
+      const double t = (double)g.pos[axis * g.rows + row] * f, left = t - rint(t);
+      const float turn = (float)left;
       float s, c;
-      sincospif(2.f * (float)(t - rint(t)), &s, &c);
+      sincospif(2.f * turn, &s, &c);
+      if constexpr (sizeof(T) == 4) {  // and by what that rounding left out
+        const float rest = (float)(left - turn) * 6.2831855f, c0 = c;
+        c = fmaf(-rest, s, c);
+        s = fmaf(rest, c0, s);
+      }
       cs[r * half + i] = make_float2(c, g.inverse ? -s : s);
     }
   }

@@ -222,3 +222,22 @@ def test_rotation_with_positions_between_the_rows():
         here.copy_(pos)
         got = S.seg_mrope_fwd(q, None, here, cfg, buf[:, :128].view(4, 2, 64))[0]
         assert torch.equal(got, want) and torch.equal(here, pos)
+
+
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rotation_near_a_quarter_turn(inverse):
+    """Angles whose cosine or sine is close to zero, fp32: x = (1, 0) turns to (cos, sin), each
+    good relative to itself: 2 ulp of the sine and cosine and one rounding (2.5 ulp), besides the
+    fp64 angle (160 turns, 14 bits of exponent: 3e-12 of a radian, 1e-11 with room)."""
+    import torch
+    rows, d, base = 1001, 64, 1e4
+    pos = np.arange(rows)
+    x = torch.zeros(rows, 1, d, device="cuda")
+    x[..., :d // 2] = 1
+    p = torch.from_numpy(np.stack([pos] * 3).astype(np.int32)).cuda()
+    f = S.seg_mrope_bwd if inverse else S.seg_mrope_fwd
+    got = f(x, None, p, S.MropeCfg((d // 2, 0, 0), base))[0][:, 0].double().cpu().numpy()
+    ref = OM.rotate(x.double().cpu().numpy(), np.stack([pos] * 3), (d // 2, 0, 0), base, inverse)[:, 0]
+    assert (np.abs(ref[pos > 0]) < 1e-3).sum() > 20
+    over = np.abs(got - ref) - 2.5 * 2.0 ** -23 * np.abs(ref) - 1e-11
+    assert over.max() <= 0, (float(over.max()), int((over > 0).sum()))
