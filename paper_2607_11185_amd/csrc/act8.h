@@ -22,6 +22,11 @@ inline long blocks_of(long cols) { return (cols + BLOCK - 1) / BLOCK; }
 
 // refuses what one launch of seg_act_pack or seg_act_unpack does not hold
 void check_launch(long rows, long cols, seg_dtype dt);
+// seg_act_pack and seg_act_unpack, timed under `name` (NULL: not)
+void pack(int64_t rows, int32_t cols, seg_dtype dt, const void *x, int64_t ldx, const seg_act8 *out,
+          const char *name, hipStream_t st);
+void unpack(int64_t rows, int32_t cols, seg_dtype dt, const seg_act8 *in, void *x, int64_t ldx,
+            const char *name, hipStream_t st);
 
 // Magnitudes compare as their bits do, infinities and NaN above all numbers.
 __device__ __forceinline__ unsigned mag(float x) { return __builtin_bit_cast(unsigned, x) & 0x7fffffffu; }

@@ -60,7 +60,7 @@ inline seg_status guarded(F &&body) {
 }
 
 // Brackets one kernel launch with HIP events when timing is enabled
-// (seg_profile_enable); a no-op otherwise.
+// (seg_profile_enable); a no-op otherwise, and with name NULL.
 class ProfScope {
  public:
   ProfScope(const char *name, hipStream_t s);

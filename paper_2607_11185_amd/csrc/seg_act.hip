@@ -219,7 +219,7 @@ struct Grid {
 // Launches kernel(T, U, STREAM): U chunks a lane, past the caches where they cannot
 // hold the tensors.
 template <class F>
-void act_launch(ActArgs &a, seg_dtype dt, F &&kernel) {
+void act_launch(ActArgs &a, seg_dtype dt, const char *name, hipStream_t st, F &&kernel) {
   act8::check_launch(a.rows, a.cols, dt);
   a.per_row = (int)chunks_of(a.cols, dt);
   a.step_rows = 64 / a.per_row;
@@ -231,6 +231,7 @@ void act_launch(ActArgs &a, seg_dtype dt, F &&kernel) {
               {{a.x, ((size_t)(a.rows - 1) * a.ldx + a.cols) * (dt == SEG_BF16 ? 2 : 4)}});
   a.narrow = nb * 256 * unroll <= 0xffffffffL;
   const double bytes = (double)a.rows * a.cols * (dt == SEG_BF16 ? 3 : 5);
+  ProfScope prof(name, st);
   auto go = [&](auto t) {
     if (unroll == 1) kernel((unsigned)nb, t, std::integral_constant<int, 1>(), std::false_type());
     else if (bytes <= STREAM_BYTES) kernel((unsigned)nb, t, std::integral_constant<int, 4>(), std::false_type());
@@ -248,30 +249,34 @@ void act8::check_launch(long rows, long cols, seg_dtype dt) {
             "tensor too large for one launch");
 }
 
+void act8::pack(int64_t rows, int32_t cols, seg_dtype dt, const void *x, int64_t ldx, const seg_act8 *out,
+                const char *name, hipStream_t st) {
+  ActArgs a{};
+  if (!act_args(rows, cols, dt, x, ldx, out, a)) return;
+  act_launch(a, dt, name, st, [&](unsigned nb, auto t, auto u, auto past) {
+    k_pack<decltype(t), decltype(u)::value, decltype(past)::value><<<nb, 256, 0, st>>>(a);
+  });
+}
+
+void act8::unpack(int64_t rows, int32_t cols, seg_dtype dt, const seg_act8 *in, void *x, int64_t ldx,
+                  const char *name, hipStream_t st) {
+  ActArgs a{};
+  if (!act_args(rows, cols, dt, x, ldx, in, a)) return;
+  act_launch(a, dt, name, st, [&](unsigned nb, auto t, auto u, auto past) {
+    k_unpack<decltype(t), decltype(u)::value, decltype(past)::value><<<nb, 256, 0, st>>>(a);
+  });
+}
+
 }  // namespace seg
 
 using namespace seg;
 
 extern "C" seg_status seg_act_pack(int64_t rows, int32_t cols, seg_dtype dt, const void *x,
                                    int64_t ldx, const seg_act8 *out, hipStream_t stream) {
-  return guarded([&] {
-    ActArgs a{};
-    if (!act_args(rows, cols, dt, x, ldx, out, a)) return;
-    ProfScope prof("act_pack", stream);
-    act_launch(a, dt, [&](unsigned nb, auto t, auto u, auto past) {
-      k_pack<decltype(t), decltype(u)::value, decltype(past)::value><<<nb, 256, 0, stream>>>(a);
-    });
-  });
+  return guarded([&] { act8::pack(rows, cols, dt, x, ldx, out, "act_pack", stream); });
 }
 
 extern "C" seg_status seg_act_unpack(int64_t rows, int32_t cols, seg_dtype dt, const seg_act8 *in,
                                      void *x, int64_t ldx, hipStream_t stream) {
-  return guarded([&] {
-    ActArgs a{};
-    if (!act_args(rows, cols, dt, x, ldx, in, a)) return;
-    ProfScope prof("act_unpack", stream);
-    act_launch(a, dt, [&](unsigned nb, auto t, auto u, auto past) {
-      k_unpack<decltype(t), decltype(u)::value, decltype(past)::value><<<nb, 256, 0, stream>>>(a);
-    });
-  });
+  return guarded([&] { act8::unpack(rows, cols, dt, in, x, ldx, "act_unpack", stream); });
 }

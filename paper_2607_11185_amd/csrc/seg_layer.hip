@@ -503,11 +503,11 @@ glu::Kept kept_rows(const Ext &ext, long r0, int I) {
 }
 
 void pack(long rows, int cols, const unsigned short *x, const seg_act8 &to, hipStream_t st) {
-  check_status(seg_act_pack(rows, cols, SEG_BF16, x, cols, &to, st));
+  act8::pack(rows, cols, SEG_BF16, x, cols, &to, nullptr, st);
 }
 
 void unpack(long rows, int cols, const seg_act8 &from, unsigned short *x, hipStream_t st) {
-  check_status(seg_act_unpack(rows, cols, SEG_BF16, &from, x, cols, st));
+  act8::unpack(rows, cols, SEG_BF16, &from, x, cols, nullptr, st);
 }
 
 void layer_fwd_impl(const seg_layout *L, const seg_sizes *sz, const seg_layer_cfg &c,

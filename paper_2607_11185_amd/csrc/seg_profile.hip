@@ -26,7 +26,7 @@ void destroy_pair(hipEvent_t a, hipEvent_t b) {
 }  // namespace
 
 ProfScope::ProfScope(const char *name, hipStream_t s) : name_(name), stream_(s) {
-  if (!g_on.load(std::memory_order_relaxed)) return;
+  if (!name || !g_on.load(std::memory_order_relaxed)) return;
   if (hipEventCreate(&start_) != hipSuccess) return;
   if (hipEventCreate(&stop_) != hipSuccess) {
     (void)hipEventDestroy(start_);

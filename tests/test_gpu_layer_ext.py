@@ -271,3 +271,35 @@ def test_output_in_place_of_the_input(name, keep_gate):
         res.append({"y": _rows(lr.pad, y), "dx": dx, **kept, **{"d" + n: t for n, t in g.items()}})
     for n in res[0]:
         assert torch.equal(res[0][n], res[1][n]), n
+
+
+def test_timing_counts_each_kernel_once():
+    """The layer's packing and unpacking are under "ly_act8", the operators' own calls under their
+    names, and calls that are refused or have no rows nowhere."""
+    import ctypes
+
+    import torch
+    lr = ExtRun(*CASES["d64_gqa4_buffers"])
+    L = _lib.lib()
+
+    def count(name):
+        ms, n = ctypes.c_double(), ctypes.c_int64()
+        _lib.check(L.seg_profile_read(name.encode(), ctypes.byref(ms), ctypes.byref(n)))
+        return n.value
+    L.seg_profile_reset()
+    L.seg_profile_enable(1)
+    try:
+        s8 = S.layer_saved8(lr.lay, lr.lc, True)
+        S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, lr.rope, lr.pos, saved8=s8)
+        assert count("ly_act8") >= 1 and count("act_pack") == 0
+        S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, lr.dy, lr.rope, lr.pos, saved8=s8)
+        assert count("ly_act8") >= 2 and count("act_unpack") == count("act_pack") == 0
+        S.seg_act_pack(S.seg_act_unpack(s8["x"]))
+        x = torch.ones(4, 32, device=lr.dev)
+        with pytest.raises(_lib.SegError):
+            S.seg_act_pack(x, S.Act8(x.view(torch.int8).flatten()[:128].view(4, 32), s8["x"].exp[:4, :1].contiguous()))
+        S.seg_act_pack(x[:0])
+        assert count("act_unpack") == count("act_pack") == 1
+    finally:
+        L.seg_profile_enable(0)
+        L.seg_profile_reset()
