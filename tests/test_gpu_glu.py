@@ -319,3 +319,79 @@ def test_sigmoid_where_it_is_subnormal(rows, hidden, inter):
     tol = np.abs(ref) * ((np.abs(g[ok]) + 8) * 2.0 ** -23 + 2.0 ** -8) * 1.01 + np.abs(g[ok]) * 2.0 ** -149 + 2.0 ** -133
     assert ok.any()
     _within(_np(out["m"])[ok], ref[:, None], tol[:, None], "m of the backward")
+
+
+# Launches that the shapes above leave out, each with ragged last tiles: rows, hidden, inter
+REST = [(136, 344, 33896), (10847, 6848, 8), (41876, 5120, 136), (8274, 8, 1256), (35082, 272, 136), (5057, 3104, 360),
+        (5648, 3472, 2408), (32792, 8, 8), (1809, 8, 5392), (727, 8, 33432), (7304, 264, 19128), (66, 8, 16576)]
+
+
+def _launch(rows, hidden, inter, which):
+    """The way a product is cut and the rows of its (rest's) tiles."""
+    import ctypes
+    way = _choice(rows, hidden, inter, which)
+    out = (ctypes.c_int32 * 4)()
+    _lib.lib().seg_glu_gemm_choice(rows, hidden, inter, which, out)
+    return which, way, out[0]
+
+
+def test_every_launch_is_tested():
+    """With both tile heights: the forward, dx and the weight gradients uncut, in parts of K, and
+    as whole rounds of tiles with a rest in halves of tiles or in parts of K."""
+    got = {_launch(*s, w) for s in [*SHAPES, LARGE, *REST] for w in range(3)}
+    few = {(0, f"few {n}", n) for n in (1, 2, 16, 32, 64)}
+    ways = {(w, way, t) for w in range(3) for t in (128, 256) for way in ("whole", "parts", "rounds + parts of the rest")}
+    ways |= {(w, "rounds + halves", 128) for w in range(3)} | {(w, "parts of the rest", 128) for w in range(3)}
+    ways |= {(0, "parts of the rest", 256)}
+    ways -= {(0, "parts", 128), (0, "parts", 256)}      # of the forward all tiles are a rest then
+    assert got >= few | ways, (few | ways) - got
+    # sizes of the timing cases and of the decoder layer's classes bring no others
+    more = {_launch(r, h, i, w) for r in (1, 4, 65, 100, 300, 1000, 1500, 3000, 4096, 8192, 16384, 65536, 138819)
+            for h, i in ((896, 4864), (1536, 8960), (2048, 5504), (3584, 18944), (4096, 14336), (8192, 28672)) for w in range(3)}
+    assert more <= got, more - got
+
+
+def _over(got, ref, tol, name):
+    worst = float((got.double() - ref).abs().sub_(tol).max())
+    assert worst <= 0, (name, worst)
+
+
+@pytest.mark.parametrize("shape", REST, ids=lambda s: "x".join(map(str, s)))
+def test_launches_of_larger_products(shape):
+    """Forward, with and without kept values, and backward from kept values with both types of
+    weight gradients, against products in 64 bits on the GPU; bounds as above."""
+    import torch
+    rows, hidden, inter = shape
+    say(shape, [_launch(*shape, w)[1:] for w in range(3)])
+    x, wg, wu, dm = _inputs(*shape, seed=7, pad=8)
+    xd, wgd, wud, dmd = (t.double() for t in (x, wg, wu, dm))
+    h = 2.0 ** -8
+    g, u = xd @ wgd.t(), xd @ wud.t()
+    n = (hidden + 1) * 2.0 ** -24
+    eg, eu = n * (xd.abs() @ wgd.abs().t()), n * (xd.abs() @ wud.abs().t())
+    silu = g * torch.sigmoid(g)
+    em = 1.1 * eg * (u.abs() + eu) + silu.abs() * eu + (silu * u).abs() * (g.abs() + 8) * 2.0 ** -23
+    m, kept = S.seg_glu_fwd(x, wg, wu, keep=True)
+    _over(m, silu * u, em + h * ((silu * u).abs() + em) + 1e-38, "m")
+    assert torch.equal(m, S.seg_glu_fwd(x, wg, wu)[0])
+    del silu, em
+    for a, v, e in zip(kept, (g, u), (eg, eu)):
+        top = torch.nn.functional.pad(v.abs(), (0, -inter % 32)).view(rows, -1, 32).amax(-1).repeat_interleave(32, 1)[:, :inter]
+        _over(S.seg_act_unpack(a, torch.float32), v, (top + e) / 127 + e, "kept")
+    del g, u, eg, eu, top
+    gv, uv = (S.seg_act_unpack(a, torch.float32).double() for a in kept)
+    s = torch.sigmoid(gv)
+    dg, du = dmd * uv * s * (1 + gv * (1 - s)), dmd * gv * s
+    ge = dg.abs() * h + (dmd * uv).abs() * (gv.abs() + 8) * 2.0 ** -22
+    ue = du.abs() * h + (dmd * gv).abs() * 2.0 ** -22
+    ga, ua = dg.abs() + ge, du.abs() + ue
+    want = {"dx": (dg @ wgd + du @ wud,
+                   ge @ wgd.abs() + ue @ wud.abs() + (2 * inter + 1) * 2.0 ** -24 * (ga @ wgd.abs() + ua @ wud.abs()))}
+    for name, d, e, a in (("dwg", dg, ge, ga), ("dwu", du, ue, ua)):
+        want[name] = d.t() @ xd, (e + (rows + 1) * 2.0 ** -24 * a).t() @ xd.abs()
+    del dg, du, ge, ue, ga, ua, s, gv, uv
+    for dt in (torch.bfloat16, torch.float32):
+        out = S.seg_glu_bwd(x, wg, wu, dm, kept, dw_dtype=dt)
+        for name, (ref, tol) in want.items():
+            more = h * (ref.abs() + tol) if out[name].dtype == torch.bfloat16 else 0
+            _over(out[name], ref, tol + more + 1e-38, name)
