@@ -395,3 +395,18 @@ def test_launches_of_larger_products(shape):
         for name, (ref, tol) in want.items():
             more = h * (ref.abs() + tol) if out[name].dtype == torch.bfloat16 else 0
             _over(out[name], ref, tol + more + 1e-38, name)
+
+
+@pytest.mark.parametrize("shape", [(1, 328, 104), (2, 328, 104), (5, 328, 104), (16, 1096, 40), (30, 1096, 104), (50, 328, 72),
+                                   (300, 328, 104), (70, 1040, 40)], ids=str)
+def test_an_infinity_reaches_its_whole_row(shape):
+    """An infinity of x makes every feature of its row non-finite: g and u are infinities or (a
+    weight of zero) NaN, and silu of an infinity times one is an infinity or NaN."""
+    import torch
+    rows, hidden, inter = shape
+    x, wg, wu, _ = _inputs(*shape, seed=6)
+    for k in (0, hidden - 3, hidden - 1):
+        x2 = x.clone()
+        x2[rows - 1, k] = float("inf")
+        m = S.seg_glu_fwd(x2, wg, wu)[0]
+        assert bool(m[:-1].isfinite().all()) and not bool(m[-1].isfinite().any()), k
