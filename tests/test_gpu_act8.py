@@ -114,3 +114,39 @@ def test_nothing_is_written_past_the_end(rows, cols):
         v = torch.full((rows * cols + 999,), 77, dtype=dt, device="cuda")
         S.seg_act_unpack(out, x=v[:rows * cols].view(rows, cols))
         assert bool((v[rows * cols:] == 77).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,wide", [(200000, 3, 3), (150000, 33, 37), (5000, 1001, 1001), (1200, 18944, 18944), (9001, 4003, 4007)])
+def test_large_tensors_equal_their_parts(rows, cols, wide, dtype):
+    """Four chunks a lane, through the caches and (the last two) past them: every row as in calls
+    of a few rows, which take one chunk a lane and equal the oracle above; nothing behind the
+    end or between the rows is written."""
+    import torch
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    base = torch.randn(rows, wide, generator=gen, device="cuda")
+    base *= torch.exp(3 * torch.randn(rows, 1, generator=gen, device="cuda"))
+    base = base.to(dt)
+    x = base[:, wide - cols:]
+    x[rows // 3] = 0
+    x[rows // 2, cols - 1] = float("inf")
+    nb = -(-cols // 32)
+    part = (1 << 19) // (nb * (4 if dtype == "bf16" else 8))
+    assert part < rows
+    say(f"{rows} x {cols} of {wide} {dtype}, parts of {part}")
+    code = torch.full((rows * cols + 4096,), 77, dtype=torch.int8, device="cuda")
+    exp = torch.full((rows * nb + 4096,), 77, dtype=torch.uint8, device="cuda")
+    a = S.Act8(code[:rows * cols].view(rows, cols), exp[:rows * nb].view(rows, nb))
+    S.seg_act_pack(x, a)
+    assert bool((code[rows * cols:] == 77).all()) and bool((exp[rows * nb:] == 77).all())
+    out = torch.full((rows + 1, wide), 7.0, dtype=dt, device="cuda")
+    S.seg_act_unpack(a, x=out[:rows, wide - cols:])
+    assert bool((out[rows:] == 7).all()) and bool((out[:, :wide - cols] == 7).all())
+    for r in range(0, rows, part):
+        s = slice(r, min(r + part, rows))
+        p = S.seg_act_pack(x[s])
+        assert torch.equal(a.code[s], p.code) and torch.equal(a.exp[s], p.exp), s
+        v, w = out[s, wide - cols:], S.seg_act_unpack(p, dt)
+        assert torch.equal(v.isnan(), w.isnan()) and torch.equal(v.nan_to_num(), w.nan_to_num()), s
+    assert bool(a.exp[rows // 2, -1] == 255) and not a.code[rows // 3].any()
