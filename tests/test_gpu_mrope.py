@@ -241,3 +241,27 @@ def test_rotation_near_a_quarter_turn(inverse):
     assert (np.abs(ref[pos > 0]) < 1e-3).sum() > 20
     over = np.abs(got - ref) - 2.5 * 2.0 ** -23 * np.abs(ref) - 1e-11
     assert over.max() <= 0, (float(over.max()), int((over > 0).sum()))
+
+
+@pytest.mark.parametrize("dtype,rows", [("f32", 20011), ("bf16", 40013)])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rotation_past_the_caches(dtype, rows, inverse):
+    """Tensors of more than 96 MB read and written, in place and not: every row as in calls of a
+    few rows."""
+    import torch
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    qkv = _rows(rows, 14, 64, dt, gen=gen)
+    pos = torch.randint(-20, 100000, (3, rows), generator=gen, device="cuda", dtype=torch.int32)
+    cfg = S.MropeCfg((8, 12, 12))
+    f = S.seg_mrope_bwd if inverse else S.seg_mrope_fwd
+    assert 2 * rows * 13 * 64 * qkv.element_size() > 96 << 20
+    say(f"{rows} x 13 x 64 {dtype}")
+    got = f(qkv[:, :12], qkv[:, 12:13], pos, cfg)
+    for r in range(0, rows, 5000):
+        s = slice(r, min(r + 5000, rows))
+        want = f(qkv[s, :12], qkv[s, 12:13], pos[:, s].contiguous(), cfg)
+        assert torch.equal(got[0][s], want[0]) and torch.equal(got[1][s], want[1]), s
+    copy = qkv.clone()
+    f(copy[:, :12], copy[:, 12:13], pos, cfg, copy[:, :12], copy[:, 12:13])
+    assert torch.equal(copy[:, :12], got[0]) and torch.equal(copy[:, 12:13], got[1]) and torch.equal(copy[:, 13:], qkv[:, 13:])
