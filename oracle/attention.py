@@ -65,6 +65,24 @@ def backward(q, k, v, mask, scale, dout):
     return dq, dk, dv
 
 
+def backward_from(q, k, v, o, lse, mask, scale, dout):
+    """The same from given O and LSE, which need not be those of q, k and v (values read
+    back with fewer bits): P = exp(S - LSE), dS = P * (dP - rowsum(dO * O))."""
+    n, hq, d = q.shape
+    hkv = k.shape[1]
+    dq, dk, dv = (np.zeros_like(t, dtype=np.float64) for t in (q, k, v))
+    for h in range(hq):
+        g = _kv_head(h, hq, hkv)
+        s = scale * (q[:, h, :] @ k[:, g, :].T)
+        p = np.exp(np.where(mask, s - lse[h][:, None], -np.inf))
+        dv[:, g, :] += p.T @ dout[:, h, :]
+        dp = dout[:, h, :] @ v[:, g, :].T
+        ds = p * (dp - (dout[:, h, :] * o[:, h, :]).sum(axis=1, keepdims=True))
+        dq[:, h, :] = scale * (ds @ k[:, g, :])
+        dk[:, g, :] += scale * (ds.T @ q[:, h, :])
+    return dq, dk, dv
+
+
 def forward_rows(q_rows, k, v, mask_rows, scale):
     """Forward for a subset of query rows: q_rows [r, hq, d], mask_rows [r, n]."""
     return forward_generic(q_rows, k, v, mask_rows, scale)

@@ -119,9 +119,10 @@ def forward(x, w, segments, masks, hq, hkv, d, eps, base, rot=None):
     return y, saved
 
 
-def backward(x, w, segments, masks, hq, hkv, d, eps, base, saved, dy, rot=None):
+def backward(x, w, segments, masks, hq, hkv, d, eps, base, saved, dy, rot=None, own_softmax=True):
     """Gradients of sum(y * dy) over the segment rows: dx and the weight
-    gradients (a dict).  Padding rows carry no gradient (their dy counts as 0)."""
+    gradients (a dict).  Padding rows carry no gradient (their dy counts as 0).
+    own_softmax false: the attention's from saved o and lse (attention.backward_from)."""
     P = x.shape[0]
     s = saved
     dy = dy * (s["pos"] >= 0)[:, None]
@@ -145,8 +146,11 @@ def backward(x, w, segments, masks, hq, hkv, d, eps, base, saved, dy, rot=None):
     dv = np.zeros((P, hkv, d))
     for sg, m in zip(segments, masks):
         rows = slice(sg.start, sg.start + sg.length)
-        dq[rows], dk[rows], dv[rows] = OA.backward(s["qr"][rows], s["kr"][rows], s["v"][rows],
-                                                    m, scale, do[rows])
+        qkv = s["qr"][rows], s["kr"][rows], s["v"][rows]
+        if own_softmax:
+            dq[rows], dk[rows], dv[rows] = OA.backward(*qkv, m, scale, do[rows])
+        else:
+            dq[rows], dk[rows], dv[rows] = OA.backward_from(*qkv, s["o"][rows], s["lse"][:, rows], m, scale, do[rows])
     pz = np.maximum(s["pos"], 0)
     rot = rot or (lambda t, inverse: rope(t, pz, base, inverse))
     dq = rot(dq, True).reshape(P, hq * d)

@@ -303,3 +303,68 @@ def test_timing_counts_each_kernel_once():
     finally:
         L.seg_profile_enable(0)
         L.seg_profile_reset()
+
+
+@pytest.mark.parametrize("keep_gate", [False, True])
+@pytest.mark.parametrize("x_by,k_by", [(32, 1), (1, 16), (32, 16)])
+def test_large_channels(x_by, k_by, keep_gate):
+    """A few channels of the residual stream 32 times (with norm weights 1 / 32 there), and two of
+    every key head 16 times the others, which leaves their blocks' other columns two or three bits.
+    The backward equals that of the kept values in 64 bits (probabilities against the forward's
+    lse) within the bound of bf16 results; next to the gradients in bf16 it is off by what 64
+    bits give for the format alone, E, and the two calls' own bounds."""
+    import torch
+    say(x_by, k_by, keep_gate)
+    lr = ExtRun(*CASES["d128_chunked"])
+    c, ch = lr.cfg, [5, 77, 200]
+    x, w, ref, masks, a, dy = lr.oracle_parts()
+    key = [h * c.head_dim + i for h in range(c.hkv) for i in (3, 70)]
+    for t in (x, lr.x):
+        t[:, ch] *= x_by
+    for n, rows, by in (("g1", ch, 1 / x_by), ("g2", ch, 1 / x_by), ("wk", key, k_by)):
+        lr.w[n][rows] *= by
+        getattr(w, n)[rows] *= by
+    y, saved = S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, lr.rope, lr.pos)
+    dx16, g16 = S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, lr.dy, lr.rope, lr.pos, x=lr.x, saved=saved)
+    s8 = S.layer_saved8(lr.lay, lr.lc, keep_gate)
+    S.seg_layer_fwd_ext(lr.lay, lr.lc, lr.w, lr.x, lr.rope, lr.pos, saved8=s8)
+    dx, grads = S.seg_layer_bwd_ext(lr.lay, lr.lc, lr.w, lr.dy, lr.rope, lr.pos, saved8=s8)
+    ok = ref.tok_src >= 0
+
+    def backward(x8, sv):
+        """from kept values: both norms' and the block's of x and y1, unless g and u are kept"""
+        sv["a"], _ = OLY.rms_forward(x8, w.g1, EPS)
+        sv["b"], _ = OLY.rms_forward(sv["y1"], w.g2, EPS)
+        if "gt" not in sv:
+            sv["gt"], sv["ut"] = sv["b"] @ w.wg.T, sv["b"] @ w.wu.T
+        sv["mm"] = OLY.silu(sv["gt"]) * sv["ut"]
+        return OLY.backward(x8, w, ref.segments, masks, **a, saved=sv, dy=dy, own_softmax=False)
+
+    def values(t, *shape):
+        t = _np(t)
+        t[~ok] = 0
+        return t.reshape(lr.P, *shape) if shape else t
+    heads = {"q": (c.hq, c.head_dim), "k": (c.hkv, c.head_dim), "v": (c.hkv, c.head_dim), "o": (c.hq, c.head_dim)}
+    sv = {n + ("r" if n in "qk" else ""): values(S.seg_act_unpack(s8[n]), *shape) for n, shape in heads.items()}
+    sv.update(y1=values(S.seg_act_unpack(s8["y1"])), lse=_np(s8["lse"]), pos=OLY.segment_positions(ref.segments, lr.P))
+    sv["r1"], sv["r2"] = (np.where(ok, _np(s8[n]), 0) for n in ("rstd1", "rstd2"))
+    if keep_gate:
+        sv["gt"], sv["ut"] = (values(S.seg_act_unpack(s8[n])) for n in ("g", "u"))
+    want = backward(values(S.seg_act_unpack(s8["x"])), sv)
+    # the format alone: 64-bit values packed
+    _, ex = OLY.forward(x, w, ref.segments, masks, **a)
+    full = OLY.backward(x, w, ref.segments, masks, **a, saved=ex, dy=dy)
+
+    def keep(t):
+        return OA8.unpack(*OA8.pack(t.reshape(lr.P, -1))).reshape(t.shape)
+    packed = {n: keep(ex[n]) if n in ("qr", "kr", "v", "o", "y1") or keep_gate and n in ("gt", "ut") else ex[n]
+              for n in ex if keep_gate or n not in ("gt", "ut")}
+    alone = backward(keep(x), packed)
+    named = lambda r: {"dx": np.where(ok[:, None], r[0], 0), **r[1]}  # noqa: E731
+    want, full, alone = named(want), named(full), named(alone)
+    for n, got in {"dx": dx, **grads}.items():
+        E = rel(alone[n], full[n])
+        d16 = rel(_np(got), _np(dx16 if n == "dx" else g16[n]))
+        say(n, f"of the kept values {rel(_np(got), want[n]):.4f}, next to bf16 {d16:.4f}, the format {E:.4f}")
+        assert rel(_np(got), want[n]) < TOL, n
+        assert d16 < E + 2 * TOL, n
