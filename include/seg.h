@@ -393,8 +393,11 @@ typedef struct {
  * k_out unused) by positions pos [3, rows]: the pair (i, i + d/2) of a head
  * turns by pos[axis(i)][row] * base^(-2i/d), where the first sections[0] pairs
  * are on axis 0, the next sections[1] on axis 1 and the last on axis 2; (d/2,
- * 0, 0) is the one-dimensional embedding of seg_layer_fwd.  Angles are formed
- * in fp64; fp32 tensors are rotated in fp32.  ldq, ldk, ldqo, ldko: elements
+ * 0, 0) is the one-dimensional embedding of seg_layer_fwd.  Not this form, and
+ * not served: axes that take turns pair by pair, and rotation of a part of a head.
+ * Pairs of adjacent columns (2i, 2i + 1) are these once a head's columns are put in
+ * the order of the even ones and then the odd ones (rows of wq and wk, alike).
+ * Angles are formed in fp64; fp32 tensors are rotated in fp32.  ldq, ldk, ldqo, ldko: elements
  * between rows (at least heads * d), so q and k may be parts of one
  * projection's rows; an output may be its input (same pointer and stride), and
  * must not overlap an input otherwise, pos among them (SEG_ERR_ARG).  Rows with a negative position on any
