@@ -470,7 +470,8 @@ size_t seg_glu_workspace_bytes(int32_t rows, int32_t hidden, int32_t inter, int3
  *   dwg = dg^T x, dwu = du^T x [inter, hidden] (dtype dw_dt; overwritten).
  * m [rows, inter] or NULL: silu(g) * u again, which the weight gradient of the
  * projection behind the block reads.  dg and du are rounded to bf16 for the
- * products.
+ * products, and so are g and u, before the slope is formed, where they are computed
+ * again: each by at most 2^-8 of itself.
  */
 seg_status seg_glu_bwd(int32_t rows, int32_t hidden, int32_t inter, const void *x, int64_t ldx,
                        const void *wg, const void *wu, const seg_act8 *g8, const seg_act8 *u8,
