@@ -492,8 +492,8 @@ seg_status seg_glu_bwd(int32_t rows, int32_t hidden, int32_t inter, const void *
  *   read back (seg_act_unpack) and lse, rstd1 and rstd2 of the forward; the
  *   probabilities of the kept q and k against that lse need not sum to one.  Next
  *   to the gradients with bf16 `saved` they are off (relative Frobenius norm) by up
- *   to 2 % where channels are alike, by up to 5 % (the gain g2 10 %) where some of x
- *   are 32 times their neighbours, by 7 to 12 % in dx, wq, wk and wv where two of
+ *   to 2 % where channels are alike, by up to 5 % (the gain g2 11 %) where some of x
+ *   are 32 times their neighbours, by 6 to 12 % in dx, g1, wq, wk and wv where two of
  *   every key head are 16 times theirs: a block's largest value sets its step.  With
  *   codes for g and u (both or none) the gate and up values are kept too, and
  *   the backward does not compute the two projections again.  y is the same,
