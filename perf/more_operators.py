@@ -144,7 +144,7 @@ def _two_to(e):
 
 
 def _pack(x, block_rows):
-    """Codes [rows, cols up to 16] and exponent bytes [blocks of rows, blocks of columns up to 4]
+    """Codes [rows, cols up to 16] and exponent bytes [blocks of columns, blocks of rows up to 16]
     of x: the least power of two 2^s (s >= -127) with max|x| <= 448 2^s for each block."""
     rows, cols = x.shape
     p = torch.nn.functional.pad(x.float(), (0, -cols % BLOCK, 0, -rows % block_rows))
@@ -155,11 +155,11 @@ def _pack(x, block_rows):
     code = (b * _two_to(127 - s)[:, None, :, None]).to(torch.float8_e4m3fn)
     code = code.view(p.shape)[:rows, :cols].view(torch.uint8)
     code = torch.nn.functional.pad(code, (0, -cols % 16))
-    return code.contiguous(), torch.nn.functional.pad((s + 127).to(torch.uint8), (0, -s.shape[1] % 4))
+    return code.contiguous(), torch.nn.functional.pad((s + 127).to(torch.uint8).t(), (0, -s.shape[0] % 16)).contiguous()
 
 
 def _unpack(code, exp, rows, cols, block_rows):
-    s = _two_to(exp.int()).repeat_interleave(block_rows, 0)[:rows].repeat_interleave(BLOCK, 1)[:, :cols]
+    s = _two_to(exp.t().int()).repeat_interleave(block_rows, 0)[:rows].repeat_interleave(BLOCK, 1)[:, :cols]
     return code[:, :cols].view(torch.float8_e4m3fn).float() * s
 
 
@@ -293,7 +293,7 @@ def exact(c, seed):
         w = value[code[:, :c["cols"]].long()]
         at = torch.arange(c["outs"], device=DEV) // c["block_rows"]
         for b in range(-(-c["cols"] // BLOCK)):
-            w[:, b * BLOCK:(b + 1) * BLOCK] *= (exp[at, b].long() + 896 << 52).view(torch.float64)[:, None]
+            w[:, b * BLOCK:(b + 1) * BLOCK] *= (exp[b, at].long() + 896 << 52).view(torch.float64)[:, None]
         return _exact_values(st["x"], 1) @ w.t()
     if c["kind"] == "top":
         ids, logits, lse = [], [], []
