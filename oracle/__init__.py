@@ -18,5 +18,6 @@ layer      decoder layer (RMSNorm, rotary GQA attention, SwiGLU) around the
 mrope      rotary positions on three axes: positions of a segment, rotation
 act8       activations in 8 bits (blocks of 32 columns, a power of two each)
 glu        gated feed-forward block, forward and backward
+fp8        8-bit floating point (blocks of 128 columns, a power of two each)
 """
-from . import layout, attention, loss, layer, mrope, act8, glu  # noqa: F401
+from . import layout, attention, loss, layer, mrope, act8, glu, fp8  # noqa: F401

@@ -30,7 +30,8 @@ EXPORTS = ["seg_layout_query", "seg_build_layout", "seg_attn_workspace_bytes", "
            "seg_mrope_bwd", "seg_act_pack", "seg_act_unpack", "seg_glu_fwd",
            "seg_glu_workspace_bytes", "seg_glu_bwd", "seg_layer_ext_workspace_bytes",
            "seg_layer_fwd_ext", "seg_layer_bwd_ext", "seg_profile_enable",
-           "seg_profile_reset", "seg_profile_read", "seg_last_error"]
+           "seg_profile_reset", "seg_profile_read", "seg_last_error",
+           "seg_fp8_pack", "seg_fp8_unpack", "seg_fp8_gemm_workspace_bytes", "seg_fp8_gemm"]
 
 P32 = ctypes.POINTER(ctypes.c_int32)
 VP = ctypes.c_void_p
@@ -104,6 +105,10 @@ class SegMropeCfg(ctypes.Structure):
 
 class SegAct8(ctypes.Structure):
     _fields_ = [("code", VP), ("exp", VP)]
+
+
+class SegFp8(ctypes.Structure):
+    _fields_ = [("code", VP), ("exp", VP), ("block_rows", ctypes.c_int32)]
 
 
 SAVED8 = ("x", "y1", "q", "o", "k", "v", "g", "u")
@@ -204,6 +209,13 @@ def lib() -> ctypes.CDLL:
         L.seg_glu_bwd.restype = ctypes.c_int
         L.seg_glu_bwd.argtypes = [i32, i32, i32, VP, i64, VP, VP, act8, act8, VP, VP, VP, dtype, VP, VP,
                                   VP, size, VP]
+        fp8 = ctypes.POINTER(SegFp8)
+        L.seg_fp8_pack.restype = L.seg_fp8_unpack.restype = L.seg_fp8_gemm.restype = ctypes.c_int
+        L.seg_fp8_pack.argtypes = [i64, i32, dtype, VP, i64, fp8, VP]
+        L.seg_fp8_unpack.argtypes = [i64, i32, dtype, fp8, VP, i64, VP]
+        L.seg_fp8_gemm_workspace_bytes.restype = size
+        L.seg_fp8_gemm_workspace_bytes.argtypes = [i32, i32, i32]
+        L.seg_fp8_gemm.argtypes = [i32, i32, i32, fp8, fp8, dtype, VP, i64, VP, size, VP]
         layer = [ctypes.POINTER(SegLayout), ctypes.POINTER(SegSizes), ctypes.POINTER(SegLayerCfg),
                  ctypes.POINTER(SegLayerExt), ctypes.POINTER(SegLayerWeights), VP]
         L.seg_layer_ext_workspace_bytes.restype = size

@@ -1,0 +1,534 @@
+// Product of two tensors in 8-bit floating point with blocks of 128 (format: fp8.h):
+//   y(m, n) = sum_b 2^(sa(m, b) + sb(n, b)) sum_{k in block b} a(m, k) b(n, k)
+// A step of the inner loop is one block of columns, 128 bytes of a row, and one matrix
+// instruction (16x16x128) takes a whole step and both operands' powers of two, so the
+// scales cost no arithmetic.  Inside the instruction the products of groups of 16
+// columns (each whole on its own) are aligned to the group's largest and lose what is
+// 2^-13 of it and below; the groups' sums and the accumulator add up in fp32.  (An
+// 8-bit instruction without scales rounds the same way.)
+//
+// The compiler takes the scaled instruction for shorter than it is: vector instructions
+// that read its result too soon got the accumulator of before.  So the results are read
+// behind settled(), which waits longer than the instruction takes; other matrix
+// instructions may follow at once, the hardware orders them.
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+#include "fp8.h"
+#include "gemm.h"
+
+namespace seg {
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// one step: SW and SX pick the byte of each lane's row in sw and sx
+template <int SW, int SX>
+__device__ __forceinline__ f32x4 mfma8(const i32x8 &w, const i32x8 &x, const f32x4 &c, unsigned sw, unsigned sx) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, 0, 0, SW, (int)sw, SX, (int)sx);
+}
+__device__ __forceinline__ i32x8 join(const i32x4 &a, const i32x4 &b) {
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+template <class F, int... I>
+__device__ __forceinline__ void each_of(F &&f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each(F &&f) {
+  each_of(f, std::make_integer_sequence<int, N>());
+}
+// the matrix instructions of before have written their results
+__device__ __forceinline__ void settled() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+struct Operand {
+  const uint8_t *code, *exp;
+  long ld, lde;  // bytes of a row of codes, of a block of columns' bytes
+  int rows, square;
+};
+
+// N consecutive columns of a row of y, from its sums: whole where the row holds them
+// (accesses of any width take any alignment of an element)
+template <class T, int N>
+__device__ __forceinline__ void store_run(T *d, int left, const float (&v)[N]) {
+  if (left >= N) {
+    typedef T V __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+    constexpr int W = 16 / sizeof(T);
+#pragma unroll
+    for (int q = 0; q < N / W; ++q) {
+      V o;
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        if constexpr (sizeof(T) == 2) o[j] = f2bf_bits(v[q * W + j]);
+        else o[j] = v[q * W + j];
+      }
+      *reinterpret_cast<V *>(d + q * W) = o;
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (j < left) store_val(d, j, v[j]);
+}
+
+struct Gemm8 {
+  Operand a, b;
+  void *y;
+  long ldy, split_stride;  // elements between rows, and between the partial sums of parts
+  int steps, part, splits, tiles;
+};
+
+// ------------------------------------------------------------------ many rows
+//
+// Tiles, waves and schedule are those of the bf16 product (k_gemm of gemm.h): 64 TM x
+// 256 a block of 8 waves in two groups half a step apart, 128 bytes of every row a
+// step, direct loads to two slots of A and three of B in LDS.  A step of 128 codes
+// takes the matrix cores the time of 64 bf16 values.
+//
+// Rows of a wave tile are dealt to the operand's fragments in turn: row q of fragment i
+// of F is row F q + i of the tile (the loads put it there).  So a lane's scales of all
+// its fragments are F neighbouring bytes, one load a step, picked by the instruction;
+// and a lane ends with 16 consecutive columns of a row, which it stores as they are.
+constexpr int BN = gemm::BN, STEP = fp8::BLOCK, THREADS = gemm::THREADS;
+
+struct Load8 {
+  gemm::gemm_i32x4 rs;
+  int voff, joff[8], chunk, bytes, add;
+
+  // F (4 or 8) fragments of 16 rows a wave tile; wave w of the group's four, load j: rows
+  // 8 (w + 4 j) .. of the tile in LDS
+  __device__ __forceinline__ void init(const uint8_t *code, long ld, int row0, int left, int F, int w, int lane) {
+    rs = gemm::gemm_desc(code + (long)row0 * ld, (long)left * ld);
+    const int p = 8 * (w & 1) + (lane >> 3);  // row of its fragment
+    chunk = ((lane & 7) ^ (p >> 1)) * 16;
+    bytes = (int)ld;
+    voff = (F * p + (w >> 1)) * (int)ld + chunk;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) joff[j] = (F == 4 ? 64 * (j / 2) + 2 * (j % 2) : 128 * (j / 4) + 2 * (j % 4)) * (int)ld;
+  }
+  __device__ __forceinline__ void prep(int k0) { add = k0 + chunk < bytes ? voff + k0 : 0x40000000; }
+  __device__ __forceinline__ void load(unsigned dst, int j, int w) const {
+    gemm::dma16(dst + (w + 4 * j) * 1024, add + joff[j], rs);
+  }
+};
+
+// The bytes of F fragments' rows of one step.
+template <int F>
+struct Scales {
+  static constexpr int N = (F + 3) / 4;
+  const uint8_t *p;
+  long lde;
+  int square;
+  __device__ __forceinline__ void init(const Operand &o, int row0, int q, int step) {
+    square = o.square;
+    lde = o.lde;
+    // rows past the end: any byte in range, their codes are zeros and their sums unused
+    const long at = square ? (row0 < o.rows ? row0 : o.rows - 1) / fp8::BLOCK : min((long)row0 + F * q, o.lde - F);
+    p = o.exp + (long)step * lde + at;
+  }
+  __device__ __forceinline__ void fetch(unsigned (&s)[N]) {
+    if (square) {
+      s[0] = *p;
+    } else if constexpr (N == 2) {
+      const uint2 v = *reinterpret_cast<const uint2 *>(p);
+      s[0] = v.x;
+      s[1] = v.y;
+    } else if constexpr (F == 4) {
+      s[0] = *reinterpret_cast<const unsigned *>(p);
+    } else if constexpr (F == 2) {
+      s[0] = *reinterpret_cast<const unsigned short *>(p);
+    } else {
+      s[0] = *p;
+    }
+    p += lde;
+  }
+  // what was fetched, waited for, as four rows' bytes a register
+  __device__ __forceinline__ void take(unsigned (&s)[N], unsigned (&to)[N]) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(s[i]));
+#pragma unroll
+    for (int i = 0; i < N; ++i) to[i] = square ? s[0] * 0x01010101u : s[i];
+  }
+};
+
+template <int TM, class T>
+__global__ void __launch_bounds__(THREADS, 1) k_gemm8(const Gemm8 g) {
+  constexpr int BM = gemm::bm_of(TM), SA = BM * STEP, SB = BN * STEP, LDS_B = SA * gemm::SLOTS_A;
+  __shared__ __attribute__((aligned(1024))) char lds[LDS_B + SB * gemm::SLOTS_B];
+  int idx = gemm::xcd_index(g.tiles * g.splits);
+  if (idx >= g.tiles * g.splits) return;
+  const int split = idx / g.tiles;
+  idx -= split * g.tiles;
+  int mt, nt;
+  gemm::tile_of(idx, (g.a.rows + BM - 1) / BM, (g.b.rows + BN - 1) / BN, mt, nt);
+  const int m0 = mt * BM, n0 = nt * BN;
+  const int lane = threadIdx.x & 63, col = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int grp = wave >> 2, w4 = wave & 3;  // waves w and w + 4 share a SIMD
+  const int wr = grp * 32 * TM, wc = w4 * 64;
+  const int s0 = split * g.part, nk = min(g.part, g.steps - s0);
+
+  constexpr int FA = 2 * TM, FB = 4;
+  Load8 ldr;  // the group's operand
+  if (grp == 0) ldr.init(g.a.code, g.a.ld, m0, min(BM, g.a.rows - m0), FA, w4, lane);
+  else ldr.init(g.b.code, g.b.ld, n0, min(BN, g.b.rows - n0), FB, w4, lane);
+  gemm::Frag<false, BM, FA> fA;
+  gemm::Frag<false, BN, FB> fB;
+  fA.init(0, wr, lane);
+  fB.init(LDS_B, wc, lane);
+  Scales<FA> ea;
+  Scales<FB> eb;
+  ea.init(g.a, m0 + wr, col, s0);
+  eb.init(g.b, n0 + wc, col, s0);
+  unsigned sa_next[Scales<FA>::N], sb_next[1], sa[Scales<FA>::N], sb[1];
+
+  f32x4 acc[FA][FB];
+#pragma unroll
+  for (int i = 0; i < FA; ++i)
+#pragma unroll
+    for (int j = 0; j < FB; ++j) acc[i][j] = f32x4{};
+
+  const unsigned base = (unsigned)(unsigned long)(__attribute__((address_space(3))) char *)lds;
+  const unsigned ring = base + (grp == 0 ? 0 : LDS_B);
+  constexpr int LA = BM / 32, LB = BN / 32;  // loads per wave of an A and of a B step
+  int k_next = s0 * STEP;
+  auto prep = [&]() __attribute__((always_inline)) {
+    ldr.prep(k_next);
+    k_next += STEP;
+  };
+  auto load = [&](int slot, int j) __attribute__((always_inline)) {
+    if (LA == LB || j < LA || grp == 1) ldr.load(ring + slot, j, w4);
+  };
+  if (nk > 0) {
+    ea.fetch(sa_next);
+    eb.fetch(sb_next);
+    ea.take(sa_next, sa);
+    eb.take(sb_next, sb);
+  }
+  prep();
+#pragma unroll
+  for (int j = 0; j < LB; ++j) load(0, j);
+  if (grp == 0) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  } else {
+    prep();
+#pragma unroll
+    for (int j = 0; j < LB; ++j) load(SB, j);
+    if (nk > 0) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LB) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+  __builtin_amdgcn_s_barrier();
+  GEMM_FENCE();
+  if (grp == 1 && nk > 0) __builtin_amdgcn_s_barrier();  // half a step behind group 0
+  GEMM_FENCE();
+
+  // barriers and waits: as in k_gemm; the scales of step t + 1 are fetched before the
+  // direct loads of step t's phase go out and waited for when its products are issued
+  int slot_b = 0, slot_b2 = 2 * SB;  // of steps t and t + 2
+#pragma unroll 1
+  for (int t = 0; t < nk; ++t) {
+    const int slot_a = (t & 1) * SA;
+    const int slot_n = grp == 0 ? SA - slot_a : slot_b2;
+    bf16x8 a[2][FA], b[2][FB];
+    if (t + 1 < nk) {
+      ea.fetch(sa_next);
+      eb.fetch(sb_next);
+    }
+    prep();
+    constexpr int NR = FA + FB, PER = LB / 2;  // reads and loads per half of a row's bytes
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+      for (int f = 0; f < NR; ++f) {
+#pragma unroll
+        for (int j = f * PER / NR; j < PER; ++j)
+          if (j * NR / PER == f) load(slot_n, kk * PER + j);
+        if (f < FB) b[kk][f] = fB.read(lds, slot_b, kk, f);
+        else a[kk][f - FB] = fA.read(lds, slot_a, kk, f - FB);
+      }
+    }
+    if (grp == 0)
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    else if (t + 2 < nk)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LB) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    GEMM_FENCE();
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+    each<FA>([&](auto i) __attribute__((always_inline)) {
+      each<FB>([&](auto jj) __attribute__((always_inline)) {
+        constexpr int I = decltype(i)::value, J = (I & 1) ? 3 - decltype(jj)::value : decltype(jj)::value;
+        acc[I][J] = mfma8<J, I & 3>(
+            join(__builtin_bit_cast(i32x4, b[0][J]), __builtin_bit_cast(i32x4, b[1][J])),
+            join(__builtin_bit_cast(i32x4, a[0][I]), __builtin_bit_cast(i32x4, a[1][I])), acc[I][J], sb[0], sa[I / 4]);
+      });
+    });
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+    slot_b = slot_b == 2 * SB ? 0 : slot_b + SB;
+    slot_b2 = slot_b2 == 2 * SB ? 0 : slot_b2 + SB;
+    if (grp == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (t + 1 < nk) {
+      ea.take(sa_next, sa);
+      eb.take(sb_next, sb);
+    }
+    if (grp == 0 || t + 1 < nk) __builtin_amdgcn_s_barrier();
+    GEMM_FENCE();
+  }
+  settled();
+  const int n = n0 + wc + 16 * lg;
+  if (n >= g.b.rows) return;
+  T *y = static_cast<T *>(g.y) + (long)split * g.split_stride;
+#pragma unroll
+  for (int i = 0; i < FA; ++i) {
+    const int m = m0 + wr + FA * col + i;
+    if (m >= g.a.rows) continue;
+    float v[16];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[4 * r + j] = acc[i][j][r];
+    // (partial sums: rows are filled up to 16)
+    store_run(y + (long)m * g.ldy + n, g.splits > 1 ? 16 : g.b.rows - n, v);
+  }
+}
+
+// Sums the parts in order: 8 columns of a row a thread.
+template <class T>
+__global__ void __launch_bounds__(256) k_finish8(const float *__restrict__ part, int parts, long stride, long ldp, int M,
+                                                 int N, T *__restrict__ y, long ldy) {
+  const unsigned n8 = (unsigned)(ldp / 8);
+  const long total = (long)M * n8;
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long)gridDim.x * 256) {
+    const long m = i / n8;
+    const int n = (int)(i - m * n8) * 8;
+    if (n >= N) continue;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < parts; ++k) {
+      const f32x4 *p = reinterpret_cast<const f32x4 *>(part + k * stride + m * ldp + n);
+      const f32x4 a = p[0], b = p[1];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] += a[j];
+        v[4 + j] += b[j];
+      }
+    }
+    store_run(y + m * ldy + n, N - n, v);
+  }
+}
+
+// ------------------------------------------------------------------ few rows
+//
+// Up to 16 NB rows of a, where the bytes of b are the work (k_glu_rows of the gated
+// block, in 8 bits): a block takes 16 CB rows of b, its waves every WAVES-th step, and
+// their sums are added up in LDS, in order.  Memory gives the codes fastest in whole
+// 128-byte lines, which is not the instruction's operand, so a lane's 16 bytes go
+// through the wave's own piece of LDS (chunk c of row r in slot c ^ (r & 7)), while the
+// loads of the wave's next step are under way; no wave waits for another.  Rows past
+// the end read the last one, and their sums go nowhere; codes past the row's end read
+// as zeros.
+template <int NB, int CB, int WAVES, class T>
+__global__ void __launch_bounds__(64 * WAVES, NB < 4 ? 4 : 2) k_few8(const Gemm8 g) {
+  constexpr int ROWS = 16 * (CB > NB ? CB : NB), STAGE = WAVES * ROWS * 8, SUMS = WAVES * CB * NB * 64;
+  __shared__ __attribute__((aligned(1024))) f32x4 lds[STAGE > SUMS ? STAGE : SUMS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, lg = lane >> 4, lr = lane >> 3, lc = lane & 7;
+  const int n0 = blockIdx.x * 16 * CB, ld = (int)g.b.ld;
+  // row p of a piece is row CB (p % 16) + p / 16 of b's (NB of a's): see k_gemm8
+  const uint8_t *bp = g.b.code + (long)n0 * ld;
+  unsigned boff[2 * CB], aoff[2 * NB];
+#pragma unroll
+  for (int i = 0; i < 2 * CB; ++i) {
+    const int p = 8 * i + lr;
+    boff[i] = (unsigned)min(CB * (p & 15) + (p >> 4), g.b.rows - 1 - n0) * (unsigned)ld + 16 * lc;
+  }
+#pragma unroll
+  for (int i = 0; i < 2 * NB; ++i) {
+    const int p = 8 * i + lr;
+    aoff[i] = (unsigned)min(NB * (p & 15) + (p >> 4), g.a.rows - 1) * (unsigned)ld + 16 * lc;
+  }
+  i32x4 w[2 * CB], x[2 * NB];
+  unsigned sw[1], sx[1], sw_next[1], sx_next[1];
+  Scales<CB> eb;
+  Scales<NB> ea;
+  eb.init(g.b, n0, r, wave);
+  ea.init(g.a, 0, r, wave);
+  eb.lde *= WAVES;
+  ea.lde *= WAVES;
+  auto load = [&](int s) __attribute__((always_inline)) {
+    const int k = s * STEP;
+    const bool in = k + 16 * lc < ld;
+#pragma unroll
+    for (int i = 0; i < 2 * CB; ++i)
+      w[i] = in ? __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(bp + k + boff[i])) : i32x4{};
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i)
+      x[i] = in ? *reinterpret_cast<const i32x4 *>(g.a.code + k + aoff[i]) : i32x4{};
+    sw_next[0] = sx_next[0] = 0;
+    if (s < g.steps) {
+      eb.fetch(sw_next);
+      ea.fetch(sx_next);
+    }
+  };
+  f32x4 acc[CB][NB];
+#pragma unroll
+  for (int b = 0; b < CB; ++b)
+#pragma unroll
+    for (int n = 0; n < NB; ++n) acc[b][n] = f32x4{};
+  i32x4 *stage = reinterpret_cast<i32x4 *>(lds) + wave * (ROWS * 8);
+  i32x4 *to = stage + lr * 8 + (lc ^ lr);
+  const i32x4 *from = stage + r * 8;
+  const int c0 = lg ^ (r & 7), c1 = (4 + lg) ^ (r & 7);
+  load(wave);
+  for (int s = wave; s < g.steps; s += WAVES) {
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) to[64 * i] = x[i];
+    __builtin_amdgcn_wave_barrier();
+    i32x8 cx[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) cx[n] = join(from[n * 128 + c0], from[n * 128 + c1]);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 2 * CB; ++i) to[64 * i] = w[i];
+    __builtin_amdgcn_wave_barrier();
+    sw[0] = eb.square ? sw_next[0] * 0x01010101u : sw_next[0];
+    sx[0] = ea.square ? sx_next[0] * 0x01010101u : sx_next[0];
+    load(s + WAVES);
+    each<CB>([&](auto b) __attribute__((always_inline)) {
+      constexpr int B = decltype(b)::value;
+      const i32x8 cw = join(from[B * 128 + c0], from[B * 128 + c1]);
+      each<NB>([&](auto n) __attribute__((always_inline)) {
+        constexpr int N = decltype(n)::value;
+        acc[B][N] = mfma8<B, N>(cw, cx[N], acc[B][N], sw[0], sx[0]);
+      });
+    });
+    __builtin_amdgcn_wave_barrier();
+  }
+  settled();
+  f32x4(*sums)[CB * NB][64] = reinterpret_cast<f32x4(*)[CB * NB][64]>(lds);
+  __syncthreads();
+#pragma unroll
+  for (int b = 0; b < CB; ++b)
+#pragma unroll
+    for (int n = 0; n < NB; ++n) sums[wave][b * NB + n][lane] = acc[b][n];
+  __syncthreads();
+  if (wave >= NB) return;
+  f32x4 v[CB];
+#pragma unroll
+  for (int b = 0; b < CB; ++b) v[b] = sums[0][b * NB + wave][lane];
+#pragma unroll 1
+  for (int q = 1; q < WAVES; ++q)
+#pragma unroll
+    for (int b = 0; b < CB; ++b) v[b] += sums[q][b * NB + wave][lane];
+  const int m = NB * r + wave, n = n0 + 4 * CB * lg;
+  if (m >= g.a.rows || n >= g.b.rows) return;
+  float o[4 * CB];
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int b = 0; b < CB; ++b) o[CB * q + b] = v[b][q];
+  store_run(static_cast<T *>(g.y) + (long)m * g.ldy + n, g.b.rows - n, o);
+}
+
+constexpr int FEW = 64;  // rows that k_few8 takes at most
+
+// Partial sums: rows of `outs` filled up to 16.
+long ld_part(int outs) { return (outs + 15) / 16 * 16; }
+bool sizes_ok(int32_t rows, int32_t outs, int32_t cols) {
+  return rows >= 0 && outs >= 1 && cols >= 1 && rows <= (1 << 20) && outs <= (1 << 20) && cols <= (1 << 20);
+}
+gemm::Choice choice_of(int rows, int outs, int cols) {
+  const long steps = fp8::blocks_of(cols);
+  const double elems = (double)rows * ld_part(outs);
+  return gemm::choose(gemm::tiles_of(rows, outs, 4), gemm::tiles_of(rows, outs, 2), steps, elems, 1L << 60);
+}
+
+template <class T>
+void few(const Gemm8 &g, hipStream_t st) {
+  const unsigned nb = (unsigned)((g.b.rows + 31) / 32);
+  if (g.a.rows <= 16) k_few8<1, 2, 8, T><<<nb, 64 * 8, 0, st>>>(g);
+  else if (g.a.rows <= 32) k_few8<2, 2, 8, T><<<nb, 64 * 8, 0, st>>>(g);
+  else k_few8<4, 2, 4, T><<<nb, 64 * 4, 0, st>>>(g);
+  SEG_LAUNCH_CHECK();
+}
+
+template <class T>
+void many(Gemm8 g, int tm, hipStream_t st) {
+  g.tiles = (int)gemm::tiles_of(g.a.rows, g.b.rows, tm);
+  const unsigned grid = (unsigned)(((long)g.tiles * g.splits + 7) / 8 * 8);
+  if (tm == 2) k_gemm8<2, T><<<grid, THREADS, 0, st>>>(g);
+  else k_gemm8<4, T><<<grid, THREADS, 0, st>>>(g);
+  SEG_LAUNCH_CHECK();
+}
+
+}  // namespace
+}  // namespace seg
+
+using namespace seg;
+
+extern "C" size_t seg_fp8_gemm_workspace_bytes(int32_t rows, int32_t outs, int32_t cols) {
+  if (!sizes_ok(rows, outs, cols) || rows <= FEW) return 0;
+  const gemm::Choice c = choice_of(rows, outs, cols);
+  return c.parts > 1 ? align_up((size_t)c.parts * rows * ld_part(outs) * 4) : 0;
+}
+
+extern "C" seg_status seg_fp8_gemm(int32_t rows, int32_t outs, int32_t cols, const seg_fp8 *a, const seg_fp8 *b,
+                                   seg_dtype dt, void *y, int64_t ldy, void *ws, size_t ws_bytes,
+                                   hipStream_t stream) {
+  return guarded([&] {
+    SEG_CHECK(dt == SEG_BF16 || dt == SEG_F32, SEG_ERR_UNSUPPORTED, "dtype %d not supported", (int)dt);
+    SEG_CHECK(rows >= 0 && outs >= 1 && cols >= 1, SEG_ERR_ARG, "bad sizes rows=%d outs=%d cols=%d", rows, outs, cols);
+    SEG_CHECK(sizes_ok(rows, outs, cols), SEG_ERR_CAPACITY, "rows %d, outs %d or cols %d above 2^20", rows, outs, cols);
+    SEG_CHECK(ldy >= outs && ldy < (1LL << 40), SEG_ERR_ARG, "row stride %lld of y for %d columns", (long long)ldy, outs);
+    if (rows == 0) return;
+    fp8::check(a, "a");
+    fp8::check(b, "b");
+    const size_t need = seg_fp8_gemm_workspace_bytes(rows, outs, cols), e = dt == SEG_BF16 ? 2 : 4;
+    SEG_CHECK(ws_bytes >= need, SEG_ERR_WORKSPACE, "workspace of %zu bytes < required %zu", ws_bytes, need);
+    SEG_CHECK(y && (ws || need == 0), SEG_ERR_ARG, "y or the workspace is NULL");
+    SEG_CHECK(reinterpret_cast<uintptr_t>(y) % e == 0, SEG_ERR_ARG, "y is not aligned to its type");
+    SEG_CHECK(need == 0 || reinterpret_cast<uintptr_t>(ws) % 16 == 0, SEG_ERR_UNSUPPORTED,
+              "the workspace is not on a 16-byte boundary");
+    check_apart({{y, ((size_t)(rows - 1) * ldy + outs) * e}, {need ? ws : nullptr, need}},
+                {{a->code, fp8::code_bytes(rows, cols)}, {a->exp, fp8::exp_bytes(rows, cols, a->block_rows)},
+                 {b->code, fp8::code_bytes(outs, cols)}, {b->exp, fp8::exp_bytes(outs, cols, b->block_rows)}});
+    auto operand = [&](const seg_fp8 *p, int n) {
+      return Operand{p->code, p->exp, fp8::ld_code(cols), fp8::ld_exp(n, p->block_rows), n, p->block_rows != 1};
+    };
+    Gemm8 g{operand(a, rows), operand(b, outs), y, ldy, 0, (int)fp8::blocks_of(cols), (int)fp8::blocks_of(cols), 1, 0};
+    ProfScope prof("fp8_gemm", stream);
+    if (rows <= FEW) {
+      if (dt == SEG_BF16) few<unsigned short>(g, stream);
+      else few<float>(g, stream);
+      return;
+    }
+    const gemm::Choice c = choice_of(rows, outs, cols);
+    if (c.parts == 1) {
+      if (dt == SEG_BF16) many<unsigned short>(g, c.tm, stream);
+      else many<float>(g, c.tm, stream);
+      return;
+    }
+    g.y = ws;
+    g.ldy = ld_part(outs);
+    g.split_stride = (long)rows * g.ldy;
+    g.splits = c.parts;
+    g.part = c.part;
+    many<float>(g, c.tm, stream);
+    const unsigned grid = (unsigned)std::min<long>(8192, ((long)rows * g.ldy / 8 + 255) / 256);
+    if (dt == SEG_BF16)
+      k_finish8<<<grid, 256, 0, stream>>>(static_cast<const float *>(ws), c.parts, g.split_stride, g.ldy, rows, outs,
+                                          static_cast<unsigned short *>(y), ldy);
+    else
+      k_finish8<<<grid, 256, 0, stream>>>(static_cast<const float *>(ws), c.parts, g.split_stride, g.ldy, rows, outs,
+                                          static_cast<float *>(y), ldy);
+    SEG_LAUNCH_CHECK();
+  });
+}

@@ -3,9 +3,10 @@
 Functions carry the C names (seg_layout_query, seg_build_layout, seg_attn_fwd,
 seg_attn_bwd, seg_logprob_loss, seg_layer_fwd, seg_layer_bwd, seg_mrope_positions,
 seg_mrope_fwd, seg_mrope_bwd, seg_act_pack, seg_act_unpack, seg_glu_fwd,
-seg_glu_bwd, seg_layer_fwd_ext, seg_layer_bwd_ext) and only marshal arguments: they allocate
-outputs and workspace with torch on the tensors' device and pass raw
-pointers plus torch's current stream to the library.
+seg_glu_bwd, seg_layer_fwd_ext, seg_layer_bwd_ext, seg_fp8_pack, seg_fp8_unpack,
+seg_fp8_gemm) and only marshal arguments: they allocate outputs and workspace with
+torch on the tensors' device and pass raw pointers plus torch's current stream to the
+library.
 """
 from __future__ import annotations
 
@@ -760,3 +761,97 @@ def seg_layer_bwd_ext(lay: Layout, cfg: LayerCfg, w: dict, dy, rope: Optional[Mr
             ctypes.byref(_layer_weights(w)), None if saved8 is not None else x.data_ptr(), sv,
             dy.data_ptr(), dx.data_ptr(), ctypes.byref(g), ws.data_ptr(), ws.numel(), _current(dev)))
     return dx, grads
+
+
+def _up(n: int, to: int) -> int:
+    return -(-n // to) * to
+
+
+@dataclasses.dataclass
+class Fp8:
+    """A tensor [rows, cols] in 8-bit floating point (e4m3) with a power of two for each
+    block of block_rows (1 or 128) rows x 128 columns: code [rows, cols up to 16] uint8
+    (zero codes behind cols) and exp [ceil(cols / 128), ceil(rows / block_rows) up to 16]
+    uint8, value = number(code) * 2^(exp - 127)."""
+    code: object
+    exp: object
+    cols: int
+    block_rows: int = 1
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, block_rows: int, device) -> "Fp8":
+        import torch
+        if block_rows not in (1, 128):
+            raise ValueError(f"blocks of {block_rows} rows, not of 1 or 128")
+        return cls(torch.empty((rows, _up(cols, 16)), dtype=torch.uint8, device=device),
+                   torch.empty((-(-cols // 128), _up(-(-rows // block_rows), 16)), dtype=torch.uint8, device=device),
+                   cols, block_rows)
+
+    @property
+    def shape(self):
+        return self.code.shape[0], self.cols
+
+    def c(self) -> "_lib.SegFp8":
+        import torch
+        rows, cols = self.shape
+        assert self.block_rows in (1, 128)
+        assert self.code.dtype == torch.uint8 and self.exp.dtype == torch.uint8
+        assert self.code.shape == (rows, _up(cols, 16))
+        assert self.exp.shape == (-(-cols // 128), _up(-(-rows // self.block_rows), 16))
+        assert self.code.is_contiguous() and self.exp.is_contiguous()
+        return _lib.SegFp8(self.code.data_ptr(), self.exp.data_ptr(), self.block_rows)
+
+
+def seg_fp8_pack(x, block_rows: int = 1, out: Optional[Fp8] = None) -> Fp8:
+    """x [rows, cols] (rows at any distance) in 8-bit floating point: a scale for each
+    128 columns of a row, or (block_rows = 128) of 128 rows, as weights have them."""
+    rows, cols = x.shape
+    dt = _dtype_code(x)
+    if out is None:
+        out = Fp8.empty(rows, cols, block_rows, x.device)
+    assert out.shape == (rows, cols) and out.block_rows == block_rows
+    dev = _device(x, out.code, out.exp)
+    with _on(dev):
+        check(_lib.lib().seg_fp8_pack(rows, cols, dt, x.data_ptr(), _rows(x), ctypes.byref(out.c()),
+                                      _current(dev)))
+    return out
+
+
+def seg_fp8_unpack(a: Fp8, dtype=None, x=None):
+    """The values of `a` in `dtype` (bf16 by default), or into x [rows, cols]."""
+    import torch
+    rows, cols = a.shape
+    if x is None:
+        x = torch.empty((rows, cols), dtype=dtype or torch.bfloat16, device=a.code.device)
+    assert x.shape == (rows, cols) and (dtype is None or x.dtype == dtype)
+    dev = _device(x, a.code, a.exp)
+    with _on(dev):
+        check(_lib.lib().seg_fp8_unpack(rows, cols, _dtype_code(x), ctypes.byref(a.c()), x.data_ptr(), _rows(x),
+                                        _current(dev)))
+    return x
+
+
+def fp8_gemm_workspace(rows: int, outs: int, cols: int, device):
+    import torch
+    n = _lib.lib().seg_fp8_gemm_workspace_bytes(rows, outs, cols)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def seg_fp8_gemm(a: Fp8, b: Fp8, dtype=None, y=None, ws=None):
+    """y [rows, outs] = a b^T of a [rows, cols] and b [outs, cols] in 8-bit floating point,
+    in `dtype` (bf16 by default), or into y (rows at any distance)."""
+    import torch
+    rows, cols = a.shape
+    outs = b.shape[0]
+    assert b.shape == (outs, cols), f"a has {cols} columns and b {b.shape[1]}"
+    if y is None:
+        y = torch.empty((rows, outs), dtype=dtype or torch.bfloat16, device=a.code.device)
+    assert y.shape == (rows, outs) and (dtype is None or y.dtype == dtype)
+    if ws is None:
+        ws = fp8_gemm_workspace(rows, outs, cols, y.device)
+    dev = _device(y, a.code, a.exp, b.code, b.exp, ws)
+    with _on(dev):
+        check(_lib.lib().seg_fp8_gemm(rows, outs, cols, ctypes.byref(a.c()), ctypes.byref(b.c()), _dtype_code(y),
+                                      y.data_ptr(), _rows(y), _ptr(ws), 0 if ws is None else ws.numel(),
+                                      _current(dev)))
+    return y

@@ -1,0 +1,94 @@
+"""Host-side checks of 8-bit floating point and its product (no GPU): structures,
+workspace sizes, and what each entry point refuses before any launch."""
+import ctypes
+
+import pytest
+
+from paper_2607_11185_amd import _lib
+from paper_2607_11185_amd import seg as S
+from tests.test_abi_host import _lib_or_skip
+from tests import test_abi_structs as TS
+
+ARG, CAP, WS, UNS = (_lib.SEG_ERR_ARG, _lib.SEG_ERR_CAPACITY, _lib.SEG_ERR_WORKSPACE, _lib.SEG_ERR_UNSUPPORTED)
+STRUCTS = {"seg_fp8": _lib.SegFp8}
+MB = 1 << 20
+
+
+def test_structures_match_header(tmp_path, monkeypatch):
+    monkeypatch.setattr(TS, "STRUCTS", STRUCTS)
+    TS.test_ctypes_structs_match_header(tmp_path)
+    TS.test_header_fields_all_mirrored()
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(rows=-1), ARG), (dict(cols=0), ARG), (dict(ldx=63), ARG), (dict(dt=5), UNS), (dict(x=None), ARG), (dict(p=None), ARG),
+    (dict(code=None), ARG), (dict(exp=None), ARG), (dict(x=17), ARG), (dict(x=18, dt=1), ARG), (dict(rows=1 << 41), CAP),
+    (dict(rows=1 << 35, cols=1 << 20, ldx=1 << 20), CAP), (dict(rows=1 << 34), CAP), (dict(block_rows=0), UNS),
+    (dict(block_rows=64), UNS), (dict(block_rows=-1), UNS), (dict(code=MB + 8), UNS), (dict(exp=2 * MB + 4), UNS)])
+def test_packing_refuses(kw, want):
+    L = _lib_or_skip()
+    a = dict(rows=4, cols=64, ldx=64, dt=0, x=16, p=True, code=MB, exp=2 * MB, block_rows=1)
+    a.update(kw)
+    s = _lib.SegFp8(a["code"], a["exp"], a["block_rows"])
+    p = ctypes.byref(s) if a["p"] else None
+    assert L.seg_fp8_pack(a["rows"], a["cols"], a["dt"], a["x"], a["ldx"], p, None) == want
+    assert L.seg_last_error()
+    assert L.seg_fp8_unpack(a["rows"], a["cols"], a["dt"], p, a["x"], a["ldx"], None) == want
+
+
+@pytest.mark.parametrize("x,code,exp", [(16, 16, MB), (16, MB, 16), (16, MB, 512), (MB, 16, 256), (4096, 256, 256 + 240), (256, 16, MB)])
+def test_packing_refuses_overlapping_arrays(x, code, exp):
+    """4 rows of 64 columns: 512 bytes of x, 256 of codes, 16 of exponents."""
+    L = _lib_or_skip()
+    s = _lib.SegFp8(code, exp, 1)
+    assert L.seg_fp8_pack(4, 64, 0, x, 64, ctypes.byref(s), None) == ARG
+
+
+def _gemm(rows=100, outs=40, cols=8192, dt=0, y=MB, ldy=40, ws=8 * MB, ws_bytes=1 << 40, a=(16 * MB, 32 * MB, 1),
+          b=(48 * MB, 64 * MB, 128)):
+    L = _lib_or_skip()
+    sa, sb = (None if v is None else ctypes.byref(_lib.SegFp8(*v)) for v in (a, b))
+    return L.seg_fp8_gemm(rows, outs, cols, sa, sb, dt, y, ldy, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(dt=2), UNS), (dict(rows=-1), ARG), (dict(outs=0), ARG), (dict(cols=0), ARG), (dict(rows=(1 << 20) + 1), CAP),
+    (dict(outs=(1 << 20) + 1, ldy=2 << 20), CAP), (dict(cols=(1 << 20) + 1), CAP), (dict(ldy=39), ARG), (dict(a=None), ARG), (dict(b=None), ARG),
+    (dict(a=(None, 32 * MB, 1)), ARG), (dict(b=(48 * MB, None, 128)), ARG), (dict(a=(16 * MB + 8, 32 * MB, 1)), UNS),
+    (dict(b=(48 * MB, 64 * MB + 1, 128)), UNS), (dict(b=(48 * MB, 64 * MB, 32)), UNS), (dict(ws_bytes=100), WS), (dict(ws=None), ARG),
+    (dict(ws=8 * MB + 4), UNS), (dict(y=None), ARG), (dict(y=MB + 1), ARG), (dict(y=MB + 2, dt=1), ARG),
+    (dict(y=16 * MB), ARG), (dict(y=32 * MB), ARG), (dict(y=48 * MB), ARG), (dict(y=64 * MB), ARG), (dict(y=8 * MB), ARG),
+    (dict(ws=16 * MB - 16), ARG), (dict(ws=MB), ARG), (dict(a=(MB, 32 * MB, 1)), ARG)])
+def test_product_refuses(kw, want):
+    assert _gemm(**kw) == want
+    assert _lib.lib().seg_last_error()
+
+
+def test_product_of_nothing_and_sizes():
+    L = _lib_or_skip()
+    assert _gemm(rows=0, a=None, b=None, y=None, ws=None, ws_bytes=0) == _lib.SEG_OK
+    for bad in ((-1, 4, 4), (4, 0, 4), (4, 4, 0), ((1 << 20) + 1, 4, 4)):
+        assert L.seg_fp8_gemm_workspace_bytes(*bad) == 0
+    assert L.seg_fp8_gemm_workspace_bytes(64, 40, 8192) == 0      # few rows need none
+    assert L.seg_fp8_gemm_workspace_bytes(100, 40, 8192) % (100 * 48 * 4) < 256
+
+
+def test_binding_refuses():
+    import torch
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        S.seg_fp8_pack(x, 64)
+    with pytest.raises(TypeError):
+        S.seg_fp8_pack(x.half())
+    with pytest.raises(AssertionError):                            # not on a GPU
+        S.seg_fp8_pack(x)
+    with pytest.raises(AssertionError):
+        S.seg_fp8_pack(x, 1, S.Fp8.empty(4, 65, 1, "cpu"))
+    with pytest.raises(AssertionError):
+        S.seg_fp8_pack(x, 128, S.Fp8.empty(4, 64, 1, "cpu"))
+    a, b = S.Fp8.empty(4, 64, 1, "cpu"), S.Fp8.empty(5, 65, 128, "cpu")
+    with pytest.raises(AssertionError):                            # other columns
+        S.seg_fp8_gemm(a, b)
+    bad = S.Fp8(a.code, a.exp[:, :8], 64, 1)
+    with pytest.raises(AssertionError):
+        bad.c()
