@@ -575,6 +575,21 @@ seg_status seg_fp8_gemm(int32_t rows, int32_t outs, int32_t cols, const seg_fp8 
                         size_t ws_bytes, hipStream_t stream);
 
 /*
+ * The k largest logits of each row of z [rows, vocab] (dtype dt, ldz >= vocab elements
+ * between rows), what a teacher hands to seg_distill_loss:
+ *   ids [rows, k] their columns and logits [rows, k] fp32 their values, as they are, in
+ *   descending order, equal values by ascending column (NaN counts as larger than all
+ *   numbers, -0 as 0); lse [rows] fp32 = log sum exp(scale * z) over the whole row
+ *   (-inf where all are -inf, NaN where one is NaN).
+ * 1 <= k <= vocab (SEG_ERR_ARG), k <= 256 (SEG_ERR_UNSUPPORTED), rows and vocab up to
+ * 2^20; outputs and workspace overlap neither z nor each other (SEG_ERR_ARG).
+ */
+size_t seg_top_logits_workspace_bytes(int32_t rows, int32_t vocab);
+seg_status seg_top_logits(int32_t rows, int32_t vocab, int32_t k, seg_dtype dt, const void *z,
+                          int64_t ldz, float scale, int32_t *ids, float *logits, float *lse,
+                          void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
  * Kernel timing.  While enabled, every kernel the library launches is
  * bracketed by HIP events recorded on its launch stream.  seg_profile_read sums
  * the device time of all recorded launches of one kernel (names: "layout",
@@ -582,7 +597,7 @@ seg_status seg_fp8_gemm(int32_t rows, int32_t outs, int32_t cols, const seg_fp8 
  * the dQ kernel forms Delta itself), "attn_bwd_dkdv", "attn_bwd_dq", "logits", "row_loss", "dz", "lp_prep", "dh", "dw", and for the layer
  * "ly_norm", "ly_rope", "ly_proj", "ly_mlp", "ly_wgrad", "ly_misc", "ly_act8"; "mrope_pos", "mrope", "act_pack",
  * "act_unpack", "glu_fwd", "glu_act", "glu_dx", "glu_dw", "fp8_pack", "fp8_unpack",
- * "fp8_gemm"), waiting for them to
+ * "fp8_gemm", "top_logits"), waiting for them to
  * finish; seg_profile_reset forgets the records.  Timing adds two event
  * records per launch and is off by default.  These three calls are the one
  * place with process-wide state (an atomic enable flag and a mutex-guarded

@@ -19,5 +19,6 @@ mrope      rotary positions on three axes: positions of a segment, rotation
 act8       activations in 8 bits (blocks of 32 columns, a power of two each)
 glu        gated feed-forward block, forward and backward
 fp8        8-bit floating point (blocks of 128 columns, a power of two each)
+top        the largest logits of each row, and the log-sum-exp
 """
-from . import layout, attention, loss, layer, mrope, act8, glu, fp8  # noqa: F401
+from . import layout, attention, loss, layer, mrope, act8, glu, fp8, top  # noqa: F401

@@ -31,7 +31,8 @@ EXPORTS = ["seg_layout_query", "seg_build_layout", "seg_attn_workspace_bytes", "
            "seg_glu_workspace_bytes", "seg_glu_bwd", "seg_layer_ext_workspace_bytes",
            "seg_layer_fwd_ext", "seg_layer_bwd_ext", "seg_profile_enable",
            "seg_profile_reset", "seg_profile_read", "seg_last_error",
-           "seg_fp8_pack", "seg_fp8_unpack", "seg_fp8_gemm_workspace_bytes", "seg_fp8_gemm"]
+           "seg_fp8_pack", "seg_fp8_unpack", "seg_fp8_gemm_workspace_bytes", "seg_fp8_gemm",
+           "seg_top_logits_workspace_bytes", "seg_top_logits"]
 
 P32 = ctypes.POINTER(ctypes.c_int32)
 VP = ctypes.c_void_p
@@ -216,6 +217,10 @@ def lib() -> ctypes.CDLL:
         L.seg_fp8_gemm_workspace_bytes.restype = size
         L.seg_fp8_gemm_workspace_bytes.argtypes = [i32, i32, i32]
         L.seg_fp8_gemm.argtypes = [i32, i32, i32, fp8, fp8, dtype, VP, i64, VP, size, VP]
+        L.seg_top_logits_workspace_bytes.restype = size
+        L.seg_top_logits_workspace_bytes.argtypes = [i32, i32]
+        L.seg_top_logits.restype = ctypes.c_int
+        L.seg_top_logits.argtypes = [i32, i32, i32, dtype, VP, i64, ctypes.c_float, VP, VP, VP, VP, size, VP]
         layer = [ctypes.POINTER(SegLayout), ctypes.POINTER(SegSizes), ctypes.POINTER(SegLayerCfg),
                  ctypes.POINTER(SegLayerExt), ctypes.POINTER(SegLayerWeights), VP]
         L.seg_layer_ext_workspace_bytes.restype = size

@@ -4,7 +4,7 @@ Functions carry the C names (seg_layout_query, seg_build_layout, seg_attn_fwd,
 seg_attn_bwd, seg_logprob_loss, seg_layer_fwd, seg_layer_bwd, seg_mrope_positions,
 seg_mrope_fwd, seg_mrope_bwd, seg_act_pack, seg_act_unpack, seg_glu_fwd,
 seg_glu_bwd, seg_layer_fwd_ext, seg_layer_bwd_ext, seg_fp8_pack, seg_fp8_unpack,
-seg_fp8_gemm) and only marshal arguments: they allocate outputs and workspace with
+seg_fp8_gemm, seg_top_logits) and only marshal arguments: they allocate outputs and workspace with
 torch on the tensors' device and pass raw pointers plus torch's current stream to the
 library.
 """
@@ -855,3 +855,33 @@ def seg_fp8_gemm(a: Fp8, b: Fp8, dtype=None, y=None, ws=None):
                                       y.data_ptr(), _rows(y), _ptr(ws), 0 if ws is None else ws.numel(),
                                       _current(dev)))
     return y
+
+
+def top_logits_workspace(rows: int, vocab: int, device):
+    import torch
+    n = _lib.lib().seg_top_logits_workspace_bytes(rows, vocab)
+    return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
+
+
+def seg_top_logits(z, k: int, scale: float = 1.0, out: Optional[dict] = None, ws=None) -> dict:
+    """The k largest of each row of z [rows, vocab] (rows at any distance): dict(ids
+    [rows, k] int32, logits [rows, k] fp32, both by value and then column; lse [rows]
+    fp32, the log-sum-exp of scale * z over the whole row)."""
+    import torch
+    rows, vocab = z.shape
+    dt, dev = _dtype_code(z), z.device
+    if out is None:
+        out = {"ids": torch.empty((rows, k), dtype=torch.int32, device=dev),
+               "logits": torch.empty((rows, k), dtype=torch.float32, device=dev),
+               "lse": torch.empty(rows, dtype=torch.float32, device=dev)}
+    for n, shape, dtype in (("ids", (rows, k), torch.int32), ("logits", (rows, k), torch.float32),
+                            ("lse", (rows,), torch.float32)):
+        assert out[n].shape == shape and out[n].dtype == dtype and out[n].is_contiguous(), n
+    if ws is None:
+        ws = top_logits_workspace(rows, vocab, dev)
+    _device(z, out["ids"], out["logits"], out["lse"], ws)
+    with _on(dev):
+        check(_lib.lib().seg_top_logits(rows, vocab, k, dt, z.data_ptr(), _rows(z), scale, out["ids"].data_ptr(),
+                                        out["logits"].data_ptr(), out["lse"].data_ptr(), ws.data_ptr(), ws.numel(),
+                                        _current(dev)))
+    return out
