@@ -590,6 +590,47 @@ seg_status seg_top_logits(int32_t rows, int32_t vocab, int32_t k, seg_dtype dt, 
                           void *ws, size_t ws_bytes, hipStream_t stream);
 
 /*
+ * Distillation from a teacher's top logits (a frozen model's answers at the trained
+ * rows): the divergence of the student's distribution over the vocabulary, with
+ * gradients.  Per row r, over its entries j with ids >= 0 (others are not there):
+ *   z = logit_scale h w^T, q = softmax(z) over the vocabulary;
+ *   t_j = teacher_scale * logits_j;  p = softmax(t) over the row's entries, or, where
+ *   t_lse is given (the teacher's own log-sum-exp of t over its whole vocabulary, as
+ *   seg_top_logits returns it for scale = teacher_scale), p_j = exp(t_j - t_lse);
+ *   loss_tok = row_weight * sum_j p_j (log p_j - log q(ids_j)), terms with p_j = 0
+ *   being 0; loss_sum = loss_scale * sum(loss_tok);
+ *   d loss_sum / d z_v = loss_scale row_weight (q_v sum_j p_j - sum_{ids_j = v} p_j).
+ * A temperature T is logit_scale = teacher_scale = 1 / T (and T^2 in loss_scale).
+ *   h [n_h, hidden], w [vocab, hidden] (dtype dt); row_index [rows] or NULL as for
+ *   seg_logprob_loss (a row whose index is not in [0, n_h) is NaN); ids, logits [rows, k];
+ *   t_lse, row_weight [rows] fp32, or NULL (row_weight: 1).
+ * A row with weight 0 or no probability at any entry has loss 0 and no gradient, whatever
+ * h, ids and logits hold there; an id of vocab or more makes its row NaN; the same id more than
+ * once counts as often as it is there.
+ * Outputs: loss_tok, lse [rows] fp32 (log sum exp z); loss_sum [1] fp32; with want_grad dh
+ * [rows, hidden] (dtype dt) and dw [vocab, hidden] (dtype dw_dt), overwritten.  dz is
+ * rounded to bf16 (2^-8) for the products, as in seg_logprob_loss.
+ * hidden a multiple of 8, k <= 256 (SEG_ERR_UNSUPPORTED), all sizes below 2^20 - 256; a
+ * bf16 w and the workspace on 16-byte boundaries; outputs and workspace overlap neither
+ * an input nor each other (SEG_ERR_ARG).
+ */
+typedef struct {
+  float logit_scale;
+  float teacher_scale;
+  float loss_scale;
+  int32_t want_grad; /* 0: forward only (dh and dw untouched, may be NULL) */
+} seg_distill_cfg;
+
+size_t seg_distill_workspace_bytes(int32_t rows, int32_t hidden, int32_t vocab, int32_t k,
+                                   seg_dtype dt, int32_t want_grad);
+seg_status seg_distill_loss(int32_t rows, int32_t hidden, int32_t vocab, int32_t k, seg_dtype dt,
+                            int32_t n_h, const void *h, const int32_t *row_index, const void *w,
+                            const int32_t *ids, const float *logits, const float *t_lse,
+                            const float *row_weight, const seg_distill_cfg *cfg, float *loss_tok,
+                            float *lse, float *loss_sum, void *dh, seg_dtype dw_dt, void *dw,
+                            void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
  * Kernel timing.  While enabled, every kernel the library launches is
  * bracketed by HIP events recorded on its launch stream.  seg_profile_read sums
  * the device time of all recorded launches of one kernel (names: "layout",
@@ -597,7 +638,7 @@ seg_status seg_top_logits(int32_t rows, int32_t vocab, int32_t k, seg_dtype dt, 
  * the dQ kernel forms Delta itself), "attn_bwd_dkdv", "attn_bwd_dq", "logits", "row_loss", "dz", "lp_prep", "dh", "dw", and for the layer
  * "ly_norm", "ly_rope", "ly_proj", "ly_mlp", "ly_wgrad", "ly_misc", "ly_act8"; "mrope_pos", "mrope", "act_pack",
  * "act_unpack", "glu_fwd", "glu_act", "glu_dx", "glu_dw", "fp8_pack", "fp8_unpack",
- * "fp8_gemm", "top_logits"), waiting for them to
+ * "fp8_gemm", "top_logits", "distill"), waiting for them to
  * finish; seg_profile_reset forgets the records.  Timing adds two event
  * records per launch and is off by default.  These three calls are the one
  * place with process-wide state (an atomic enable flag and a mutex-guarded

@@ -20,5 +20,6 @@ act8       activations in 8 bits (blocks of 32 columns, a power of two each)
 glu        gated feed-forward block, forward and backward
 fp8        8-bit floating point (blocks of 128 columns, a power of two each)
 top        the largest logits of each row, and the log-sum-exp
+distill    distillation from a teacher's top logits, with gradients
 """
-from . import layout, attention, loss, layer, mrope, act8, glu, fp8, top  # noqa: F401
+from . import layout, attention, loss, layer, mrope, act8, glu, fp8, top, distill  # noqa: F401

@@ -32,7 +32,8 @@ EXPORTS = ["seg_layout_query", "seg_build_layout", "seg_attn_workspace_bytes", "
            "seg_layer_fwd_ext", "seg_layer_bwd_ext", "seg_profile_enable",
            "seg_profile_reset", "seg_profile_read", "seg_last_error",
            "seg_fp8_pack", "seg_fp8_unpack", "seg_fp8_gemm_workspace_bytes", "seg_fp8_gemm",
-           "seg_top_logits_workspace_bytes", "seg_top_logits"]
+           "seg_top_logits_workspace_bytes", "seg_top_logits",
+           "seg_distill_workspace_bytes", "seg_distill_loss"]
 
 P32 = ctypes.POINTER(ctypes.c_int32)
 VP = ctypes.c_void_p
@@ -110,6 +111,11 @@ class SegAct8(ctypes.Structure):
 
 class SegFp8(ctypes.Structure):
     _fields_ = [("code", VP), ("exp", VP), ("block_rows", ctypes.c_int32)]
+
+
+class SegDistillCfg(ctypes.Structure):
+    _fields_ = [("logit_scale", ctypes.c_float), ("teacher_scale", ctypes.c_float),
+                ("loss_scale", ctypes.c_float), ("want_grad", ctypes.c_int32)]
 
 
 SAVED8 = ("x", "y1", "q", "o", "k", "v", "g", "u")
@@ -221,6 +227,13 @@ def lib() -> ctypes.CDLL:
         L.seg_top_logits_workspace_bytes.argtypes = [i32, i32]
         L.seg_top_logits.restype = ctypes.c_int
         L.seg_top_logits.argtypes = [i32, i32, i32, dtype, VP, i64, ctypes.c_float, VP, VP, VP, VP, size, VP]
+        L.seg_distill_workspace_bytes.restype = size
+        L.seg_distill_workspace_bytes.argtypes = [i32, i32, i32, i32, dtype, i32]
+        L.seg_distill_loss.restype = ctypes.c_int
+        # rows, hidden, vocab, k, dt, n_h, h, row_index, w, ids, logits, t_lse, row_weight, cfg,
+        # loss_tok, lse, loss_sum, dh, dw_dt, dw, ws, ws_bytes, stream
+        L.seg_distill_loss.argtypes = [i32, i32, i32, i32, dtype, i32, VP, VP, VP, VP, VP, VP, VP,
+                                       ctypes.POINTER(SegDistillCfg), VP, VP, VP, VP, dtype, VP, VP, size, VP]
         layer = [ctypes.POINTER(SegLayout), ctypes.POINTER(SegSizes), ctypes.POINTER(SegLayerCfg),
                  ctypes.POINTER(SegLayerExt), ctypes.POINTER(SegLayerWeights), VP]
         L.seg_layer_ext_workspace_bytes.restype = size

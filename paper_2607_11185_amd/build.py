@@ -13,7 +13,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libseg.so")
 SOURCES = ["seg_layout.hip", "seg_attn.hip", "seg_logprob.hip", "seg_layer.hip",
            "seg_mrope.hip", "seg_act.hip", "seg_glu.hip", "seg_fp8.hip", "seg_fp8_gemm.hip", "seg_top.hip",
-           "seg_profile.hip"]
+           "seg_distill.hip", "seg_profile.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -4,9 +4,9 @@ Functions carry the C names (seg_layout_query, seg_build_layout, seg_attn_fwd,
 seg_attn_bwd, seg_logprob_loss, seg_layer_fwd, seg_layer_bwd, seg_mrope_positions,
 seg_mrope_fwd, seg_mrope_bwd, seg_act_pack, seg_act_unpack, seg_glu_fwd,
 seg_glu_bwd, seg_layer_fwd_ext, seg_layer_bwd_ext, seg_fp8_pack, seg_fp8_unpack,
-seg_fp8_gemm, seg_top_logits) and only marshal arguments: they allocate outputs and workspace with
-torch on the tensors' device and pass raw pointers plus torch's current stream to the
-library.
+seg_fp8_gemm, seg_top_logits, seg_distill_loss) and only marshal arguments: they
+allocate outputs and workspace with torch on the tensors' device and pass raw pointers
+plus torch's current stream to the library.
 """
 from __future__ import annotations
 
@@ -884,4 +884,66 @@ def seg_top_logits(z, k: int, scale: float = 1.0, out: Optional[dict] = None, ws
         check(_lib.lib().seg_top_logits(rows, vocab, k, dt, z.data_ptr(), _rows(z), scale, out["ids"].data_ptr(),
                                         out["logits"].data_ptr(), out["lse"].data_ptr(), ws.data_ptr(), ws.numel(),
                                         _current(dev)))
+    return out
+
+
+@dataclasses.dataclass
+class DistillCfg:
+    """Settings of the distillation loss (seg_distill_cfg)."""
+    logit_scale: float = 1.0
+    teacher_scale: float = 1.0
+    loss_scale: float = 1.0
+    want_grad: bool = True
+
+    def c(self) -> "_lib.SegDistillCfg":
+        return _lib.SegDistillCfg(self.logit_scale, self.teacher_scale, self.loss_scale, int(self.want_grad))
+
+
+def distill_workspace(rows: int, hidden: int, vocab: int, k: int, dt: int, want_grad: bool, device):
+    import torch
+    n = _lib.lib().seg_distill_workspace_bytes(rows, hidden, vocab, k, dt, int(want_grad))
+    return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
+
+
+def seg_distill_loss(h, row_index, w, ids, logits, cfg: DistillCfg, t_lse=None, row_weight=None,
+                     dw_dtype=None, out: Optional[dict] = None, ws=None) -> dict:
+    """Divergence of the student's distribution from a teacher's top logits, with
+    gradients when cfg.want_grad.
+
+    h [n_h, H]; row_index [R] int32 or None; w [V, H]; ids [R, k] int32 (negative: no
+    entry) and logits [R, k] fp32, as seg_top_logits returns them; t_lse [R] fp32 or None
+    (the teacher's probabilities are then normalised over the entries); row_weight [R]
+    fp32 or None.  Returns dict(loss_tok, lse, loss_sum, dh, dw): dw in dw_dtype (fp32 by
+    default), dh and dw None without want_grad.
+    """
+    import torch
+    dev = h.device
+    (n_h, H), (R, k), V = h.shape, ids.shape, w.shape[0]
+    dt = _dtype_code(h)
+    assert w.shape == (V, H) and w.dtype == h.dtype and h.is_contiguous() and w.is_contiguous()
+    assert ids.dtype == torch.int32 and ids.is_contiguous()
+    assert row_index is None or (row_index.shape == (R,) and row_index.dtype == torch.int32 and row_index.is_contiguous())
+    assert logits.shape == (R, k) and logits.dtype == torch.float32 and logits.is_contiguous()
+    for t in (t_lse, row_weight):
+        assert t is None or (t.shape == (R,) and t.dtype == torch.float32 and t.is_contiguous())
+    if out is None:
+        f32 = dict(dtype=torch.float32, device=dev)
+        out = {"loss_tok": torch.empty(R, **f32), "lse": torch.empty(R, **f32), "loss_sum": torch.empty(1, **f32),
+               "dh": torch.empty((R, H), dtype=h.dtype, device=dev) if cfg.want_grad else None,
+               "dw": torch.empty((V, H), dtype=dw_dtype or torch.float32, device=dev) if cfg.want_grad else None}
+    for n, shape in (("loss_tok", (R,)), ("lse", (R,)), ("loss_sum", (1,))):
+        assert out[n].shape == shape and out[n].dtype == torch.float32 and out[n].is_contiguous(), n
+    dh, dw = out.get("dh"), out.get("dw")
+    if cfg.want_grad:
+        assert dh.shape == (R, H) and dh.dtype == h.dtype and dh.is_contiguous()
+        assert dw.shape == (V, H) and dw.is_contiguous() and (dw_dtype is None or dw.dtype == dw_dtype)
+    if ws is None:
+        ws = distill_workspace(R, H, V, k, dt, cfg.want_grad, dev)
+    _device(h, w, ids, logits, row_index, t_lse, row_weight, dh, dw, ws, *(out[n] for n in ("loss_tok", "lse", "loss_sum")))
+    with _on(dev):
+        check(_lib.lib().seg_distill_loss(
+            R, H, V, k, dt, n_h, h.data_ptr(), _ptr(row_index), w.data_ptr(), ids.data_ptr(), logits.data_ptr(),
+            _ptr(t_lse), _ptr(row_weight), ctypes.byref(cfg.c()), out["loss_tok"].data_ptr(), out["lse"].data_ptr(),
+            out["loss_sum"].data_ptr(), _ptr(dh), _dtype_code(dw) if cfg.want_grad else 0, _ptr(dw), ws.data_ptr(),
+            ws.numel(), _current(dev)))
     return out

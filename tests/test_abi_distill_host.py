@@ -10,7 +10,7 @@ from tests.test_abi_host import _lib_or_skip
 from tests import test_abi_structs as TS
 
 ARG, CAP, WS, UNS = (_lib.SEG_ERR_ARG, _lib.SEG_ERR_CAPACITY, _lib.SEG_ERR_WORKSPACE, _lib.SEG_ERR_UNSUPPORTED)
-STRUCTS = {"seg_fp8": _lib.SegFp8}
+STRUCTS = {"seg_fp8": _lib.SegFp8, "seg_distill_cfg": _lib.SegDistillCfg}
 MB = 1 << 20
 
 
@@ -119,3 +119,52 @@ def test_top_logits_of_nothing_and_sizes():
     for bad in ((-1, 4), (4, 0), ((1 << 20) + 1, 4), (4, (1 << 20) + 1)):
         assert L.seg_top_logits_workspace_bytes(*bad) == 0
     assert L.seg_top_logits_workspace_bytes(1, 1) > 0
+
+
+# -------------------------------------------------------------- distillation
+
+def _distill(rows=40, hidden=64, vocab=1000, k=10, dt=0, n_h=40, h=MB, row_index=None, w=2 * MB, ids=3 * MB, logits=4 * MB,
+             t_lse=None, weight=None, cfg=(1.0, 1.0, 1.0, 1), loss_tok=5 * MB, lse=6 * MB, loss_sum=7 * MB, dh=8 * MB, dw_dt=0,
+             dw=9 * MB, ws=64 * MB, ws_bytes=1 << 40):
+    c = None if cfg is None else ctypes.byref(_lib.SegDistillCfg(*cfg))
+    return _lib_or_skip().seg_distill_loss(rows, hidden, vocab, k, dt, n_h, h, row_index, w, ids, logits, t_lse, weight, c, loss_tok,
+                                           lse, loss_sum, dh, dw_dt, dw, ws, ws_bytes, None)
+
+
+INF = float("inf")
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(cfg=None), ARG), (dict(dt=2), ARG), (dict(dw_dt=2), ARG), (dict(rows=-1), ARG), (dict(hidden=0), ARG), (dict(vocab=0), ARG),
+    (dict(n_h=-1), ARG), (dict(k=0), ARG), (dict(k=1001), ARG), (dict(k=257), UNS), (dict(hidden=60), UNS), (dict(rows=1 << 20, n_h=1 << 20), CAP),
+    (dict(vocab=1 << 20), CAP), (dict(hidden=(1 << 20) + 8), CAP), (dict(cfg=(INF, 1, 1, 1)), ARG), (dict(cfg=(1, float("nan"), 1, 1)), ARG),
+    (dict(cfg=(1, 1, -INF, 1)), ARG), (dict(n_h=39), ARG), (dict(ws_bytes=1000), WS), (dict(h=None), ARG), (dict(w=None), ARG),
+    (dict(ids=None), ARG), (dict(logits=None), ARG), (dict(loss_tok=None), ARG), (dict(lse=None), ARG), (dict(loss_sum=None), ARG),
+    (dict(dh=None), ARG), (dict(dw=None), ARG), (dict(ws=None), ARG), (dict(h=MB + 1), ARG), (dict(dh=8 * MB + 1), ARG), (dict(dw=9 * MB + 2, dw_dt=1), ARG),
+    (dict(w=2 * MB + 8), UNS), (dict(ws=64 * MB + 8), UNS), (dict(dw=2 * MB), ARG), (dict(dh=MB + 5118), ARG), (dict(loss_tok=3 * MB), ARG),
+    (dict(lse=5 * MB + 156), ARG), (dict(loss_sum=4 * MB), ARG), (dict(ws=9 * MB), ARG), (dict(dh=9 * MB), ARG), (dict(t_lse=6 * MB), ARG),
+    (dict(weight=5 * MB), ARG), (dict(row_index=8 * MB), ARG)])
+def test_distillation_refuses(kw, want):
+    assert _distill(**kw) == want
+    assert _lib.lib().seg_last_error()
+
+
+def test_distillation_sizes():
+    L = _lib_or_skip()
+    for bad in ((-1, 64, 1000, 10), (4, 0, 1000, 10), (4, 64, 0, 10), (4, 64, 1000, 0), (4, 64, 1000, 257), (1 << 20, 64, 1000, 10)):
+        assert L.seg_distill_workspace_bytes(*bad, 0, 1) == 0
+    a, b = (L.seg_distill_workspace_bytes(40, 64, 1000, 10, 0, g) for g in (0, 1))
+    assert 0 < a < b < L.seg_distill_workspace_bytes(40, 64, 1000, 10, 1, 1)
+    assert _distill(rows=0, n_h=0, dw=None) == ARG and _distill(ws_bytes=b - 1) == WS
+
+
+def test_distillation_binding_refuses():
+    import torch
+    h, w = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(30, 64, dtype=torch.bfloat16)
+    ids, logits = torch.zeros(4, 5, dtype=torch.int32), torch.zeros(4, 5)
+    good = dict(h=h, row_index=None, w=w, ids=ids, logits=logits, cfg=S.DistillCfg())
+    for bad in (dict(w=w[:, :32]), dict(w=w.float()), dict(ids=ids.long()), dict(logits=logits[:, :4]), dict(logits=logits.double()),
+                dict(row_index=torch.zeros(4, dtype=torch.int64)), dict(row_index=torch.zeros(3, dtype=torch.int32)),
+                dict(t_lse=torch.zeros(3)), dict(row_weight=torch.zeros(4, 1)), dict(dw_dtype=torch.float16), dict()):
+        with pytest.raises((AssertionError, TypeError)):
+            S.seg_distill_loss(**{**good, **bad})
