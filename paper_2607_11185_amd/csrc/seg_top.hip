@@ -16,6 +16,7 @@
 #include <cmath>
 #include <type_traits>
 
+#include "act8.h"
 #include "common.h"
 
 namespace seg {
@@ -72,141 +73,216 @@ __device__ __forceinline__ float2 meet(float2 a, float2 b) {
 }
 
 // A block takes `span` columns of a row, a lane 8 neighbouring ones at a time, so 8
-// lanes a group.  The maximum in front of the sum stays inside fp32's numbers, so that
-// infinities meet no infinity: -inf adds 0, inf gives inf, NaN stays NaN.
-template <class T>
-__global__ void __launch_bounds__(256) k_top_scan(const TopArgs a) {
-  __shared__ float2 red[4];
-  const int row = blockIdx.x / (unsigned)a.parts, part = blockIdx.x - row * (unsigned)a.parts;
-  const T *z = static_cast<const T *>(a.z) + (long)row * a.ldz;
-  const int c0 = part * a.span, c1 = min(a.vocab, c0 + a.span);
+// lanes a group.  The reference in front of the sum is the largest value so far, kept
+// inside fp32's numbers, so that infinities meet no infinity: -inf adds 0, inf gives inf,
+// NaN stays NaN.  Bound by the vector units and HBM about alike (7,680 x 151,936 bf16): nine
+// issue slots an element, four of them the exponential; whole numbers are formed of a
+// lane's largest value only, and NaN looked for two values at a time.
+template <class T, bool STREAM>
+__device__ __forceinline__ float2 scan(const TopArgs &a, const T *__restrict__ z, int c0, int c1, unsigned *gmax,
+                                       float2 (&red)[4]) {
   float2 s = make_float2(-FAR, 0.f);
-  constexpr int U = 4;
-  auto step = [&](int first, auto whole) __attribute__((always_inline)) {
+  // U pieces of 2,048 columns; WHOLE: all of them are there
+  auto step = [&](int first, auto pieces, auto whole) __attribute__((always_inline)) {
+    constexpr int U = decltype(pieces)::value;
     constexpr bool WHOLE = decltype(whole)::value;
     const int c = first + threadIdx.x * 8;
     typename Piece<T>::X v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = c + 2048 * u;
-      if (WHOLE || at + 8 <= c1) v[u] = *reinterpret_cast<const typename Piece<T>::X *>(z + at);
-      else
+      if (WHOLE || at + 8 <= c1) {
+        const typename Piece<T>::X *p = reinterpret_cast<const typename Piece<T>::X *>(z + at);
+        v[u] = STREAM ? __builtin_nontemporal_load(p) : *p;
+      } else
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[u][j] = at + j < c1 ? z[at + j] : T();
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = c + 2048 * u;
-      float y[8], m = s.x;
-      unsigned top = 0;
+      float x[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool in = WHOLE || at + j < c1;
-        const float x = value<T>(v[u][j]);
-        top = max(top, in ? order(x) : 0u);
-        y[j] = in ? x * a.scale : -INFINITY;
-        m = fmaxf(m, y[j]);
+      for (int j = 0; j < 8; ++j) x[j] = value<T>(v[u][j]);
+      auto in = [&](int j) { return WHOLE || at + j < c1; };
+      float most = -INFINITY, m;
+      bool nan = false;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) most = in(j) ? fmaxf(most, x[j]) : most;
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) nan = nan || __builtin_isunordered(x[j], x[j + 1]);
+      if (a.scale >= 0.f) {
+        m = most * a.scale;
+      } else {
+        float least = INFINITY;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) least = in(j) ? fminf(least, x[j]) : least;
+        m = least * a.scale;
       }
-      m = fminf(m, FAR);
+      m = fminf(fmaxf(s.x, m), FAR);
       s.y *= exp_of(s.x - m);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s.y += exp_of(y[j] - m);
+      for (int j = 0; j < 8; ++j) {
+        const float e = exp_of(fmaf(x[j], a.scale, -m));
+        s.y += in(j) ? e : 0.f;
+      }
       s.x = m;
-      top = max(top, (unsigned)__shfl_xor((int)top, 1, 64));
-      top = max(top, (unsigned)__shfl_xor((int)top, 2, 64));
-      top = max(top, (unsigned)__shfl_xor((int)top, 4, 64));
-      if ((threadIdx.x & 7) == 0 && (WHOLE || at < c1)) a.gmax[(long)row * a.groups + at / GROUP] = top;
+      const unsigned top = act8::max8(WHOLE || at < c1 ? (nan ? 0xffffffffu : order(most)) : 0u);
+      if ((threadIdx.x & 7) == 0 && (WHOLE || at < c1)) gmax[at / GROUP] = top;
     }
   };
   int first = c0;
-  for (; first + 2048 * U <= c1; first += 2048 * U) step(first, std::true_type());
-  if (first < c1) step(first, std::false_type());
+  typedef std::integral_constant<int, 4> Four;
+  typedef std::integral_constant<int, 1> One;
+  for (; first + 4 * 2048 <= c1; first += 4 * 2048) step(first, Four(), std::true_type());
+  if (first + 2048 < c1) step(first, Four(), std::false_type());
+  else if (first < c1) step(first, One(), std::false_type());
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) s = meet(s, make_float2(__shfl_xor(s.x, o, 64), __shfl_xor(s.y, o, 64)));
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0)
-    a.stats[(long)row * a.parts + part] = meet(meet(red[0], red[1]), meet(red[2], red[3]));
+  return meet(meet(red[0], red[1]), meet(red[2], red[3]));
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) k_top_scan(const TopArgs a) {
+  __shared__ float2 red[4];
+  const int row = blockIdx.x / (unsigned)a.parts, part = blockIdx.x - row * (unsigned)a.parts;
+  const int c0 = part * a.span;
+  const float2 s = scan<T, false>(a, static_cast<const T *>(a.z) + (long)row * a.ldz, c0, min(a.vocab, c0 + a.span),
+                                  a.gmax + (long)row * a.groups, red);
+  if (threadIdx.x == 0) a.stats[(long)row * a.parts + part] = s;
 }
 
 typedef unsigned long long u64;
 
-// The threshold t such that exactly `want` (at least 1, at most all) of the block's keys
-// are >= t; keys are distinct and none is 0.  keys(f) calls f(key) for every key of the thread.  8 bits of the
-// key a pass, from bit `shift` on down; ends early where a digit's keys are wanted whole.
+// What a block's threads share to find a threshold.
 struct Pick {
   unsigned hist[256];
-  unsigned wave[4];
-  u64 prefix;
-  unsigned want, done;
+  unsigned wave[16];
+  unsigned least, most, digit, want, done;
 };
 
-template <class K>
-__device__ __forceinline__ u64 threshold(K &&keys, unsigned want, Pick &p) {
-  u64 prefix = 0;
-  for (int shift = 56; shift >= 0; shift -= 8) {
-    p.hist[threadIdx.x] = 0;
+// The threshold t such that exactly `want` (at least 1, at most all) of the numbers of the
+// block are >= t, or, where that cuts equal ones, the number t that is cut, with how many of
+// the equal ones are wanted.  each(f) calls f(number) for every one of the thread.  The
+// numbers between the least and the most that may still be t are counted in up to 256 equal
+// ranges, and the range that holds t is the next to be cut: two or three times for values of
+// one size, four at most (digits of the bits from the top down would meet values of one
+// exponent in one or two counters first).
+struct Cut {
+  unsigned t, want;  // want: of the numbers equal to t; 0: all that are >= t
+};
+template <int THREADS, class K>
+__device__ __forceinline__ Cut threshold(K &&each, unsigned want, Pick &p) {
+  unsigned lo = 0xffffffffu, hi = 0;
+  each([&](unsigned x) {
+    lo = min(lo, x);
+    hi = max(hi, x);
+  });
+  if (threadIdx.x == 0) {
+    p.least = 0xffffffffu;
+    p.most = 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    lo = min(lo, (unsigned)__shfl_xor((int)lo, o, 64));
+    hi = max(hi, (unsigned)__shfl_xor((int)hi, o, 64));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    atomicMin(&p.least, lo);
+    atomicMax(&p.most, hi);
+  }
+  __syncthreads();
+  lo = p.least;
+  hi = p.most;
+  while (lo < hi) {
+    const int shift = max(0, 24 - (int)__builtin_clz(hi - lo));  // (hi - lo) >> shift is at most 255
+    for (int i = threadIdx.x; i < 256; i += THREADS) p.hist[i] = 0;
     __syncthreads();
-    keys([&](u64 key) {
-      if (shift == 56 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&p.hist[(key >> shift) & 255], 1u);
+    each([&](unsigned x) {
+      if (x >= lo && x <= hi) atomicAdd(&p.hist[(x - lo) >> shift], 1u);
     });
     __syncthreads();
-    // keys with a digit >= that of the thread
-    const unsigned own = p.hist[threadIdx.x];
-    unsigned n = own;
+    if (threadIdx.x < 256) {  // numbers in the thread's range and those above it
+      const unsigned own = p.hist[threadIdx.x];
+      unsigned n = own;
 #pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      const unsigned t = __shfl_down(n, o, 64);
-      if ((threadIdx.x & 63) + o < 64) n += t;
-    }
-    if ((threadIdx.x & 63) == 0) p.wave[threadIdx.x >> 6] = n;
-    __syncthreads();
-    for (int w = (threadIdx.x >> 6) + 1; w < 4; ++w) n += p.wave[w];
-    if (n >= want && n - own < want) {
-      p.prefix = prefix | (u64)threadIdx.x << shift;
-      p.want = want - (n - own);
-      p.done = n == want;
+      for (int o = 1; o < 64; o *= 2) {
+        const unsigned t = __shfl_down(n, o, 64);
+        if ((threadIdx.x & 63) + o < 64) n += t;
+      }
+      if ((threadIdx.x & 63) == 0) p.wave[threadIdx.x >> 6] = n;
+      p.hist[threadIdx.x] = n;
     }
     __syncthreads();
-    prefix = p.prefix;
+    if (threadIdx.x < 256) {
+      unsigned n = p.hist[threadIdx.x];
+      unsigned next = (threadIdx.x & 63) < 63 ? p.hist[threadIdx.x + 1] : 0;
+      for (int w = (threadIdx.x >> 6) + 1; w < 4; ++w) {
+        n += p.wave[w];
+        next += p.wave[w];
+      }
+      if (n >= want && next < want) {
+        p.digit = threadIdx.x;
+        p.want = want - next;
+        p.done = n == want;
+      }
+    }
+    __syncthreads();
+    lo += p.digit << shift;
+    hi = lo + min(hi - lo, (1u << shift) - 1);
     want = p.want;
     const bool done = p.done;
     __syncthreads();
-    if (done) break;
+    if (done) return Cut{lo, 0};
   }
-  return prefix;
+  return Cut{lo, want};
 }
 
-// A block a row.
-constexpr int CANDS = 1024;
+// The selection from the groups' numbers, `key` of group threadIdx.x + THREADS i.  They, and
+// every pass over them, stay in registers: from memory a pass cost a latency (7,680 rows,
+// k = 64: 212 us).
+constexpr int CANDS = 1024, PER = 16, COLS = 8;
 
-template <class T>
-__global__ void __launch_bounds__(256) k_top_pick(const TopArgs a) {
-  __shared__ Pick pick;
-  __shared__ u64 cand[CANDS];
-  __shared__ int group[MAX_K];
-  __shared__ unsigned count, low;
-  const int row = blockIdx.x;
-  const T *z = static_cast<const T *>(a.z) + (long)row * a.ldz;
-  const unsigned *gm = a.gmax + (long)row * a.groups;
+struct Pool {
+  Pick pick;
+  u64 cand[CANDS];
+  int group[MAX_K];
+  unsigned count, low;
+};
+
+template <class T, int THREADS>
+__device__ __forceinline__ void pick_row(const TopArgs &a, int row, const T *__restrict__ z, const unsigned (&key)[PER],
+                                         Pool &p) {
+  Pick &pick = p.pick;
+  u64(&cand)[CANDS] = p.cand;
+  int(&group)[MAX_K] = p.group;
+  unsigned &count = p.count, &low = p.low;
   if (threadIdx.x == 0) {
-    float2 s = a.stats[(long)row * a.parts];
-    for (int i = 1; i < a.parts; ++i) s = meet(s, a.stats[(long)row * a.parts + i]);
-    a.lse[row] = s.x + log2f(s.y) * LN2;
     count = 0;
     low = 0xffffffffu;
   }
   __syncthreads();
-  // the groups: value, then the first ones
+  // the groups: by value, then the first ones
   const int ng = min(a.k, a.groups);
   auto groups = [&](auto f) __attribute__((always_inline)) {
-    for (int i = threadIdx.x; i < a.groups; i += 256) f((u64)gm[i] << 32 | (unsigned)~i);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (key[i]) f(key[i], threadIdx.x + THREADS * i);
   };
-  const u64 tg = ng < a.groups ? threshold(groups, ng, pick) : 0;
-  groups([&](u64 key) {
-    if (key >= tg) {
-      group[atomicAdd(&count, 1u)] = (int)~(unsigned)key;
-      atomicMin(&low, (unsigned)(key >> 32));
+  Cut c{0, 0}, ci{0, 0};
+  if (ng < a.groups) {
+    c = threshold<THREADS>([&](auto f) __attribute__((always_inline)) { groups([&](unsigned x, int) { f(x); }); }, ng, pick);
+    if (c.want)
+      ci = threshold<THREADS>(
+          [&](auto f) __attribute__((always_inline)) { groups([&](unsigned x, int g) { if (x == c.t) f(~(unsigned)g); }); }, c.want, pick);
+  }
+  groups([&](unsigned x, int g) {
+    if (x > c.t || (x == c.t && (!c.want || ~(unsigned)g >= ci.t))) {
+      group[atomicAdd(&count, 1u)] = g;
+      atomicMin(&low, x);
     }
   });
   __syncthreads();
@@ -216,42 +292,119 @@ __global__ void __launch_bounds__(256) k_top_pick(const TopArgs a) {
   __syncthreads();
   if (threadIdx.x == 0) count = 0;
   __syncthreads();
+  // 8 columns a piece, 8 pieces a group
   auto columns = [&](auto f) __attribute__((always_inline)) {
-    for (int i = threadIdx.x; i < ng * GROUP; i += 256) {
-      const int c = group[i / GROUP] * GROUP + i % GROUP;
-      if (c >= a.vocab) continue;
-      const unsigned o = order(value<T>(z[c]));
-      if (o >= least) f((u64)o << 32 | (unsigned)~c);
+    for (int i = threadIdx.x; i < ng * (GROUP / COLS); i += THREADS) {
+      const int c0 = group[i / (GROUP / COLS)] * GROUP + i % (GROUP / COLS) * COLS;
+      typename Piece<T>::X v{};
+      if (c0 + COLS <= a.vocab) v = *reinterpret_cast<const typename Piece<T>::X *>(z + c0);
+      else
+#pragma unroll
+        for (int j = 0; j < COLS; ++j)
+          if (c0 + j < a.vocab) v[j] = z[c0 + j];
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) {
+        const unsigned o = order(value<T>(v[j]));
+        if (c0 + j < a.vocab && o >= least) f(o, c0 + j);
+      }
     }
   };
-  columns([&](u64 key) {
+  columns([&](unsigned x, int at) {
     const unsigned n = atomicAdd(&count, 1u);
-    if (n < CANDS) cand[n] = key;
+    if (n < CANDS) cand[n] = (u64)x << 32 | (unsigned)~at;
   });
   __syncthreads();
   int n = (int)count;
-  if (n > CANDS) {  // many of the same value: the k first by their own threshold
+  if (n > CANDS) {  // many of the same value: the k first by a threshold of their own
     __syncthreads();
-    const u64 t = threshold(columns, a.k, pick);
+    const Cut t = threshold<THREADS>([&](auto f) __attribute__((always_inline)) { columns([&](unsigned x, int) { f(x); }); }, a.k, pick);
+    Cut ti{0, 0};
+    if (t.want)
+      ti = threshold<THREADS>(
+          [&](auto f) __attribute__((always_inline)) { columns([&](unsigned x, int at) { if (x == t.t) f(~(unsigned)at); }); }, t.want, pick);
     if (threadIdx.x == 0) count = 0;
     __syncthreads();
-    columns([&](u64 key) {
-      if (key >= t) cand[atomicAdd(&count, 1u)] = key;
+    columns([&](unsigned x, int at) {
+      if (x > t.t || (x == t.t && (!t.want || ~(unsigned)at >= ti.t)))
+        cand[atomicAdd(&count, 1u)] = (u64)x << 32 | (unsigned)~at;
     });
     __syncthreads();
     n = a.k;
   }
   // each candidate's place is the number of those in front of it
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const u64 key = cand[i];
+  for (int i = threadIdx.x; i < n; i += THREADS) {
+    const u64 own = cand[i];
+    const int c0 = (int)~(unsigned)own;
+    const T v = z[c0];
     int at = 0;
-    for (int j = 0; j < n; ++j) at += cand[j] > key;
+    for (int j = 0; j < n; ++j) at += cand[j] > own;
     if (at < a.k) {
-      const int c = (int)~(unsigned)key;
-      a.ids[(long)row * a.k + at] = c;
-      a.logits[(long)row * a.k + at] = value<T>(z[c]);
+      a.ids[(long)row * a.k + at] = c0;
+      a.logits[(long)row * a.k + at] = value<T>(v);
     }
   }
+}
+
+// A block a row, behind the scan.
+template <class T, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_top_pick(const TopArgs a) {
+  __shared__ Pool pool;
+  const int row = blockIdx.x;
+  const unsigned *gm = a.gmax + (long)row * a.groups;
+  unsigned key[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int g = threadIdx.x + THREADS * i;
+    key[i] = g < a.groups ? gm[g] : 0;  // (0 is below every value's number)
+  }
+  if (threadIdx.x < 64) {  // the parts' sums, each lane's in order and then the lanes'
+    float2 s = make_float2(-FAR, 0.f);
+    for (int i = threadIdx.x; i < a.parts; i += 64) s = meet(s, a.stats[(long)row * a.parts + i]);
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) s = meet(s, make_float2(__shfl_xor(s.x, o, 64), __shfl_xor(s.y, o, 64)));
+    if (threadIdx.x == 0) a.lse[row] = s.x + log2f(s.y) * LN2;
+  }
+  pick_row<T, THREADS>(a, row, static_cast<const T *>(a.z) + (long)row * a.ldz, key, pool);
+}
+
+// Both for a row, a block each: with many rows some blocks select while others read.
+template <class T, bool STREAM>
+__global__ void __launch_bounds__(256) k_top_row(const TopArgs a) {
+  __shared__ Pool pool;
+  __shared__ float2 red[4];
+  extern __shared__ unsigned gmax[];
+  const int row = blockIdx.x;
+  const T *z = static_cast<const T *>(a.z) + (long)row * a.ldz;
+  const float2 s = scan<T, STREAM>(a, z, 0, a.vocab, gmax, red);
+  if (threadIdx.x == 0) a.lse[row] = s.x + log2f(s.y) * LN2;
+  unsigned key[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int g = threadIdx.x + 256 * i;
+    key[i] = g < a.groups ? gmax[g] : 0;
+  }
+  pick_row<T, 256>(a, row, z, key, pool);
+}
+
+// Rows from which on a block takes a whole one.
+constexpr int WHOLE_ROWS = 512;
+
+template <class T>
+void launch(const TopArgs &a, hipStream_t st) {
+  // (1,024 threads hold the groups of any vocabulary, 256 those of 262,144 columns)
+  const bool narrow = a.groups <= 256 * PER;
+  if (narrow && a.rows >= WHOLE_ROWS) {
+    const size_t lds = (size_t)a.groups * 4;
+    if ((double)a.rows * a.vocab * sizeof(T) > STREAM_BYTES) k_top_row<T, true><<<a.rows, 256, lds, st>>>(a);
+    else k_top_row<T, false><<<a.rows, 256, lds, st>>>(a);
+    SEG_LAUNCH_CHECK();
+    return;
+  }
+  k_top_scan<T><<<(unsigned)((long)a.rows * a.parts), 256, 0, st>>>(a);
+  SEG_LAUNCH_CHECK();
+  if (narrow) k_top_pick<T, 256><<<a.rows, 256, 0, st>>>(a);
+  else k_top_pick<T, 1024><<<a.rows, 1024, 0, st>>>(a);
+  SEG_LAUNCH_CHECK();
 }
 
 struct TopWs {
@@ -259,11 +412,13 @@ struct TopWs {
   int groups, parts, span;
 };
 
-// Parts of a row: blocks of SPAN columns, fewer where that leaves the chip idle
+// Parts of a row: spans of SPAN columns, halved down to the 2,048 of one piece while the
+// chip has more CUs than blocks (one row of 151,936 fp32: 4.8 us in 10 parts, 3.3 in 75)
 TopWs top_ws(int rows, int vocab) {
   TopWs w{};
   w.groups = (vocab + GROUP - 1) / GROUP;
   w.span = SPAN;
+  while (w.span > 2048 && (long)rows * ((vocab + w.span - 1) / w.span) < 256) w.span /= 2;
   w.parts = (vocab + w.span - 1) / w.span;
   w.gmax = 0;
   w.stats = align_up((size_t)rows * w.groups * 4);
@@ -306,16 +461,7 @@ extern "C" seg_status seg_top_logits(int32_t rows, int32_t vocab, int32_t k, seg
     const TopArgs a{z, ldz, rows, vocab, k, w.groups, w.parts, w.span, scale, reinterpret_cast<unsigned *>(base + w.gmax),
                     reinterpret_cast<float2 *>(base + w.stats), ids, logits, lse};
     ProfScope prof("top_logits", stream);
-    const unsigned grid = (unsigned)((long)rows * w.parts);
-    if (dt == SEG_BF16) {
-      k_top_scan<unsigned short><<<grid, 256, 0, stream>>>(a);
-      SEG_LAUNCH_CHECK();
-      k_top_pick<unsigned short><<<rows, 256, 0, stream>>>(a);
-    } else {
-      k_top_scan<float><<<grid, 256, 0, stream>>>(a);
-      SEG_LAUNCH_CHECK();
-      k_top_pick<float><<<rows, 256, 0, stream>>>(a);
-    }
-    SEG_LAUNCH_CHECK();
+    if (dt == SEG_BF16) launch<unsigned short>(a, stream);
+    else launch<float>(a, stream);
   });
 }

@@ -53,7 +53,9 @@ def _z(rows, vocab, dtype, seed=0, std=2.5):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,vocab,k", [(1, 1, 1), (2, 5, 5), (3, 63, 20), (4, 64, 64), (2, 65, 7), (5, 256, 256), (3, 1001, 1),
                                           (7, 1001, 200), (2, 16384, 256), (3, 16385, 256), (37, 32000, 64), (1, 151936, 20),
-                                          (2, 151936, 256), (300, 5003, 33), (1, 1 << 20, 50)])
+                                          (2, 151936, 256), (300, 5003, 33), (1, 1 << 20, 50), (3, 300000, 100),
+                                          # a block a row
+                                          (512, 40, 7), (600, 1001, 33), (515, 5000, 256), (700, 2048, 1), (513, 20001, 64)])
 def test_columns_and_values(rows, vocab, k, dtype):
     say(rows, vocab, k, dtype)
     _check(_z(rows, vocab, dtype), k)
@@ -71,11 +73,14 @@ def test_parts_of_wider_rows(vocab, wide, at, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("vocab,k", [(40000, 64), (40000, 256), (700, 256), (100, 9)])
-def test_orders_and_ties(vocab, k, dtype):
+@pytest.mark.parametrize("rows", [9, 540])
+@pytest.mark.parametrize("vocab,k", [(40000, 64), (40000, 256), (700, 256), (100, 9), (151936, 3)])
+def test_orders_and_ties(vocab, k, rows, dtype):
     """All alike; two values; ascending and descending; ties across groups; both zeros."""
     import torch
-    z = torch.empty(9, vocab, device="cuda")
+    if rows * vocab > 1 << 25:
+        rows = 9
+    z = torch.zeros(rows, vocab, device="cuda")
     n = torch.arange(vocab, device="cuda").float()
     z[0] = 1.25
     z[1] = (n % 2)
