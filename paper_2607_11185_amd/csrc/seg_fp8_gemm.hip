@@ -7,10 +7,11 @@
 // 2^-13 of it and below; the groups' sums and the accumulator add up in fp32.  (An
 // 8-bit instruction without scales rounds the same way.)
 //
-// The compiler takes the scaled instruction for shorter than it is: vector instructions
-// that read its result too soon got the accumulator of before.  So the results are read
-// behind settled(), which waits longer than the instruction takes; other matrix
-// instructions may follow at once, the hardware orders them.
+// The compiler does not always keep vector instructions that read the result of such an
+// instruction away from it for long enough (copies of an accumulator at the end of a
+// loop got the one of before).  So results are read, and loops closed, behind settled(),
+// which waits longer than the instruction takes; other matrix instructions may follow
+// at once, the hardware orders them.
 #include <algorithm>
 #include <type_traits>
 
@@ -40,10 +41,15 @@ template <int N, class F>
 __device__ __forceinline__ void each(F &&f) {
   each_of(f, std::make_integer_sequence<int, N>());
 }
-// the matrix instructions of before have written their results
-__device__ __forceinline__ void settled() {
+// the matrix instructions of before have written their results to acc
+template <int NI, int NJ>
+__device__ __forceinline__ void settled(f32x4 (&acc)[NI][NJ]) {
   __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));
+  asm volatile("s_nop 15\n\ts_nop 3" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -58,8 +64,9 @@ struct Operand {
 template <class T, int N>
 __device__ __forceinline__ void store_run(T *d, int left, const float (&v)[N]) {
   if (left >= N) {
-    typedef T V __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
-    constexpr int W = 16 / sizeof(T);
+    constexpr int W = N < 16 / (int)sizeof(T) ? N : 16 / (int)sizeof(T);  // columns of an access
+    static_assert(N % W == 0, "whole accesses");
+    typedef T V __attribute__((ext_vector_type(W), aligned(sizeof(T))));
 #pragma unroll
     for (int q = 0; q < N / W; ++q) {
       V o;
@@ -95,13 +102,13 @@ struct Gemm8 {
 // of F is row F q + i of the tile (the loads put it there).  So a lane's scales of all
 // its fragments are F neighbouring bytes, one load a step, picked by the instruction;
 // and a lane ends with 16 consecutive columns of a row, which it stores as they are.
-constexpr int BN = gemm::BN, STEP = fp8::BLOCK, THREADS = gemm::THREADS;
+constexpr int STEP = fp8::BLOCK, THREADS = gemm::THREADS;
 
 struct Load8 {
   gemm::gemm_i32x4 rs;
   int voff, joff[8], chunk, bytes, add;
 
-  // F (4 or 8) fragments of 16 rows a wave tile; wave w of the group's four, load j: rows
+  // F (2, 4 or 8) fragments of 16 rows a wave tile; wave w of the group's four, load j: rows
   // 8 (w + 4 j) .. of the tile in LDS
   __device__ __forceinline__ void init(const uint8_t *code, long ld, int row0, int left, int F, int w, int lane) {
     rs = gemm::gemm_desc(code + (long)row0 * ld, (long)left * ld);
@@ -110,7 +117,8 @@ struct Load8 {
     bytes = (int)ld;
     voff = (F * p + (w >> 1)) * (int)ld + chunk;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) joff[j] = (F == 4 ? 64 * (j / 2) + 2 * (j % 2) : 128 * (j / 4) + 2 * (j % 4)) * (int)ld;
+    for (int j = 0; j < 8; ++j)
+      joff[j] = (F == 2 ? 32 * j : F == 4 ? 64 * (j / 2) + 2 * (j % 2) : 128 * (j / 4) + 2 * (j % 4)) * (int)ld;
   }
   __device__ __forceinline__ void prep(int k0) { add = k0 + chunk < bytes ? voff + k0 : 0x40000000; }
   __device__ __forceinline__ void load(unsigned dst, int j, int w) const {
@@ -157,8 +165,8 @@ struct Scales {
   }
 };
 
-template <int TM, class T>
-__global__ void __launch_bounds__(THREADS, 1) k_gemm8(const Gemm8 g) {
+template <int TM, int BN, class T>
+__global__ void __launch_bounds__(THREADS, BN == 128 ? 4 : 2) k_gemm8(const Gemm8 g) {
   constexpr int BM = gemm::bm_of(TM), SA = BM * STEP, SB = BN * STEP, LDS_B = SA * gemm::SLOTS_A;
   __shared__ __attribute__((aligned(1024))) char lds[LDS_B + SB * gemm::SLOTS_B];
   int idx = gemm::xcd_index(g.tiles * g.splits);
@@ -171,10 +179,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_gemm8(const Gemm8 g) {
   const int lane = threadIdx.x & 63, col = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = wave >> 2, w4 = wave & 3;  // waves w and w + 4 share a SIMD
-  const int wr = grp * 32 * TM, wc = w4 * 64;
+  const int wr = grp * 32 * TM, wc = w4 * (BN / 4);
   const int s0 = split * g.part, nk = min(g.part, g.steps - s0);
 
-  constexpr int FA = 2 * TM, FB = 4;
+  constexpr int FA = 2 * TM, FB = BN / 64;
+  static_assert(BM <= BN, "a group has as many loads of B as of A, or more");
   Load8 ldr;  // the group's operand
   if (grp == 0) ldr.init(g.a.code, g.a.ld, m0, min(BM, g.a.rows - m0), FA, w4, lane);
   else ldr.init(g.b.code, g.b.ld, n0, min(BN, g.b.rows - n0), FB, w4, lane);
@@ -265,7 +274,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_gemm8(const Gemm8 g) {
     __builtin_amdgcn_s_setprio(1);
     each<FA>([&](auto i) __attribute__((always_inline)) {
       each<FB>([&](auto jj) __attribute__((always_inline)) {
-        constexpr int I = decltype(i)::value, J = (I & 1) ? 3 - decltype(jj)::value : decltype(jj)::value;
+        constexpr int I = decltype(i)::value, J = (I & 1) ? FB - 1 - decltype(jj)::value : decltype(jj)::value;
         acc[I][J] = mfma8<J, I & 3>(
             join(__builtin_bit_cast(i32x4, b[0][J]), __builtin_bit_cast(i32x4, b[1][J])),
             join(__builtin_bit_cast(i32x4, a[0][I]), __builtin_bit_cast(i32x4, a[1][I])), acc[I][J], sb[0], sa[I / 4]);
@@ -274,7 +283,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_gemm8(const Gemm8 g) {
     // here and not behind the next barrier, where the compiler would move them (51% of the
     // matrix cores' time, 2,140 TFLOP/s at 8192^3)
 #pragma unroll
-    for (int i = 0; i < FA; ++i) asm volatile("" : "+v"(acc[i][0]), "+v"(acc[i][1]), "+v"(acc[i][2]), "+v"(acc[i][3]));
+    for (int i = 0; i < FA; ++i)
+#pragma unroll
+      for (int j = 0; j < FB; j += 2) asm volatile("" : "+v"(acc[i][j]), "+v"(acc[i][j + 1]));
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
     slot_b = slot_b == 2 * SB ? 0 : slot_b + SB;
@@ -287,21 +298,21 @@ __global__ void __launch_bounds__(THREADS, 1) k_gemm8(const Gemm8 g) {
     if (grp == 0 || t + 1 < nk) __builtin_amdgcn_s_barrier();
     GEMM_FENCE();
   }
-  settled();
-  const int n = n0 + wc + 16 * lg;
+  settled(acc);
+  const int n = n0 + wc + 4 * FB * lg;
   if (n >= g.b.rows) return;
   T *y = static_cast<T *>(g.y) + (long)split * g.split_stride;
 #pragma unroll
   for (int i = 0; i < FA; ++i) {
     const int m = m0 + wr + FA * col + i;
     if (m >= g.a.rows) continue;
-    float v[16];
+    float v[4 * FB];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[4 * r + j] = acc[i][j][r];
+      for (int j = 0; j < FB; ++j) v[FB * r + j] = acc[i][j][r];
     // (partial sums: rows are filled up to 16)
-    store_run(y + (long)m * g.ldy + n, g.splits > 1 ? 16 : g.b.rows - n, v);
+    store_run(y + (long)m * g.ldy + n, g.splits > 1 ? 4 * FB : g.b.rows - n, v);
   }
 }
 
@@ -336,11 +347,11 @@ __global__ void __launch_bounds__(256) k_finish8(const float *__restrict__ part,
 // their sums are added up in LDS, in order.  Memory gives the codes fastest in whole
 // 128-byte lines, which is not the instruction's operand, so a lane's 16 bytes go
 // through the wave's own piece of LDS (chunk c of row r in slot c ^ (r & 7)), while the
-// loads of the wave's next step are under way; no wave waits for another.  Rows past
-// the end read the last one, and their sums go nowhere; codes past the row's end read
-// as zeros.
-template <int NB, int CB, int WAVES, class T>
-__global__ void __launch_bounds__(64 * WAVES, NB < 4 ? 4 : 2) k_few8(const Gemm8 g) {
+// loads of the wave's next DEPTH steps are under way; no wave waits for another.  Rows of
+// b past the end read the last one, and their sums go nowhere; rows of a past the end are
+// not read, and codes past a row's end read as zeros.
+template <int NB, int CB, int WAVES, int DEPTH, int OCC, class T>
+__global__ void __launch_bounds__(64 * WAVES, OCC) k_few8(const Gemm8 g) {
   constexpr int ROWS = 16 * (CB > NB ? CB : NB), STAGE = WAVES * ROWS * 8, SUMS = WAVES * CB * NB * 64;
   __shared__ __attribute__((aligned(1024))) f32x4 lds[STAGE > SUMS ? STAGE : SUMS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -349,6 +360,7 @@ __global__ void __launch_bounds__(64 * WAVES, NB < 4 ? 4 : 2) k_few8(const Gemm8
   // row p of a piece is row CB (p % 16) + p / 16 of b's (NB of a's): see k_gemm8
   const uint8_t *bp = g.b.code + (long)n0 * ld;
   unsigned boff[2 * CB], aoff[2 * NB];
+  bool ain[2 * NB];
 #pragma unroll
   for (int i = 0; i < 2 * CB; ++i) {
     const int p = 8 * i + lr;
@@ -357,29 +369,33 @@ __global__ void __launch_bounds__(64 * WAVES, NB < 4 ? 4 : 2) k_few8(const Gemm8
 #pragma unroll
   for (int i = 0; i < 2 * NB; ++i) {
     const int p = 8 * i + lr;
-    aoff[i] = (unsigned)min(NB * (p & 15) + (p >> 4), g.a.rows - 1) * (unsigned)ld + 16 * lc;
+    const int row = NB * (p & 15) + (p >> 4);
+    ain[i] = row < g.a.rows;
+    aoff[i] = (unsigned)row * (unsigned)ld + 16 * lc;
   }
-  i32x4 w[2 * CB], x[2 * NB];
-  unsigned sw[1], sx[1], sw_next[1], sx_next[1];
+  struct Set {  // a step of the wave
+    i32x4 w[2 * CB], x[2 * NB];
+    unsigned sw[1], sx[1];
+  };
   Scales<CB> eb;
   Scales<NB> ea;
   eb.init(g.b, n0, r, wave);
   ea.init(g.a, 0, r, wave);
   eb.lde *= WAVES;
   ea.lde *= WAVES;
-  auto load = [&](int s) __attribute__((always_inline)) {
+  auto load = [&](Set &t, int s) __attribute__((always_inline)) {
     const int k = s * STEP;
     const bool in = k + 16 * lc < ld;
 #pragma unroll
     for (int i = 0; i < 2 * CB; ++i)
-      w[i] = in ? __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(bp + k + boff[i])) : i32x4{};
+      t.w[i] = in ? __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(bp + k + boff[i])) : i32x4{};
 #pragma unroll
     for (int i = 0; i < 2 * NB; ++i)
-      x[i] = in ? *reinterpret_cast<const i32x4 *>(g.a.code + k + aoff[i]) : i32x4{};
-    sw_next[0] = sx_next[0] = 0;
+      t.x[i] = in && ain[i] ? *reinterpret_cast<const i32x4 *>(g.a.code + k + aoff[i]) : i32x4{};
+    t.sw[0] = t.sx[0] = 0;
     if (s < g.steps) {
-      eb.fetch(sw_next);
-      ea.fetch(sx_next);
+      eb.fetch(t.sw);
+      ea.fetch(t.sx);
     }
   };
   f32x4 acc[CB][NB];
@@ -391,32 +407,39 @@ __global__ void __launch_bounds__(64 * WAVES, NB < 4 ? 4 : 2) k_few8(const Gemm8
   i32x4 *to = stage + lr * 8 + (lc ^ lr);
   const i32x4 *from = stage + r * 8;
   const int c0 = lg ^ (r & 7), c1 = (4 + lg) ^ (r & 7);
-  load(wave);
-  for (int s = wave; s < g.steps; s += WAVES) {
+  // the products of a step, and the loads of the wave's step `next` in its place
+  auto step = [&](Set &t, int next) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 2 * NB; ++i) to[64 * i] = x[i];
+    for (int i = 0; i < 2 * NB; ++i) to[64 * i] = t.x[i];
     __builtin_amdgcn_wave_barrier();
     i32x8 cx[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n) cx[n] = join(from[n * 128 + c0], from[n * 128 + c1]);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int i = 0; i < 2 * CB; ++i) to[64 * i] = w[i];
+    for (int i = 0; i < 2 * CB; ++i) to[64 * i] = t.w[i];
     __builtin_amdgcn_wave_barrier();
-    sw[0] = eb.square ? sw_next[0] * 0x01010101u : sw_next[0];
-    sx[0] = ea.square ? sx_next[0] * 0x01010101u : sx_next[0];
-    load(s + WAVES);
+    const unsigned sw = eb.square ? t.sw[0] * 0x01010101u : t.sw[0], sx = ea.square ? t.sx[0] * 0x01010101u : t.sx[0];
+    load(t, next);
     each<CB>([&](auto b) __attribute__((always_inline)) {
       constexpr int B = decltype(b)::value;
       const i32x8 cw = join(from[B * 128 + c0], from[B * 128 + c1]);
       each<NB>([&](auto n) __attribute__((always_inline)) {
         constexpr int N = decltype(n)::value;
-        acc[B][N] = mfma8<B, N>(cw, cx[N], acc[B][N], sw[0], sx[0]);
+        acc[B][N] = mfma8<B, N>(cw, cx[N], acc[B][N], sw, sx);
       });
     });
+    settled(acc);
     __builtin_amdgcn_wave_barrier();
+  };
+  Set t[DEPTH];
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d) load(t[d], wave + d * WAVES);
+  for (int s = wave; s < g.steps; s += WAVES * DEPTH) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+      if (d == 0 || s + d * WAVES < g.steps) step(t[d], s + (d + DEPTH) * WAVES);
   }
-  settled();
   f32x4(*sums)[CB * NB][64] = reinterpret_cast<f32x4(*)[CB * NB][64]>(lds);
   __syncthreads();
 #pragma unroll
@@ -449,27 +472,98 @@ long ld_part(int outs) { return (outs + 15) / 16 * 16; }
 bool sizes_ok(int32_t rows, int32_t outs, int32_t cols) {
   return rows >= 0 && outs >= 1 && cols >= 1 && rows <= (1 << 20) && outs <= (1 << 20) && cols <= (1 << 20);
 }
-gemm::Choice choice_of(int rows, int outs, int cols) {
-  const long steps = fp8::blocks_of(cols);
-  const double elems = (double)rows * ld_part(outs);
-  return gemm::choose(gemm::tiles_of(rows, outs, 4), gemm::tiles_of(rows, outs, 2), steps, elems, 1L << 60);
+struct Choice {
+  int tm, bn, parts, part;
+};
+long tiles_of(int rows, int outs, int tm, int bn) {
+  return ((rows + 64 * tm - 1) / (64 * tm)) * (((long)outs + bn - 1) / bn);
+}
+// How a product is launched, by the time that each way is expected to take: us of blocks
+// that fill u of the chip's CUs, by steps s of 128 columns; a full chip's clocks are lower.
+//   256 x 256 tiles: 6 + s (1.06 + 0.49 u) a round;  128 x 256: 4 + s (0.8 + 0.3 u);
+//   128 x 128, two of them on a CU: 4 + 0.65 s for the first 256, another s (0.3 + 0.15 u)
+//   with the second;
+// and for parts of K their fp32 sums, 4.5 + 0.3 a MB.  Measured / expected over 65 to 2,048
+// rows, us (best of the three, parts of K in brackets): 128 x 18,944 x 3,584 (rows, outs,
+// cols) 30.4 / 22.2, 512 45.9 / 42.4, 1,500 94.4 / 94.4; 256 x 3,584 x 18,944 (8) 41.4 / 37.3,
+// 1,024 (4) 81 / 81; 300 x 5,504 x 2,048 14.4 / 14.4, 2,048 29.2 / 28.4.  One kind of tile for
+// all: 41.7, 45.9, 94.4; 178, 176; 24.2, 29.2 (256 x 256, whole).
+double expect(int tm, int bn, long blocks, double s) {
+  const long slots = bn == 128 ? 512 : 256, full = blocks / slots, rest = blocks % slots;
+  auto round = [&](double n) {  // n blocks, at most the slots
+    if (bn == 128) return 4 + s * (0.65 + (n > 256 ? 0.3 + 0.15 * (n - 256) / 256 : 0.0));
+    return tm == 2 ? 4 + s * (0.8 + 0.3 * n / 256) : 6 + s * (1.06 + 0.49 * n / 256);
+  };
+  return full * round((double)slots) + (rest ? round((double)rest) : 0.0);
 }
 
-template <class T>
-void few(const Gemm8 &g, hipStream_t st) {
-  const unsigned nb = (unsigned)((g.b.rows + 31) / 32);
-  if (g.a.rows <= 16) k_few8<1, 2, 8, T><<<nb, 64 * 8, 0, st>>>(g);
-  else if (g.a.rows <= 32) k_few8<2, 2, 8, T><<<nb, 64 * 8, 0, st>>>(g);
-  else k_few8<4, 2, 4, T><<<nb, 64 * 4, 0, st>>>(g);
+Choice choice_of(int rows, int outs, int cols) {
+  const int steps = (int)fp8::blocks_of(cols);
+  const double mb = (double)rows * ld_part(outs) * 4e-6;
+  Choice best{};
+  double best_us = 0;
+  for (int v = 0; v < 3; ++v) {
+    const int tm = v == 0 ? 4 : 2, bn = v == 2 ? 128 : 256;
+    const long tiles = tiles_of(rows, outs, tm, bn);
+    for (int p = 1; p <= 16; ++p) {
+      const int per = (steps + p - 1) / p;
+      if (p > 1 && (per < 2 || (p - 1) * per >= steps || tiles * p > 2048)) continue;
+      const double us = expect(tm, bn, tiles * p, per) + (p > 1 ? 4.5 + 0.3 * mb * p : 0.0);
+      if (best_us == 0 || us < best_us) {
+        best = Choice{tm, bn, p, per};
+        best_us = us;
+      }
+    }
+  }
+  return best;
+}
+
+template <int NB, int CB, int WAVES, int DEPTH, int OCC, class T>
+void few_as(const Gemm8 &g, hipStream_t st) {
+  k_few8<NB, CB, WAVES, DEPTH, OCC, T><<<(unsigned)((g.b.rows + 16 * CB - 1) / (16 * CB)), 64 * WAVES, 0, st>>>(g);
   SEG_LAUNCH_CHECK();
 }
 
+// Narrow blocks where there are few of them (each CU then has more waves on its rows of b),
+// wide ones, which read a less often, where there are many.  Measured, us, rows x outs x
+// cols, the kernel taken / another: 1 x 18,944 x 3,584 12.9 / 14.2 (16 waves), 16.7 (32 rows
+// of b a block, one step ahead); 1 x 3,584 x 18,944 13.2 / 15.5 (8 waves, two steps ahead); 24
+// x 18,944 x 3,584 17.1 / 20.4 (16 rows of b); 24 x 3,584 x 18,944 23.5 / 26.4 (32 rows); 64
+// x 18,944 x 3,584 25.4 / 26.1; 64 x 3,584 x 18,944 32.1 / 37.4; 64 x 5,504 x 2,048 7.6 / 10.0
+// (64 rows); 64 x 151,936 x 3,584 121 / 155 (32 rows).
+struct Few {
+  int nb, cb, waves;
+};
+Few few_choice(int rows, int outs, int cols) {
+  if (rows <= 16) return {1, 1, outs <= 16 * 256 && cols > 16 * STEP ? 16 : 8};
+  if (rows <= 32) return outs <= 32 * 128 ? Few{2, 1, 8} : Few{2, 2, 4};
+  return outs <= 32 * 128 ? Few{4, 1, 8} : outs <= 32 * 512 ? Few{4, 2, 8} : Few{4, 4, 4};
+}
+
 template <class T>
-void many(Gemm8 g, int tm, hipStream_t st) {
-  g.tiles = (int)gemm::tiles_of(g.a.rows, g.b.rows, tm);
+void few(const Gemm8 &g, const Few &f, hipStream_t st) {
+  if (f.nb == 1) {
+    if (f.waves == 16) few_as<1, 1, 16, 1, 4, T>(g, st);
+    else few_as<1, 1, 8, 2, 4, T>(g, st);
+  } else if (f.nb == 2) {
+    if (f.cb == 1) few_as<2, 1, 8, 2, 4, T>(g, st);
+    else few_as<2, 2, 4, 2, 2, T>(g, st);
+  } else if (f.cb == 1) {
+    few_as<4, 1, 8, 1, 2, T>(g, st);
+  } else if (f.cb == 2) {
+    few_as<4, 2, 8, 1, 2, T>(g, st);
+  } else {
+    few_as<4, 4, 4, 1, 2, T>(g, st);
+  }
+}
+
+template <class T>
+void many(Gemm8 g, const Choice &c, hipStream_t st) {
+  g.tiles = (int)tiles_of(g.a.rows, g.b.rows, c.tm, c.bn);
   const unsigned grid = (unsigned)(((long)g.tiles * g.splits + 7) / 8 * 8);
-  if (tm == 2) k_gemm8<2, T><<<grid, THREADS, 0, st>>>(g);
-  else k_gemm8<4, T><<<grid, THREADS, 0, st>>>(g);
+  if (c.bn == 128) k_gemm8<2, 128, T><<<grid, THREADS, 0, st>>>(g);
+  else if (c.tm == 2) k_gemm8<2, 256, T><<<grid, THREADS, 0, st>>>(g);
+  else k_gemm8<4, 256, T><<<grid, THREADS, 0, st>>>(g);
   SEG_LAUNCH_CHECK();
 }
 
@@ -478,9 +572,25 @@ void many(Gemm8 g, int tm, hipStream_t st) {
 
 using namespace seg;
 
+// How a product is launched (for tests): out = {rows of a tile / 64, columns, parts of K}, or
+// for few rows {16-row blocks of a, of b, - waves}.
+extern "C" void seg_fp8_gemm_choice(int32_t rows, int32_t outs, int32_t cols, int32_t *out) {
+  if (rows <= FEW) {
+    const Few f = few_choice(rows, outs, cols);
+    out[0] = f.nb;
+    out[1] = f.cb;
+    out[2] = -f.waves;
+    return;
+  }
+  const Choice c = choice_of(rows, outs, cols);
+  out[0] = c.tm;
+  out[1] = c.bn;
+  out[2] = c.parts;
+}
+
 extern "C" size_t seg_fp8_gemm_workspace_bytes(int32_t rows, int32_t outs, int32_t cols) {
   if (!sizes_ok(rows, outs, cols) || rows <= FEW) return 0;
-  const gemm::Choice c = choice_of(rows, outs, cols);
+  const Choice c = choice_of(rows, outs, cols);
   return c.parts > 1 ? align_up((size_t)c.parts * rows * ld_part(outs) * 4) : 0;
 }
 
@@ -510,14 +620,15 @@ extern "C" seg_status seg_fp8_gemm(int32_t rows, int32_t outs, int32_t cols, con
     Gemm8 g{operand(a, rows), operand(b, outs), y, ldy, 0, (int)fp8::blocks_of(cols), (int)fp8::blocks_of(cols), 1, 0};
     ProfScope prof("fp8_gemm", stream);
     if (rows <= FEW) {
-      if (dt == SEG_BF16) few<unsigned short>(g, stream);
-      else few<float>(g, stream);
+      const Few f = few_choice(rows, outs, cols);
+      if (dt == SEG_BF16) few<unsigned short>(g, f, stream);
+      else few<float>(g, f, stream);
       return;
     }
-    const gemm::Choice c = choice_of(rows, outs, cols);
+    const Choice c = choice_of(rows, outs, cols);
     if (c.parts == 1) {
-      if (dt == SEG_BF16) many<unsigned short>(g, c.tm, stream);
-      else many<float>(g, c.tm, stream);
+      if (dt == SEG_BF16) many<unsigned short>(g, c, stream);
+      else many<float>(g, c, stream);
       return;
     }
     g.y = ws;
@@ -525,7 +636,7 @@ extern "C" seg_status seg_fp8_gemm(int32_t rows, int32_t outs, int32_t cols, con
     g.split_stride = (long)rows * g.ldy;
     g.splits = c.parts;
     g.part = c.part;
-    many<float>(g, c.tm, stream);
+    many<float>(g, c, stream);
     const unsigned grid = (unsigned)std::min<long>(8192, ((long)rows * g.ldy / 8 + 255) / 256);
     if (dt == SEG_BF16)
       k_finish8<<<grid, 256, 0, stream>>>(static_cast<const float *>(ws), c.parts, g.split_stride, g.ldy, rows, outs,

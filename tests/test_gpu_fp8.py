@@ -11,6 +11,8 @@ sum|a b|; a bf16 output rounds once more, 2^-8.  Over a whole tensor of normal v
 dropped parts are independent: each at most 2^-13 of its group's largest product, about
 3 of the products' size, so sqrt(1/3) 3 2^-13 < 2^-12 of the result (relative
 Frobenius norm)."""
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -164,7 +166,10 @@ def _within(got, ref, tol, what):
 
 SHAPES = [(1, 1, 1), (1, 16, 128), (1, 300, 1000), (3, 33, 129), (16, 64, 256), (17, 100, 2040), (32, 2048, 640), (33, 31, 1300),
           (64, 130, 4096), (65, 7, 100), (70, 257, 513), (130, 520, 1111), (257, 256, 2048), (300, 1032, 128), (777, 5001, 2040),
-          (128, 640, 9001), (2, 40, 16384)]
+          (128, 640, 9001), (2, 40, 16384),
+          # each kernel for few rows, and each kind of tile
+          (5, 4200, 2200), (9, 48, 2304), (20, 4200, 300), (25, 100, 1500), (40, 100, 1500), (50, 4200, 700), (47, 16500, 300),
+          (300, 12000, 128), (400, 19000, 128), (65, 12000, 4096), (130, 5000, 16384)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -181,10 +186,18 @@ def test_product(shape, ba, bb, dtype):
 def test_every_way_of_cutting():
     """The shapes take each kernel, whole and in parts of K."""
     L = _lib.lib()
-    few = {(s[0] - 1) // 16 for s in SHAPES if s[0] <= 64}
-    assert few >= {0, 1, 2, 3}
-    parts = {L.seg_fp8_gemm_workspace_bytes(*s) > 0 for s in SHAPES if s[0] > 64}
-    assert parts == {True, False}
+    f = L.seg_fp8_gemm_choice
+    f.restype, f.argtypes = None, [ctypes.c_int32] * 3 + [ctypes.c_void_p]
+    got = set()
+    for s in SHAPES:
+        out = (ctypes.c_int32 * 3)()
+        f(*s, out)
+        got.add((out[0], out[1], min(out[2], 2)))
+        assert (L.seg_fp8_gemm_workspace_bytes(*s) > 0) == (out[2] > 1)
+    # 16-row blocks of a, of b, waves
+    assert got >= {(1, 1, -16), (1, 1, -8), (2, 1, -8), (2, 2, -4), (4, 1, -8), (4, 2, -8), (4, 4, -4)}, got
+    # rows of a tile / 64, columns, whole or in parts
+    assert got >= {(4, 256, 1), (2, 256, 1), (2, 128, 1), (4, 256, 2), (2, 256, 2), (2, 128, 2)}, got
 
 
 @pytest.mark.parametrize("shape", [(40, 512, 4096), (513, 1024, 4096), (2, 256, 8192)], ids=lambda s: "x".join(map(str, s)))
