@@ -73,15 +73,18 @@ __device__ __forceinline__ float sum_wave(float v) {
   return over_wave(v, [](float a, float b) { return a + b; });
 }
 
-// 16 rows a block: their LSE from the slabs as in the action-token loss (16 threads a row),
-// then a wave a row, up to four of its columns a lane.
+// ROWS rows a block: their LSE from the slabs as in the action-token loss, then a wave a
+// row, up to four of its columns a lane.  16 rows read the slabs in whole lines; with few
+// rows 4 to a block leave no wave a second row (37 rows x 1,001: 10.6 us with 16, 4.4 with
+// 4; 1,024 x 32,000 20.8 / 9.6).
 //   A row without weight, or whose teacher gives no probability to any column, has loss 0
 // and no gradient whatever its h holds: its dz is zero, and so is its row of hb from here
 // on, as 0 x NaN would reach dW.
 //   The same column more than once: each of its places gets the sum over all of them, in
 // order, so it does not matter which is written last.
+template <int ROWS>
 __global__ void __launch_bounds__(256) k_distill_rows(const RowArgs a) {
-  constexpr int ROWS = 16, SL = 256 / ROWS, E = MAX_K / 64;
+  constexpr int SL = 256 / ROWS, E = MAX_K / 64;
   __shared__ float2 red[SL][ROWS];
   __shared__ float lse_of[ROWS];
   __shared__ int col_of[4][MAX_K];
@@ -93,10 +96,14 @@ __global__ void __launch_bounds__(256) k_distill_rows(const RowArgs a) {
 #pragma unroll 4
       for (int i = part; i < a.slabs; i += SL) s = meet(s, a.stats[(long)i * a.rows + r]);
     }
+    if (ROWS == 4) {  // 16 threads of a row are lanes of a wave: their order first
+#pragma unroll
+      for (int o = 4; o < 64; o *= 2) s = meet(s, make_float2(__shfl_xor(s.x, o, 64), __shfl_xor(s.y, o, 64)));
+    }
     red[part][t] = s;
     __syncthreads();
     if (part == 0) {
-      for (int k = 1; k < SL; ++k) s = meet(s, red[k][t]);
+      for (int k = ROWS == 4 ? 16 : 1; k < SL; k += ROWS == 4 ? 16 : 1) s = meet(s, red[k][t]);
       // (no sum: every logit of the row is NaN)
       lse_of[t] = s.y == 0.f ? __builtin_nanf("") : (s.x + log2f(s.y)) * LN2;
     }
@@ -258,7 +265,8 @@ void distill_impl(const Distill &a, char *base, const DistillWs &L, hipStream_t 
     ProfScope prof("distill", st);
     const RowArgs r{stats, zt, L.slabs, R, Rp, V, a.k, H, grad, a.ids, a.logits, a.t_lse, a.weight, a.cfg.teacher_scale,
                     a.cfg.loss_scale, a.loss_tok, a.lse, factor, place, hb};
-    k_distill_rows<<<(R + 15) / 16, 256, 0, st>>>(r);
+    if (R >= 4096) k_distill_rows<16><<<(R + 15) / 16, 256, 0, st>>>(r);
+    else k_distill_rows<4><<<(R + 3) / 4, 256, 0, st>>>(r);
     SEG_LAUNCH_CHECK();
     if (!grad) {
       k_loss_sum<<<1, 256, 0, st>>>(a.loss_tok, R, a.cfg.loss_scale, a.loss_sum);
