@@ -385,9 +385,12 @@ def _current(dev) -> int:
 def _on(dev):
     """Calls are made with the tensors' GPU as the current one."""
     import torch
-    if torch.cuda.current_device() == dev.index:
-        return contextlib.nullcontext()
+    if torch._C._cuda_getDevice() == dev.index:
+        return _HERE
     return torch.cuda.device(dev)
+
+
+_HERE = contextlib.nullcontext()
 
 
 @dataclasses.dataclass
@@ -793,27 +796,35 @@ class Fp8:
 
     def c(self) -> "_lib.SegFp8":
         import torch
-        rows, cols = self.shape
-        assert self.block_rows in (1, 128)
-        assert self.code.dtype == torch.uint8 and self.exp.dtype == torch.uint8
-        assert self.code.shape == (rows, _up(cols, 16))
-        assert self.exp.shape == (-(-cols // 128), _up(-(-rows // self.block_rows), 16))
-        assert self.code.is_contiguous() and self.exp.is_contiguous()
-        return _lib.SegFp8(self.code.data_ptr(), self.exp.data_ptr(), self.block_rows)
+        code, exp, cols, br, u8 = self.code, self.exp, self.cols, self.block_rows, torch.uint8
+        rows = code.shape[0]
+        assert br in (1, 128)
+        assert code.dtype == u8 and exp.dtype == u8
+        assert code.shape == (rows, _up(cols, 16))
+        assert exp.shape == (-(-cols // 128), _up(-(-rows // br), 16))
+        assert code.is_contiguous() and exp.is_contiguous()
+        return _lib.SegFp8(code.data_ptr(), exp.data_ptr(), br)
 
 
 def seg_fp8_pack(x, block_rows: int = 1, out: Optional[Fp8] = None) -> Fp8:
     """x [rows, cols] (rows at any distance) in 8-bit floating point: a scale for each
     128 columns of a row, or (block_rows = 128) of 128 rows, as weights have them."""
+    import torch
     rows, cols = x.shape
     dt = _dtype_code(x)
     if out is None:
-        out = Fp8.empty(rows, cols, block_rows, x.device)
-    assert out.shape == (rows, cols) and out.block_rows == block_rows
+        if block_rows not in (1, 128):
+            raise ValueError(f"blocks of {block_rows} rows, not of 1 or 128")
+        u8 = torch.uint8
+        out = Fp8(x.new_empty((rows, _up(cols, 16)), dtype=u8),
+                  x.new_empty((-(-cols // 128), _up(-(-rows // block_rows), 16)), dtype=u8), cols, block_rows)
+        c = _lib.SegFp8(out.code.data_ptr(), out.exp.data_ptr(), block_rows)
+    else:
+        assert out.shape == (rows, cols) and out.block_rows == block_rows
+        c = out.c()
     dev = _device(x, out.code, out.exp)
     with _on(dev):
-        check(_lib.lib().seg_fp8_pack(rows, cols, dt, x.data_ptr(), _rows(x), ctypes.byref(out.c()),
-                                      _current(dev)))
+        check(_lib.lib().seg_fp8_pack(rows, cols, dt, x.data_ptr(), _rows(x), ctypes.byref(c), _current(dev)))
     return out
 
 
@@ -822,7 +833,7 @@ def seg_fp8_unpack(a: Fp8, dtype=None, x=None):
     import torch
     rows, cols = a.shape
     if x is None:
-        x = torch.empty((rows, cols), dtype=dtype or torch.bfloat16, device=a.code.device)
+        x = a.code.new_empty((rows, cols), dtype=dtype or torch.bfloat16)
     assert x.shape == (rows, cols) and (dtype is None or x.dtype == dtype)
     dev = _device(x, a.code, a.exp)
     with _on(dev):
@@ -845,7 +856,7 @@ def seg_fp8_gemm(a: Fp8, b: Fp8, dtype=None, y=None, ws=None):
     outs = b.shape[0]
     assert b.shape == (outs, cols), f"a has {cols} columns and b {b.shape[1]}"
     if y is None:
-        y = torch.empty((rows, outs), dtype=dtype or torch.bfloat16, device=a.code.device)
+        y = a.code.new_empty((rows, outs), dtype=dtype or torch.bfloat16)
     assert y.shape == (rows, outs) and (dtype is None or y.dtype == dtype)
     if ws is None:
         ws = fp8_gemm_workspace(rows, outs, cols, y.device)
@@ -871,12 +882,12 @@ def seg_top_logits(z, k: int, scale: float = 1.0, out: Optional[dict] = None, ws
     rows, vocab = z.shape
     dt, dev = _dtype_code(z), z.device
     if out is None:
-        out = {"ids": torch.empty((rows, k), dtype=torch.int32, device=dev),
-               "logits": torch.empty((rows, k), dtype=torch.float32, device=dev),
-               "lse": torch.empty(rows, dtype=torch.float32, device=dev)}
-    for n, shape, dtype in (("ids", (rows, k), torch.int32), ("logits", (rows, k), torch.float32),
-                            ("lse", (rows,), torch.float32)):
-        assert out[n].shape == shape and out[n].dtype == dtype and out[n].is_contiguous(), n
+        out = {"ids": z.new_empty((rows, k), dtype=torch.int32), "logits": z.new_empty((rows, k), dtype=torch.float32),
+               "lse": z.new_empty(rows, dtype=torch.float32)}
+    else:
+        for n, shape, dtype in (("ids", (rows, k), torch.int32), ("logits", (rows, k), torch.float32),
+                                ("lse", (rows,), torch.float32)):
+            assert out[n].shape == shape and out[n].dtype == dtype and out[n].is_contiguous(), n
     if ws is None:
         ws = top_logits_workspace(rows, vocab, dev)
     _device(z, out["ids"], out["logits"], out["lse"], ws)
@@ -926,15 +937,17 @@ def seg_distill_loss(h, row_index, w, ids, logits, cfg: DistillCfg, t_lse=None, 
     assert logits.shape == (R, k) and logits.dtype == torch.float32 and logits.is_contiguous()
     for t in (t_lse, row_weight):
         assert t is None or (t.shape == (R,) and t.dtype == torch.float32 and t.is_contiguous())
-    if out is None:
-        f32 = dict(dtype=torch.float32, device=dev)
-        out = {"loss_tok": torch.empty(R, **f32), "lse": torch.empty(R, **f32), "loss_sum": torch.empty(1, **f32),
-               "dh": torch.empty((R, H), dtype=h.dtype, device=dev) if cfg.want_grad else None,
-               "dw": torch.empty((V, H), dtype=dw_dtype or torch.float32, device=dev) if cfg.want_grad else None}
-    for n, shape in (("loss_tok", (R,)), ("lse", (R,)), ("loss_sum", (1,))):
-        assert out[n].shape == shape and out[n].dtype == torch.float32 and out[n].is_contiguous(), n
+    fresh = out is None
+    if fresh:
+        f32 = torch.float32
+        out = {"loss_tok": h.new_empty(R, dtype=f32), "lse": h.new_empty(R, dtype=f32), "loss_sum": h.new_empty(1, dtype=f32),
+               "dh": h.new_empty((R, H)) if cfg.want_grad else None,
+               "dw": h.new_empty((V, H), dtype=dw_dtype or f32) if cfg.want_grad else None}
+    else:
+        for n, shape in (("loss_tok", (R,)), ("lse", (R,)), ("loss_sum", (1,))):
+            assert out[n].shape == shape and out[n].dtype == torch.float32 and out[n].is_contiguous(), n
     dh, dw = out.get("dh"), out.get("dw")
-    if cfg.want_grad:
+    if cfg.want_grad and not fresh:
         assert dh.shape == (R, H) and dh.dtype == h.dtype and dh.is_contiguous()
         assert dw.shape == (V, H) and dw.is_contiguous() and (dw_dtype is None or dw.dtype == dw_dtype)
     if ws is None:
