@@ -18,6 +18,7 @@
 
 #include "act8.h"
 #include "common.h"
+#include "fp8.h"
 
 namespace seg {
 namespace {
@@ -28,14 +29,6 @@ constexpr float FAR = 3.4028234663852886e38f;
 constexpr int GROUP = 64;    // columns
 constexpr int MAX_K = 256;
 constexpr int SPAN = 16384;  // columns of a block of the scan, at most
-
-// Whole numbers in the order of the values: NaN first, zeros alike.  No value has 0.
-__device__ __forceinline__ unsigned order(float x) {
-  unsigned u = __builtin_bit_cast(unsigned, x);
-  if (x != x) return 0xffffffffu;
-  if (x == 0.f) u = 0;
-  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
-}
 
 template <class T>
 struct Piece;
@@ -53,6 +46,16 @@ __device__ __forceinline__ float value(T v) {
   else return v;
 }
 
+// Whole numbers in the order of the values: NaN first, zeros alike; 16 bits for bf16, whose
+// thresholds then take one pass less.  No value has 0.
+template <class T>
+__device__ __forceinline__ unsigned order(float x) {
+  unsigned u = __builtin_bit_cast(unsigned, x);
+  if (x == 0.f) u = 0;
+  u ^= (unsigned)((int)u >> 31) | 0x80000000u;
+  if (x != x) u = 0xffffffffu;
+  return sizeof(T) == 2 ? u >> 16 : u;
+}
 struct TopArgs {
   const void *z;
   long ldz;
@@ -127,7 +130,7 @@ __device__ __forceinline__ float2 scan(const TopArgs &a, const T *__restrict__ z
         s.y += in(j) ? e : 0.f;
       }
       s.x = m;
-      const unsigned top = act8::max8(WHOLE || at < c1 ? (nan ? 0xffffffffu : order(most)) : 0u);
+      const unsigned top = act8::max8(WHOLE || at < c1 ? order<T>(nan ? __builtin_nanf("") : most) : 0u);
       if ((threadIdx.x & 7) == 0 && (WHOLE || at < c1)) gmax[at / GROUP] = top;
     }
   };
@@ -158,9 +161,8 @@ typedef unsigned long long u64;
 
 // What a block's threads share to find a threshold.
 struct Pick {
-  unsigned hist[256];
-  unsigned wave[16];
-  unsigned least, most, digit, want, done;
+  __attribute__((aligned(16))) unsigned hist[256];
+  unsigned least, most, own, digit, want, done;
 };
 
 // The threshold t such that exactly `want` (at least 1, at most all) of the numbers of the
@@ -169,10 +171,13 @@ struct Pick {
 // numbers between the least and the most that may still be t are counted in up to 256 equal
 // ranges, and the range that holds t is the next to be cut: two or three times for values of
 // one size, four at most (digits of the bits from the top down would meet values of one
-// exponent in one or two counters first).
+// exponent in one or two counters first).  Counters that many threads meet in are what a
+// pass costs, so it starts from a bound that leaves most numbers out.
 struct Cut {
   unsigned t, want;  // want: of the numbers equal to t; 0: all that are >= t
 };
+__device__ __forceinline__ unsigned max_wave(unsigned x) { return act8::max_groups(fp8::max16(x)); }
+
 template <int THREADS, class K>
 __device__ __forceinline__ Cut threshold(K &&each, unsigned want, Pick &p) {
   unsigned lo = 0xffffffffu, hi = 0;
@@ -180,63 +185,55 @@ __device__ __forceinline__ Cut threshold(K &&each, unsigned want, Pick &p) {
     lo = min(lo, x);
     hi = max(hi, x);
   });
+  const unsigned own = ~max_wave(~hi);  // of the threads' largest (0 where one has none), the smallest
+  lo = ~max_wave(~lo);
+  hi = max_wave(hi);
   if (threadIdx.x == 0) {
-    p.least = 0xffffffffu;
+    p.least = p.own = 0xffffffffu;
     p.most = 0;
   }
+  if (threadIdx.x < 256) p.hist[threadIdx.x] = 0;
   __syncthreads();
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    lo = min(lo, (unsigned)__shfl_xor((int)lo, o, 64));
-    hi = max(hi, (unsigned)__shfl_xor((int)hi, o, 64));
-  }
   if ((threadIdx.x & 63) == 0) {
     atomicMin(&p.least, lo);
+    atomicMin(&p.own, own);
     atomicMax(&p.most, hi);
   }
   __syncthreads();
   lo = p.least;
   hi = p.most;
+  // as many numbers as threads are at least the smallest of the threads' largest
+  if (want <= THREADS && p.own > 0) lo = p.own;
   while (lo < hi) {
     const int shift = max(0, 24 - (int)__builtin_clz(hi - lo));  // (hi - lo) >> shift is at most 255
-    for (int i = threadIdx.x; i < 256; i += THREADS) p.hist[i] = 0;
-    __syncthreads();
     each([&](unsigned x) {
       if (x >= lo && x <= hi) atomicAdd(&p.hist[(x - lo) >> shift], 1u);
     });
     __syncthreads();
-    if (threadIdx.x < 256) {  // numbers in the thread's range and those above it
-      const unsigned own = p.hist[threadIdx.x];
-      unsigned n = own;
+    if (threadIdx.x < 64) {  // four counters a lane, those of the largest numbers in lane 0
+      uint4 *h = reinterpret_cast<uint4 *>(p.hist) + (63 - threadIdx.x);
+      const uint4 c = *h;
+      *h = make_uint4(0, 0, 0, 0);
+      unsigned above = c.x + c.y + c.z + c.w;  // with all above them
 #pragma unroll
       for (int o = 1; o < 64; o *= 2) {
-        const unsigned t = __shfl_down(n, o, 64);
-        if ((threadIdx.x & 63) + o < 64) n += t;
+        const unsigned t = __shfl_up(above, o, 64);
+        if ((int)threadIdx.x >= o) above += t;
       }
-      if ((threadIdx.x & 63) == 0) p.wave[threadIdx.x >> 6] = n;
-      p.hist[threadIdx.x] = n;
-    }
-    __syncthreads();
-    if (threadIdx.x < 256) {
-      unsigned n = p.hist[threadIdx.x];
-      unsigned next = (threadIdx.x & 63) < 63 ? p.hist[threadIdx.x + 1] : 0;
-      for (int w = (threadIdx.x >> 6) + 1; w < 4; ++w) {
-        n += p.wave[w];
-        next += p.wave[w];
-      }
-      if (n >= want && next < want) {
-        p.digit = threadIdx.x;
-        p.want = want - next;
-        p.done = n == want;
-      }
+      const unsigned n[5] = {above - (c.x + c.y + c.z + c.w), above - (c.x + c.y + c.z), above - (c.x + c.y), above - c.x, above};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)  // counter 3 - j: n[j] numbers above it, n[j + 1] with it
+        if (n[j] < want && n[j + 1] >= want) {
+          p.digit = 4 * (63 - threadIdx.x) + 3 - j;
+          p.want = want - n[j];
+          p.done = n[j + 1] == want;
+        }
     }
     __syncthreads();
     lo += p.digit << shift;
     hi = lo + min(hi - lo, (1u << shift) - 1);
     want = p.want;
-    const bool done = p.done;
-    __syncthreads();
-    if (done) return Cut{lo, 0};
+    if (p.done) return Cut{lo, 0};
   }
   return Cut{lo, want};
 }
@@ -252,6 +249,23 @@ struct Pool {
   int group[MAX_K];
   unsigned count, low;
 };
+
+// The first k of n candidates to their places: each counts those in front of it.
+template <class T, int THREADS>
+__device__ __forceinline__ void place(const TopArgs &a, int row, const T *__restrict__ z, const u64 (&cand)[CANDS], int n) {
+  for (int i = threadIdx.x; i < n; i += THREADS) {
+    const u64 own = cand[i];
+    const int c = (int)~(unsigned)own;
+    const T v = z[c];
+    int at = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) at += cand[j] > own;
+    if (at < a.k) {
+      a.ids[(long)row * a.k + at] = c;
+      a.logits[(long)row * a.k + at] = value<T>(v);
+    }
+  }
+}
 
 template <class T, int THREADS>
 __device__ __forceinline__ void pick_row(const TopArgs &a, int row, const T *__restrict__ z, const unsigned (&key)[PER],
@@ -304,7 +318,7 @@ __device__ __forceinline__ void pick_row(const TopArgs &a, int row, const T *__r
           if (c0 + j < a.vocab) v[j] = z[c0 + j];
 #pragma unroll
       for (int j = 0; j < COLS; ++j) {
-        const unsigned o = order(value<T>(v[j]));
+        const unsigned o = order<T>(value<T>(v[j]));
         if (c0 + j < a.vocab && o >= least) f(o, c0 + j);
       }
     }
@@ -331,18 +345,7 @@ __device__ __forceinline__ void pick_row(const TopArgs &a, int row, const T *__r
     __syncthreads();
     n = a.k;
   }
-  // each candidate's place is the number of those in front of it
-  for (int i = threadIdx.x; i < n; i += THREADS) {
-    const u64 own = cand[i];
-    const int c0 = (int)~(unsigned)own;
-    const T v = z[c0];
-    int at = 0;
-    for (int j = 0; j < n; ++j) at += cand[j] > own;
-    if (at < a.k) {
-      a.ids[(long)row * a.k + at] = c0;
-      a.logits[(long)row * a.k + at] = value<T>(v);
-    }
-  }
+  place<T, THREADS>(a, row, z, cand, n);
 }
 
 // A block a row, behind the scan.
@@ -386,14 +389,85 @@ __global__ void __launch_bounds__(256) k_top_row(const TopArgs a) {
   pick_row<T, 256>(a, row, z, key, pool);
 }
 
-// Rows from which on a block takes a whole one.
-constexpr int WHOLE_ROWS = 512;
+// Up to 16 THREADS columns, a block a row: the columns themselves stay in registers, without
+// groups (where k is near their number nearly all columns would be read again and sorted
+// out a second time).
+template <class T, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_top_small(const TopArgs a) {
+  __shared__ Pool p;
+  __shared__ float2 red[THREADS / 64];
+  const int row = blockIdx.x;
+  const T *z = static_cast<const T *>(a.z) + (long)row * a.ldz;
+  T v[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int at = threadIdx.x + THREADS * i;
+    v[i] = at < a.vocab ? z[at] : T();
+  }
+  unsigned key[PER];
+  float y[PER];
+  float2 s = make_float2(-FAR, 0.f);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const bool in = threadIdx.x + THREADS * i < a.vocab;
+    key[i] = in ? order<T>(value<T>(v[i])) : 0;  // (0 is below every value's number)
+    y[i] = in ? value<T>(v[i]) * a.scale : -INFINITY;
+    s.x = fmaxf(s.x, y[i]);
+  }
+  s.x = fminf(s.x, FAR);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) s.y += exp_of(y[i] - s.x);
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) s = meet(s, make_float2(__shfl_xor(s.x, o, 64), __shfl_xor(s.y, o, 64)));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  if (threadIdx.x == 0) p.count = 0;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < THREADS / 64; ++w) s = meet(s, red[w]);
+    a.lse[row] = s.x + log2f(s.y) * LN2;
+  }
+  auto columns = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (key[i]) f(key[i], (int)threadIdx.x + THREADS * i);
+  };
+  Cut c{0, 0}, ci{0, 0};
+  if (a.k < a.vocab) {
+    c = threshold<THREADS>([&](auto f) __attribute__((always_inline)) { columns([&](unsigned x, int) { f(x); }); }, a.k, p.pick);
+    if (c.want)
+      ci = threshold<THREADS>(
+          [&](auto f) __attribute__((always_inline)) { columns([&](unsigned x, int at) { if (x == c.t) f(~(unsigned)at); }); }, c.want, p.pick);
+  }
+  columns([&](unsigned x, int at) {
+    if (x > c.t || (x == c.t && (!c.want || ~(unsigned)at >= ci.t)))
+      p.cand[atomicAdd(&p.count, 1u)] = (u64)x << 32 | (unsigned)~at;
+  });
+  __syncthreads();
+  place<T, THREADS>(a, row, z, p.cand, a.k);
+}
+
+// Without groups: up to 4,096 columns (2,000 x 4,000 fp32, k = 20: 19.4 us, with them 23.4),
+// and up to 16,384 where there are fewer groups than twice k.
+inline bool is_small(const TopArgs &a) {
+  return a.vocab <= 256 * PER || (a.vocab <= 1024 * PER && a.groups < 2 * a.k);
+}
+
+// Whether a block takes a whole row: with many rows, or some of moderate length (the parts'
+// way / this, us: 1,024 x 151,936 bf16 89.8 / 71.9, 300 38.5 / 50.1; 400 x 32,000 bf16 23.0 /
+// 19.6, 200 fp32 17.4 / 14.9).
+inline bool is_whole(const TopArgs &a) {
+  return a.groups <= 256 * PER && (a.rows >= 512 || (a.rows >= 64 && a.vocab <= 65536));
+}
 
 template <class T>
 void launch(const TopArgs &a, hipStream_t st) {
-  // (1,024 threads hold the groups of any vocabulary, 256 those of 262,144 columns)
-  const bool narrow = a.groups <= 256 * PER;
-  if (narrow && a.rows >= WHOLE_ROWS) {
+  if (is_small(a)) {
+    if (a.vocab <= 256 * PER) k_top_small<T, 256><<<a.rows, 256, 0, st>>>(a);
+    else k_top_small<T, 1024><<<a.rows, 1024, 0, st>>>(a);
+    SEG_LAUNCH_CHECK();
+    return;
+  }
+  if (is_whole(a)) {
     const size_t lds = (size_t)a.groups * 4;
     if ((double)a.rows * a.vocab * sizeof(T) > STREAM_BYTES) k_top_row<T, true><<<a.rows, 256, lds, st>>>(a);
     else k_top_row<T, false><<<a.rows, 256, lds, st>>>(a);
@@ -402,7 +476,8 @@ void launch(const TopArgs &a, hipStream_t st) {
   }
   k_top_scan<T><<<(unsigned)((long)a.rows * a.parts), 256, 0, st>>>(a);
   SEG_LAUNCH_CHECK();
-  if (narrow) k_top_pick<T, 256><<<a.rows, 256, 0, st>>>(a);
+  // (1,024 threads hold the groups of any vocabulary, 256 those of 262,144 columns)
+  if (a.groups <= 256 * PER) k_top_pick<T, 256><<<a.rows, 256, 0, st>>>(a);
   else k_top_pick<T, 1024><<<a.rows, 1024, 0, st>>>(a);
   SEG_LAUNCH_CHECK();
 }

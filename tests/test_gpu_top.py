@@ -54,7 +54,9 @@ def _z(rows, vocab, dtype, seed=0, std=2.5):
 @pytest.mark.parametrize("rows,vocab,k", [(1, 1, 1), (2, 5, 5), (3, 63, 20), (4, 64, 64), (2, 65, 7), (5, 256, 256), (3, 1001, 1),
                                           (7, 1001, 200), (2, 16384, 256), (3, 16385, 256), (37, 32000, 64), (1, 151936, 20),
                                           (2, 151936, 256), (300, 5003, 33), (1, 1 << 20, 50), (3, 300000, 100),
-                                          # a block a row
+                                          # without groups, and a block a row with them
+                                          (4, 4096, 256), (3, 4097, 70), (2, 16384, 1), (5, 12000, 255), (530, 4500, 40), (530, 16384, 256),
+                                          (600, 4000, 16), (70, 5000, 9), (64, 65536, 32), (66, 65537, 32), (63, 20000, 100),
                                           (512, 40, 7), (600, 1001, 33), (515, 5000, 256), (700, 2048, 1), (513, 20001, 64)])
 def test_columns_and_values(rows, vocab, k, dtype):
     say(rows, vocab, k, dtype)
