@@ -1,16 +1,19 @@
 // The k largest logits of each row, with their columns, and the row's log-sum-exp.
 //
 // Order: by value, descending, then by column, ascending; NaN counts as larger than
-// all numbers, -0 as 0.  Two kernels:
+// all numbers, -0 as 0.  Two steps:
 //
-//   k_top_scan   one pass over the logits: running maximum and sum of the softmax, and
-//                the largest of every 64 columns (a group) as a whole number in order;
-//   k_top_pick   of each row: the k largest groups (ties: the first ones), and of their
-//                columns the k largest.
+//   scan   one pass over the logits: running maximum and sum of the softmax, and the
+//          largest of every 64 columns (a group) as a whole number in order;
+//   pick   of each row: the k largest groups (ties: the first ones), and of their columns
+//          the k largest;
+//
+// as two kernels over parts of rows and over rows (k_top_scan, k_top_pick) or as one over
+// rows (k_top_row).  Small vocabularies take one step without groups (k_top_small).
 //
 // The k largest logits lie in the k largest groups: a column outside them is preceded
 // by the largest of each of those groups, which is larger, or as large and further to
-// the front, as the groups are runs of columns.  So the second kernel reads k groups
+// the front, as the groups are runs of columns.  So the second step reads k groups
 // again and not the row, and no order of the values makes it do more.
 #include <algorithm>
 #include <cmath>
@@ -448,26 +451,26 @@ __global__ void __launch_bounds__(THREADS) k_top_small(const TopArgs a) {
 
 // Without groups: up to 4,096 columns (2,000 x 4,000 fp32, k = 20: 19.4 us, with them 23.4),
 // and up to 16,384 where there are fewer groups than twice k.
-inline bool is_small(const TopArgs &a) {
-  return a.vocab <= 256 * PER || (a.vocab <= 1024 * PER && a.groups < 2 * a.k);
+inline bool is_small(int vocab, int k) {
+  return vocab <= 256 * PER || (vocab <= 1024 * PER && (vocab + GROUP - 1) / GROUP < 2 * k);
 }
 
 // Whether a block takes a whole row: with many rows, or some of moderate length (the parts'
 // way / this, us: 1,024 x 151,936 bf16 89.8 / 71.9, 300 38.5 / 50.1; 400 x 32,000 bf16 23.0 /
 // 19.6, 200 fp32 17.4 / 14.9).
-inline bool is_whole(const TopArgs &a) {
-  return a.groups <= 256 * PER && (a.rows >= 512 || (a.rows >= 64 && a.vocab <= 65536));
+inline bool is_whole(int rows, int vocab) {
+  return vocab <= 256 * PER * GROUP && (rows >= 512 || (rows >= 64 && vocab <= 65536));
 }
 
 template <class T>
 void launch(const TopArgs &a, hipStream_t st) {
-  if (is_small(a)) {
+  if (is_small(a.vocab, a.k)) {
     if (a.vocab <= 256 * PER) k_top_small<T, 256><<<a.rows, 256, 0, st>>>(a);
     else k_top_small<T, 1024><<<a.rows, 1024, 0, st>>>(a);
     SEG_LAUNCH_CHECK();
     return;
   }
-  if (is_whole(a)) {
+  if (is_whole(a.rows, a.vocab)) {
     const size_t lds = (size_t)a.groups * 4;
     if ((double)a.rows * a.vocab * sizeof(T) > STREAM_BYTES) k_top_row<T, true><<<a.rows, 256, lds, st>>>(a);
     else k_top_row<T, false><<<a.rows, 256, lds, st>>>(a);
@@ -495,7 +498,7 @@ TopWs top_ws(int rows, int vocab) {
   w.span = SPAN;
   while (w.span > 2048 && (long)rows * ((vocab + w.span - 1) / w.span) < 256) w.span /= 2;
   w.parts = (vocab + w.span - 1) / w.span;
-  w.gmax = 0;
+  if (is_small(vocab, 1) || is_whole(rows, vocab)) return w;  // none
   w.stats = align_up((size_t)rows * w.groups * 4);
   w.total = w.stats + align_up((size_t)rows * w.parts * sizeof(float2));
   return w;
@@ -525,12 +528,13 @@ extern "C" seg_status seg_top_logits(int32_t rows, int32_t vocab, int32_t k, seg
     if (rows == 0) return;
     const TopWs w = top_ws(rows, vocab);
     SEG_CHECK(ws_bytes >= w.total, SEG_ERR_WORKSPACE, "workspace of %zu bytes < required %zu", ws_bytes, w.total);
-    SEG_CHECK(z && ids && logits && lse && ws, SEG_ERR_ARG, "a tensor pointer is NULL");
+    SEG_CHECK(z && ids && logits && lse && (ws || w.total == 0), SEG_ERR_ARG, "a tensor pointer is NULL");
     const size_t e = dt == SEG_BF16 ? 2 : 4;
     SEG_CHECK(reinterpret_cast<uintptr_t>(z) % e == 0, SEG_ERR_ARG, "z is not aligned to its type");
-    SEG_CHECK(reinterpret_cast<uintptr_t>(ws) % 16 == 0, SEG_ERR_UNSUPPORTED, "the workspace is not on a 16-byte boundary");
+    SEG_CHECK(w.total == 0 || reinterpret_cast<uintptr_t>(ws) % 16 == 0, SEG_ERR_UNSUPPORTED, "the workspace is not on a 16-byte boundary");
     SEG_CHECK((double)rows * w.parts <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "too many rows for one launch");
-    check_apart({{ids, (size_t)rows * k * 4}, {logits, (size_t)rows * k * 4}, {lse, (size_t)rows * 4}, {ws, w.total}},
+    check_apart({{ids, (size_t)rows * k * 4}, {logits, (size_t)rows * k * 4}, {lse, (size_t)rows * 4},
+                 {w.total ? ws : nullptr, w.total}},
                 {{z, ((size_t)(rows - 1) * ldz + vocab) * e}});
     char *base = static_cast<char *>(ws);
     const TopArgs a{z, ldz, rows, vocab, k, w.groups, w.parts, w.span, scale, reinterpret_cast<unsigned *>(base + w.gmax),

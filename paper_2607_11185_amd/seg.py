@@ -871,7 +871,7 @@ def seg_fp8_gemm(a: Fp8, b: Fp8, dtype=None, y=None, ws=None):
 def top_logits_workspace(rows: int, vocab: int, device):
     import torch
     n = _lib.lib().seg_top_logits_workspace_bytes(rows, vocab)
-    return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
 def seg_top_logits(z, k: int, scale: float = 1.0, out: Optional[dict] = None, ws=None) -> dict:
@@ -893,8 +893,8 @@ def seg_top_logits(z, k: int, scale: float = 1.0, out: Optional[dict] = None, ws
     _device(z, out["ids"], out["logits"], out["lse"], ws)
     with _on(dev):
         check(_lib.lib().seg_top_logits(rows, vocab, k, dt, z.data_ptr(), _rows(z), scale, out["ids"].data_ptr(),
-                                        out["logits"].data_ptr(), out["lse"].data_ptr(), ws.data_ptr(), ws.numel(),
-                                        _current(dev)))
+                                        out["logits"].data_ptr(), out["lse"].data_ptr(), _ptr(ws),
+                                        0 if ws is None else ws.numel(), _current(dev)))
     return out
 
 

@@ -96,14 +96,14 @@ def test_binding_refuses():
 
 # ---------------------------------------------------------------- top logits
 
-def _top(rows=4, vocab=1000, k=10, dt=0, z=MB, ldz=1000, scale=1.0, ids=2 * MB, logits=3 * MB, lse=4 * MB, ws=8 * MB,
+def _top(rows=4, vocab=5000, k=10, dt=0, z=MB, ldz=5000, scale=1.0, ids=2 * MB, logits=3 * MB, lse=4 * MB, ws=8 * MB,
          ws_bytes=1 << 40):
     return _lib_or_skip().seg_top_logits(rows, vocab, k, dt, z, ldz, scale, ids, logits, lse, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("kw,want", [
-    (dict(dt=2), UNS), (dict(rows=-1), ARG), (dict(vocab=0), ARG), (dict(k=0), ARG), (dict(k=1001), ARG), (dict(k=257), UNS),
-    (dict(vocab=(1 << 20) + 1, ldz=2 << 20), CAP), (dict(rows=(1 << 20) + 1), CAP), (dict(ldz=999), ARG),
+    (dict(dt=2), UNS), (dict(rows=-1), ARG), (dict(vocab=0), ARG), (dict(k=0), ARG), (dict(k=5001), ARG), (dict(k=257), UNS),
+    (dict(vocab=(1 << 20) + 1, ldz=2 << 20), CAP), (dict(rows=(1 << 20) + 1), CAP), (dict(ldz=4999), ARG),
     (dict(scale=float("nan")), ARG), (dict(scale=float("inf")), ARG), (dict(ws_bytes=100), WS), (dict(z=None), ARG), (dict(ids=None), ARG),
     (dict(logits=None), ARG), (dict(lse=None), ARG), (dict(ws=None), ARG), (dict(z=MB + 1), ARG), (dict(z=MB + 2, dt=1), ARG),
     (dict(ws=8 * MB + 8), UNS), (dict(ids=MB + 7996), ARG), (dict(lse=3 * MB + 156), ARG), (dict(logits=8 * MB), ARG),
@@ -118,7 +118,9 @@ def test_top_logits_of_nothing_and_sizes():
     assert _top(rows=0, z=None, ids=None, logits=None, lse=None, ws=None, ws_bytes=0) == _lib.SEG_OK
     for bad in ((-1, 4), (4, 0), ((1 << 20) + 1, 4), (4, (1 << 20) + 1)):
         assert L.seg_top_logits_workspace_bytes(*bad) == 0
-    assert L.seg_top_logits_workspace_bytes(1, 1) > 0
+    assert L.seg_top_logits_workspace_bytes(4, 5000) > 0 and L.seg_top_logits_workspace_bytes(511, 151936) > 0
+    # one kernel, no workspace: small vocabularies and many rows
+    assert L.seg_top_logits_workspace_bytes(4, 4096) == L.seg_top_logits_workspace_bytes(512, 151936) == 0
 
 
 # -------------------------------------------------------------- distillation

@@ -298,3 +298,21 @@ def test_large_outputs_past_32_bits():
     part = S.Fp8(a.code[at].contiguous(), torch.nn.functional.pad(a.exp[:, at], (0, 10)).contiguous(), cols, 1)
     ref, tol = _product(part, b)
     _within(y[at], ref, tol + 2.0 ** -8 * (np.abs(ref) + tol), "rows")
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_packing_past_32_bits(block_rows):
+    """Rows behind 2^32 bytes of x and 2^31 codes."""
+    import torch
+    rows, cols = 600001, 4100
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    tail = torch.randn(130, cols, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    at = rows - 130 if block_rows == 1 else (rows - 1) // 128 * 128 - 65
+    x[at:at + 130] = tail[:rows - at]
+    x[7, 4099] = 3.0
+    a = S.seg_fp8_pack(x, block_rows)
+    first = at // 128 * 128
+    want = S.seg_fp8_unpack(S.seg_fp8_pack(x[first:].contiguous(), block_rows))
+    got = S.seg_fp8_unpack(a)
+    assert torch.equal(got[first:], want) and bool(want[at - first:].any())
+    assert float(got[7, 4099]) == 3.0 and int(got[:first].count_nonzero()) == 1
