@@ -370,8 +370,10 @@ def seg_layer_bwd(lay: Layout, cfg: LayerCfg, w: dict, x, saved: dict, dy, dx=No
 def _device(*tensors):
     """The GPU that all the tensors (None: left out) are on."""
     dev = tensors[0].device
+    assert dev.type == "cuda", f"tensors on {dev}"
+    index = dev.index
     for t in tensors:
-        assert t is None or (t.is_cuda and t.device == dev), f"tensors on {dev} and {t.device}"
+        assert t is None or t.get_device() == index, f"tensors on {dev} and {t.device}"
     return dev
 
 
