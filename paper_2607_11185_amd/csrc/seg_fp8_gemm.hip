@@ -165,10 +165,17 @@ struct Scales {
   }
 };
 
-template <int TM, int BN, class T>
-__global__ void __launch_bounds__(THREADS, BN == 128 ? 4 : 2) k_gemm8(const Gemm8 g) {
-  constexpr int BM = gemm::bm_of(TM), SA = BM * STEP, SB = BN * STEP, LDS_B = SA * gemm::SLOTS_A;
-  __shared__ __attribute__((aligned(1024))) char lds[LDS_B + SB * gemm::SLOTS_B];
+// What a grid with a block a CU is given instead of a second block: four slots for each
+// operand, and the scales of the block's steps in LDS before the first of them.  (A scale
+// from memory is waited for with all loads before it, also those of later steps.)
+constexpr int DEEP_STEPS = 128;
+
+template <int TM, int BN, bool DEEP, class T>
+__global__ void __launch_bounds__(THREADS, BN == 128 && !DEEP ? 4 : 2) k_gemm8(const Gemm8 g) {
+  constexpr int BM = gemm::bm_of(TM), SA = BM * STEP, SB = BN * STEP;
+  constexpr int SLOTS_A = DEEP ? 4 : gemm::SLOTS_A, SLOTS_B = DEEP ? 4 : gemm::SLOTS_B;
+  constexpr int LDS_B = SA * SLOTS_A, LDS_S = LDS_B + SB * SLOTS_B;  // scales: [step][BM + BN]
+  __shared__ __attribute__((aligned(1024))) char lds[LDS_S + (DEEP ? DEEP_STEPS * (BM + BN) : 0)];
   int idx = gemm::xcd_index(g.tiles * g.splits);
   if (idx >= g.tiles * g.splits) return;
   const int split = idx / g.tiles;
@@ -193,8 +200,6 @@ __global__ void __launch_bounds__(THREADS, BN == 128 ? 4 : 2) k_gemm8(const Gemm
   fB.init(LDS_B, wc, lane);
   Scales<FA> ea;
   Scales<FB> eb;
-  ea.init(g.a, m0 + wr, col, s0);
-  eb.init(g.b, n0 + wc, col, s0);
   unsigned sa_next[Scales<FA>::N], sb_next[1], sa[Scales<FA>::N], sb[1];
 
   f32x4 acc[FA][FB];
@@ -214,38 +219,63 @@ __global__ void __launch_bounds__(THREADS, BN == 128 ? 4 : 2) k_gemm8(const Gemm
   auto load = [&](int slot, int j) __attribute__((always_inline)) {
     if (LA == LB || j < LA || grp == 1) ldr.load(ring + slot, j, w4);
   };
-  if (nk > 0) {
+  if (!DEEP && nk > 0) {
+    ea.init(g.a, m0 + wr, col, s0);
+    eb.init(g.b, n0 + wc, col, s0);
     ea.fetch(sa_next);
     eb.fetch(sb_next);
     ea.take(sa_next, sa);
     eb.take(sb_next, sb);
   }
-  prep();
+  // the first SLOTS - 1 steps of the group's operand; the first of them has landed
 #pragma unroll
-  for (int j = 0; j < LB; ++j) load(0, j);
-  if (grp == 0) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  } else {
+  for (int d = 0; d + 1 < (SLOTS_A > SLOTS_B ? SLOTS_A : SLOTS_B); ++d) {
+    if (grp == 0 && d + 1 >= SLOTS_A) continue;
     prep();
 #pragma unroll
-    for (int j = 0; j < LB; ++j) load(SB, j);
-    if (nk > 0) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LB) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    for (int j = 0; j < LB; ++j) load(d * (grp == 0 ? SA : SB), j);
+  }
+  if constexpr (DEEP) {
+    for (int i = threadIdx.x; i < nk * ((BM + BN) / 16); i += THREADS) {
+      const int step = i / ((BM + BN) / 16), at = i % ((BM + BN) / 16) * 16;
+      const Operand &o = at < BM ? g.a : g.b;
+      const int row = at < BM ? m0 + at : n0 + at - BM;
+      const uint8_t *p = o.exp + (long)(s0 + step) * o.lde;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (o.square) {
+        v.x = v.y = v.z = v.w = row < o.rows ? p[row / fp8::BLOCK] * 0x01010101u : 0u;
+      } else if (row < o.lde) {
+        v = *reinterpret_cast<const uint4 *>(p + row);
+      }
+      *reinterpret_cast<uint4 *>(lds + LDS_S + step * (BM + BN) + at) = v;
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  } else if (grp == 0 || nk <= 0) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  } else {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LB) : "memory");
   }
   __builtin_amdgcn_s_barrier();
   GEMM_FENCE();
   if (grp == 1 && nk > 0) __builtin_amdgcn_s_barrier();  // half a step behind group 0
   GEMM_FENCE();
 
-  // barriers and waits: as in k_gemm; the scales of step t + 1 are fetched before the
-  // direct loads of step t's phase go out and waited for when its products are issued
-  int slot_b = 0, slot_b2 = 2 * SB;  // of steps t and t + 2
+  // Barriers and waits are those of k_gemm: before the barrier that opens group 0's reads
+  // of step t + 1, both groups have waited for their loads of that step, and those of the
+  // SLOTS - 2 steps behind it stay in flight.  The scales of step t + 1 are fetched before
+  // the direct loads of step t's phase go out and waited for when its products are issued
+  // (DEEP: read with the fragments).
+  int slot_a = 0, slot_b = 0, old_a = (SLOTS_A - 1) * SA, old_b = (SLOTS_B - 1) * SB;  // of steps t and t - 1
 #pragma unroll 1
   for (int t = 0; t < nk; ++t) {
-    const int slot_a = (t & 1) * SA;
-    const int slot_n = grp == 0 ? SA - slot_a : slot_b2;
+    const int slot_n = grp == 0 ? old_a : old_b;
     bf16x8 a[2][FA], b[2][FB];
-    if (t + 1 < nk) {
+    if constexpr (DEEP) {
+      const char *sc = lds + LDS_S + t * (BM + BN);
+      static_assert(!DEEP || (FA == 4 && FB == 2), "a word of scales of a, a half of b");
+      sa[0] = *reinterpret_cast<const unsigned *>(sc + wr + FA * col);
+      sb[0] = *reinterpret_cast<const unsigned short *>(sc + BM + wc + FB * col);
+    } else if (t + 1 < nk) {
       ea.fetch(sa_next);
       eb.fetch(sb_next);
     }
@@ -262,12 +292,8 @@ __global__ void __launch_bounds__(THREADS, BN == 128 ? 4 : 2) k_gemm8(const Gemm
         else a[kk][f - FB] = fA.read(lds, slot_a, kk, f - FB);
       }
     }
-    if (grp == 0)
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    else if (t + 2 < nk)
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LB) : "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    if (grp == 0) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS_B - 2) * LB) : "memory");
     __builtin_amdgcn_s_barrier();
     GEMM_FENCE();
     __builtin_amdgcn_sched_barrier(0);
@@ -288,16 +314,19 @@ __global__ void __launch_bounds__(THREADS, BN == 128 ? 4 : 2) k_gemm8(const Gemm
       for (int j = 0; j < FB; j += 2) asm volatile("" : "+v"(acc[i][j]), "+v"(acc[i][j + 1]));
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
-    slot_b = slot_b == 2 * SB ? 0 : slot_b + SB;
-    slot_b2 = slot_b2 == 2 * SB ? 0 : slot_b2 + SB;
-    if (grp == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (t + 1 < nk) {
+    old_a = slot_a;
+    old_b = slot_b;
+    slot_a = slot_a == (SLOTS_A - 1) * SA ? 0 : slot_a + SA;
+    slot_b = slot_b == (SLOTS_B - 1) * SB ? 0 : slot_b + SB;
+    if (grp == 0) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS_A - 2) * LA) : "memory");
+    if (!DEEP && t + 1 < nk) {
       ea.take(sa_next, sa);
       eb.take(sb_next, sb);
     }
     if (grp == 0 || t + 1 < nk) __builtin_amdgcn_s_barrier();
     GEMM_FENCE();
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives the block
   settled(acc);
   const int n = n0 + wc + 4 * FB * lg;
   if (n >= g.b.rows) return;
@@ -472,27 +501,40 @@ long ld_part(int outs) { return (outs + 15) / 16 * 16; }
 bool sizes_ok(int32_t rows, int32_t outs, int32_t cols) {
   return rows >= 0 && outs >= 1 && cols >= 1 && rows <= (1 << 20) && outs <= (1 << 20) && cols <= (1 << 20);
 }
+// 256 x 256, 128 x 256, 128 x 128 with two blocks a CU, or with one (DEEP)
+enum Tiles { WIDE, HALF, TWO, ONE };
 struct Choice {
-  int tm, bn, parts, part;
+  Tiles tiles;
+  int parts, part;
 };
-long tiles_of(int rows, int outs, int tm, int bn) {
-  return ((rows + 64 * tm - 1) / (64 * tm)) * (((long)outs + bn - 1) / bn);
+long tiles_of(int rows, int outs, Tiles v) {
+  const long bm = v == WIDE ? 256 : 128, bn = v == WIDE || v == HALF ? 256 : 128;
+  return (rows + bm - 1) / bm * ((outs + bn - 1) / bn);
 }
+
 // How a product is launched, by the time that each way is expected to take: us of blocks
 // that fill u of the chip's CUs, by steps s of 128 columns; a full chip's clocks are lower.
 //   256 x 256 tiles: 6 + s (1.06 + 0.49 u) a round;  128 x 256: 4 + s (0.8 + 0.3 u);
-//   128 x 128, two of them on a CU: 4 + 0.65 s for the first 256, another s (0.3 + 0.15 u)
-//   with the second;
-// and for parts of K their fp32 sums, 4.5 + 0.3 a MB.  Measured / expected over 65 to 2,048
-// rows, us (best of the three, parts of K in brackets): 128 x 18,944 x 3,584 (rows, outs,
-// cols) 30.4 / 22.2, 512 45.9 / 42.4, 1,500 94.4 / 94.4; 256 x 3,584 x 18,944 (8) 41.4 / 37.3,
-// 1,024 (4) 81 / 81; 300 x 5,504 x 2,048 14.4 / 14.4, 2,048 29.2 / 28.4.  One kind of tile for
-// all: 41.7, 45.9, 94.4; 178, 176; 24.2, 29.2 (256 x 256, whole).
-double expect(int tm, int bn, long blocks, double s) {
-  const long slots = bn == 128 ? 512 : 256, full = blocks / slots, rest = blocks % slots;
+//   128 x 128, two of them on a CU: 4 + s (0.6 + 0.1 u) for the first 256, another s (0.25 +
+//   0.2 u) with the second; DEEP, for one round alone: 4 + s (0.52 + 0.12 u);
+// and for parts of K their fp32 sums, 4.5 + 0.3 a MB.  Measured, us, rows x outs x cols (parts
+// of K in brackets), 256 x 256 tiles / 128 x 256 / 128 x 128 / DEEP, the one taken first:
+//   128 x 18,944 x 3,584     DEEP 26.2; 41.6 / 40.4 / 30.5
+//   256 x 3,584 x 18,944     DEEP (4) 37.2; (8) 48.9 / (8) 43.5 / (8) 41.6
+//   512 x 5,504 x 2,048      DEEP 14.0; 24.8 / 18.3 / 14.9
+//   1,024 x 5,504 x 2,048    128 x 128 20.0; 25.7 / 20.3 / - / 25.6
+//   1,500 x 5,001 x 2,040    128 x 256 22.9; 29.0 / - / 23.5 / 28.4
+//   1,500 x 18,944 x 3,584   256 x 256 97.4; - / 128 / 128 / 140
+// (8,192 x 18,944 x 3,584 in two launches, nine rounds and the rest in quarters of tiles:
+// 478, in one 470.)
+double expect(int v, long blocks, double s) {
+  const long slots = v == TWO ? 512 : 256, full = blocks / slots, rest = blocks % slots;
   auto round = [&](double n) {  // n blocks, at most the slots
-    if (bn == 128) return 4 + s * (0.65 + (n > 256 ? 0.3 + 0.15 * (n - 256) / 256 : 0.0));
-    return tm == 2 ? 4 + s * (0.8 + 0.3 * n / 256) : 6 + s * (1.06 + 0.49 * n / 256);
+    const double u = std::min(n, 256.0) / 256, second = std::max(n - 256, 0.0) / 256;
+    return v == WIDE ? 6 + s * (1.06 + 0.49 * u)
+         : v == HALF ? 4 + s * (0.8 + 0.3 * u)
+         : v == TWO ? 4 + s * (0.6 + 0.1 * u + (second > 0 ? 0.25 + 0.2 * second : 0))
+                    : 4 + s * (0.52 + 0.12 * u);
   };
   return full * round((double)slots) + (rest ? round((double)rest) : 0.0);
 }
@@ -502,15 +544,15 @@ Choice choice_of(int rows, int outs, int cols) {
   const double mb = (double)rows * ld_part(outs) * 4e-6;
   Choice best{};
   double best_us = 0;
-  for (int v = 0; v < 3; ++v) {
-    const int tm = v == 0 ? 4 : 2, bn = v == 2 ? 128 : 256;
-    const long tiles = tiles_of(rows, outs, tm, bn);
+  for (Tiles v : {WIDE, HALF, TWO, ONE}) {
+    const long tiles = tiles_of(rows, outs, v);
     for (int p = 1; p <= 16; ++p) {
       const int per = (steps + p - 1) / p;
       if (p > 1 && (per < 2 || (p - 1) * per >= steps || tiles * p > 2048)) continue;
-      const double us = expect(tm, bn, tiles * p, per) + (p > 1 ? 4.5 + 0.3 * mb * p : 0.0);
+      if (v == ONE && (tiles * p > 256 || per > DEEP_STEPS)) continue;
+      const double us = expect(v, tiles * p, per) + (p > 1 ? 4.5 + 0.3 * mb * p : 0.0);
       if (best_us == 0 || us < best_us) {
-        best = Choice{tm, bn, p, per};
+        best = Choice{v, p, per};
         best_us = us;
       }
     }
@@ -559,11 +601,14 @@ void few(const Gemm8 &g, const Few &f, hipStream_t st) {
 
 template <class T>
 void many(Gemm8 g, const Choice &c, hipStream_t st) {
-  g.tiles = (int)tiles_of(g.a.rows, g.b.rows, c.tm, c.bn);
+  g.tiles = (int)tiles_of(g.a.rows, g.b.rows, c.tiles);
   const unsigned grid = (unsigned)(((long)g.tiles * g.splits + 7) / 8 * 8);
-  if (c.bn == 128) k_gemm8<2, 128, T><<<grid, THREADS, 0, st>>>(g);
-  else if (c.tm == 2) k_gemm8<2, 256, T><<<grid, THREADS, 0, st>>>(g);
-  else k_gemm8<4, 256, T><<<grid, THREADS, 0, st>>>(g);
+  switch (c.tiles) {
+    case WIDE: k_gemm8<4, 256, false, T><<<grid, THREADS, 0, st>>>(g); break;
+    case HALF: k_gemm8<2, 256, false, T><<<grid, THREADS, 0, st>>>(g); break;
+    case TWO: k_gemm8<2, 128, false, T><<<grid, THREADS, 0, st>>>(g); break;
+    case ONE: k_gemm8<2, 128, true, T><<<grid, THREADS, 0, st>>>(g); break;
+  }
   SEG_LAUNCH_CHECK();
 }
 
@@ -572,8 +617,8 @@ void many(Gemm8 g, const Choice &c, hipStream_t st) {
 
 using namespace seg;
 
-// How a product is launched (for tests): out = {rows of a tile / 64, columns, parts of K}, or
-// for few rows {16-row blocks of a, of b, - waves}.
+// How a product is launched (for tests): out = {Tiles, 0, parts of K}, or for few rows
+// {16-row blocks of a, of b, - waves}.
 extern "C" void seg_fp8_gemm_choice(int32_t rows, int32_t outs, int32_t cols, int32_t *out) {
   if (rows <= FEW) {
     const Few f = few_choice(rows, outs, cols);
@@ -583,8 +628,8 @@ extern "C" void seg_fp8_gemm_choice(int32_t rows, int32_t outs, int32_t cols, in
     return;
   }
   const Choice c = choice_of(rows, outs, cols);
-  out[0] = c.tm;
-  out[1] = c.bn;
+  out[0] = c.tiles;
+  out[1] = 0;
   out[2] = c.parts;
 }
 

@@ -169,7 +169,8 @@ SHAPES = [(1, 1, 1), (1, 16, 128), (1, 300, 1000), (3, 33, 129), (16, 64, 256), 
           (128, 640, 9001), (2, 40, 16384),
           # each kernel for few rows, and each kind of tile
           (5, 4200, 2200), (9, 48, 2304), (20, 4200, 300), (25, 100, 1500), (40, 100, 1500), (50, 4200, 700), (47, 16500, 300),
-          (300, 12000, 128), (400, 19000, 128), (65, 12000, 4096), (130, 5000, 16384)]
+          (300, 12000, 128), (400, 19000, 128), (65, 12000, 4096), (130, 5000, 16384), (130, 19000, 128), (65, 5504, 16384),
+          (700, 5504, 128), (1400, 1300, 16384), (257, 200, 17000)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -196,8 +197,8 @@ def test_every_way_of_cutting():
         assert (L.seg_fp8_gemm_workspace_bytes(*s) > 0) == (out[2] > 1)
     # 16-row blocks of a, of b, waves
     assert got >= {(1, 1, -16), (1, 1, -8), (2, 1, -8), (2, 2, -4), (4, 1, -8), (4, 2, -8), (4, 4, -4)}, got
-    # rows of a tile / 64, columns, whole or in parts
-    assert got >= {(4, 256, 1), (2, 256, 1), (2, 128, 1), (4, 256, 2), (2, 256, 2), (2, 128, 2)}, got
+    # 256 x 256 tiles, 128 x 256, 128 x 128 two and one to a CU, whole and in parts of K
+    assert got >= {(v, 0, p) for v in range(4) for p in (1, 2)}, got
 
 
 @pytest.mark.parametrize("shape", [(40, 512, 4096), (513, 1024, 4096), (2, 256, 8192)], ids=lambda s: "x".join(map(str, s)))
