@@ -59,6 +59,7 @@ __device__ __forceinline__ unsigned order(float x) {
   if (x != x) u = 0xffffffffu;
   return sizeof(T) == 2 ? u >> 16 : u;
 }
+
 struct TopArgs {
   const void *z;
   long ldz;
