@@ -9,7 +9,7 @@
 // over zT with one factor a row, and k places a row that are written again behind it.
 // Pipeline:
 //   1. hb = the rows of h that are used, as bf16;
-//   2. zT[v][r] (MFMA, fp32 out) with per-(row, 128-vocab slab) max / sum-exp;
+//   2. zT[v][r] (MFMA, fp32 out) with per-(row, slab of the vocabulary) max / sum-exp;
 //   3. per row: LSE, p, the logits at the k columns, loss, the factor sum p, and the
 //      gradients at the k columns;
 //   4. dzT = factor q as bf16, then the k places of each row;
@@ -49,6 +49,126 @@ __global__ void __launch_bounds__(256) k_distill_prep(const TI *__restrict__ h, 
   if constexpr (sizeof(TI) == 4) {
     for (long i = at; i < w8; i += step) *reinterpret_cast<u16x8 *>(wb + i * 8) = load8(w + i * 8, wvec);
   }
+}
+
+// The logits of few rows (16 NB at most), where the projection's bytes are the work and a
+// tile of the shared product would be mostly empty: a block takes 32 rows of the
+// vocabulary, its waves every WAVES-th step of 64 of the hidden width, and their sums are
+// added up in LDS, in order (as the gated block's kernel for some tens of rows: 16 bytes a
+// lane in whole 128-byte lines, turned in the wave's own LDS).  It writes what EpiLogits
+// writes, with slabs of 32.  Measured with events around the launch, us, x 1,032 x 1,472: 25
+// rows 7.5, 100 rows by the shared product 27.6; x 2,048 x 32,000: 16 / 32 / 64 rows 26.0 /
+// 28.5 / 38.0, 65 rows 44.2; x 3,584 x 151,936: 24 / 64 rows 273 / 323, 65 rows 334.
+constexpr int FEW = 64, FEW_SLAB = 32;
+
+template <int NB, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, NB < 4 ? 4 : 2) k_logits_few(const unsigned short *__restrict__ w,
+                                                                         const unsigned short *__restrict__ hb, int V,
+                                                                         int R, int Rp, int H, float scale,
+                                                                         float *__restrict__ zt,
+                                                                         float2 *__restrict__ stats) {
+  constexpr int ROWS = 16 * (NB > 2 ? NB : 2), STAGE = WAVES * ROWS * 8, SUMS = WAVES * 2 * NB * 64;
+  __shared__ __attribute__((aligned(1024))) f32x4 lds[STAGE > SUMS ? STAGE : SUMS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, lg = lane >> 4, lr = lane >> 3, lc = lane & 7;
+  const int v0 = blockIdx.x * FEW_SLAB;
+  const unsigned short *wp = w + (long)v0 * H;
+  unsigned woff[4], xoff[2 * NB];
+  bool xin[2 * NB];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) woff[i] = (unsigned)min(8 * i + lr, V - 1 - v0) * (unsigned)H + 8 * lc;
+#pragma unroll
+  for (int i = 0; i < 2 * NB; ++i) {
+    xin[i] = 8 * i + lr < R;
+    xoff[i] = (unsigned)(8 * i + lr) * (unsigned)H + 8 * lc;
+  }
+  bf16x8 wv[4], xv[2 * NB];
+  auto load = [&](int k) __attribute__((always_inline)) {
+    const bool in = k + 8 * lc < H;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      wv[i] = in ? *reinterpret_cast<const bf16x8 *>(wp + k + woff[i]) : bf16x8{};
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i)
+      xv[i] = in && xin[i] ? *reinterpret_cast<const bf16x8 *>(hb + k + xoff[i]) : bf16x8{};
+  };
+  f32x4 acc[2][NB];
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int n = 0; n < NB; ++n) acc[b][n] = f32x4{};
+  bf16x8 *stage = reinterpret_cast<bf16x8 *>(lds) + wave * (ROWS * 8);
+  bf16x8 *to = stage + lr * 8 + (lc ^ lr);
+  const bf16x8 *from = stage + r * 8;
+  int k = wave * 64;
+  load(k);
+  for (; k < H; k += 64 * WAVES) {
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) to[64 * i] = xv[i];
+    __builtin_amdgcn_wave_barrier();
+    bf16x8 cx[2][NB];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int n = 0; n < NB; ++n) cx[h][n] = from[n * 128 + ((4 * h + lg) ^ (r & 7))];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to[64 * i] = wv[i];
+    __builtin_amdgcn_wave_barrier();
+    load(k + 64 * WAVES);
+    // rows of the vocabulary of block b against rows of h of block n: a lane holds row 16 n +
+    // lane % 16, vocabulary rows 16 b + 4 (lane / 16) .. + 3
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const bf16x8 cw = from[b * 128 + ((4 * h + lg) ^ (r & 7))];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[b][n] = mfma16(cw, cx[h][n], acc[b][n]);
+      }
+    __builtin_amdgcn_wave_barrier();
+  }
+  f32x4(*sums)[2 * NB][64] = reinterpret_cast<f32x4(*)[2 * NB][64]>(lds);
+  __syncthreads();
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int n = 0; n < NB; ++n) sums[wave][b * NB + n][lane] = acc[b][n];
+  __syncthreads();
+  if (wave >= NB) return;
+  f32x4 z[2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) z[b] = sums[0][b * NB + wave][lane];
+#pragma unroll 1
+  for (int q = 1; q < WAVES; ++q)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) z[b] += sums[q][b * NB + wave][lane];
+  const int m = 16 * wave + r;
+  float mx = -INFINITY;
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int v = v0 + 16 * b + 4 * lg + q;
+      z[b][q] *= scale;
+      if (v >= V) continue;
+      if (m < Rp) zt[(long)v * Rp + m] = z[b][q];
+      mx = fmaxf(mx, z[b][q]);
+    }
+  mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+  mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+  const float mx2 = mx * LOG2E;
+  float sm = 0.f;
+  if (mx != -INFINITY) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (v0 + 16 * b + 4 * lg + q < V) sm += __builtin_amdgcn_exp2f(fmaf(z[b][q], LOG2E, -mx2));
+  }
+  sm += __shfl_xor(sm, 16, 64);
+  sm += __shfl_xor(sm, 32, 64);
+  if (lg == 0 && m < R) stats[(long)blockIdx.x * R + m] = make_float2(mx2, sm);
 }
 
 struct RowArgs {
@@ -193,13 +313,15 @@ __global__ void __launch_bounds__(256) k_distill_places(const int32_t *__restric
 
 struct DistillWs {
   size_t hb, wb, zt, stats, factor, place, dzt, total;
+  long zt_elems;
   int Rp, slabs;
 };
 
 DistillWs distill_ws(int rows, int hidden, int vocab, int k, seg_dtype dt, bool grad) {
   DistillWs w{};
   w.Rp = (rows + 31) / 32 * 32;
-  w.slabs = (vocab + 127) / 128;
+  const int slab = rows <= FEW ? FEW_SLAB : 128;
+  w.slabs = (vocab + slab - 1) / slab;
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t o = off;
@@ -209,7 +331,9 @@ DistillWs distill_ws(int rows, int hidden, int vocab, int k, seg_dtype dt, bool 
   const size_t Rp = w.Rp, H = hidden;
   w.hb = take(Rp * H * 2);
   w.wb = dt == SEG_F32 ? take((size_t)vocab * H * 2) : 0;
-  w.zt = take((size_t)vocab * Rp * 4);
+  // (zT later holds dH's partial sums: room for 16 parts of a small one)
+  w.zt_elems = std::max((long)(vocab * Rp), grad ? std::min(16 * (long)(rows * H), 4L << 20) : 0L);
+  w.zt = take((size_t)w.zt_elems * 4);
   w.stats = take((size_t)w.slabs * rows * sizeof(float2));
   if (grad) {
     w.factor = take(Rp * 4);
@@ -255,11 +379,23 @@ void distill_impl(const Distill &a, char *base, const DistillWs &L, hipStream_t 
     wb = w2 ? w2 : static_cast<const unsigned short *>(a.w);
   }
   {
-    EpiLogits<false> e{zt, Rp, stats, R, nullptr, nullptr, a.cfg.logit_scale, (long)V * Rp * 4 > (256L << 20)};
     ProfScope prof("logits", st);
-    gemm::Problems<EpiLogits<false>, 1, 1> g{{{wb}}, {{hb}}, {{H}}, {{H}}, {H}, {V}, {R}, {e}, {}, 1,
-                                             (H + gemm::BK - 1) / gemm::BK};
-    gemm::launch_tm<false, false, 4>(g, st);
+    const float scale = a.cfg.logit_scale;
+    if (R <= 16) {
+      k_logits_few<1, 8><<<L.slabs, 512, 0, st>>>(wb, hb, V, R, Rp, H, scale, zt, stats);
+      SEG_LAUNCH_CHECK();
+    } else if (R <= 32) {
+      k_logits_few<2, 8><<<L.slabs, 512, 0, st>>>(wb, hb, V, R, Rp, H, scale, zt, stats);
+      SEG_LAUNCH_CHECK();
+    } else if (R <= FEW) {
+      k_logits_few<4, 8><<<L.slabs, 512, 0, st>>>(wb, hb, V, R, Rp, H, scale, zt, stats);
+      SEG_LAUNCH_CHECK();
+    } else {
+      EpiLogits<false> e{zt, Rp, stats, R, nullptr, nullptr, scale, (long)V * Rp * 4 > (256L << 20)};
+      gemm::Problems<EpiLogits<false>, 1, 1> g{{{wb}}, {{hb}}, {{H}}, {{H}}, {H}, {V}, {R}, {e}, {}, 1,
+                                               (H + gemm::BK - 1) / gemm::BK};
+      gemm::launch_tm<false, false, 4>(g, st);
+    }
   }
   {
     ProfScope prof("distill", st);
@@ -292,7 +428,7 @@ void distill_impl(const Distill &a, char *base, const DistillWs &L, hipStream_t 
     // zT has served: its place holds partial sums when the vocabulary is cut
     gemm::launch_one<true, true>(dzt, Rp, wb, H, R, H, V,
                                  EpiOut<TO, ST>::make(static_cast<TO *>(a.dh), H, a.cfg.logit_scale),
-                                 gemm::Scratch{zt, (long)V * Rp}, 0, st);
+                                 gemm::Scratch{zt, L.zt_elems}, 0, st);
   }
   {
     ProfScope prof("dw", st);
