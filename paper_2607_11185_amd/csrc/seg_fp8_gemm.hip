@@ -566,16 +566,22 @@ void few_as(const Gemm8 &g, hipStream_t st) {
   SEG_LAUNCH_CHECK();
 }
 
+// Above 32 rows many of b's bytes are better read by tiles: 64 rows, this way / by tiles,
+// 4,096 x 4,096 9.9 / 15.0, 8,192 x 8,192 22.1 / 20.7, 3,584 x 18,944 33.3 / 22.9, 18,944 x
+// 3,584 24.6 / 21.6, 151,936 x 3,584 125 / 129.
+bool is_few(int rows, int outs, int cols) {
+  return rows <= FEW / 2 || (rows <= FEW && (double)outs * cols < (1 << 25));
+}
+
+struct Few {
+  int nb, cb, waves;
+};
 // Narrow blocks where there are few of them (each CU then has more waves on its rows of b),
 // wide ones, which read a less often, where there are many.  Measured, us, rows x outs x
 // cols, the kernel taken / another: 1 x 18,944 x 3,584 12.9 / 14.2 (16 waves), 16.7 (32 rows
 // of b a block, one step ahead); 1 x 3,584 x 18,944 13.2 / 15.5 (8 waves, two steps ahead); 24
 // x 18,944 x 3,584 17.1 / 20.4 (16 rows of b); 24 x 3,584 x 18,944 23.5 / 26.4 (32 rows); 64
-// x 18,944 x 3,584 25.4 / 26.1; 64 x 3,584 x 18,944 32.1 / 37.4; 64 x 5,504 x 2,048 7.6 / 10.0
-// (64 rows); 64 x 151,936 x 3,584 121 / 155 (32 rows).
-struct Few {
-  int nb, cb, waves;
-};
+// x 3,584 x 3,584 8.7 / 9.8 (32 rows); 64 x 5,504 x 2,048 7.6 / 10.0 (64 rows).
 Few few_choice(int rows, int outs, int cols) {
   if (rows <= 16) return {1, 1, outs <= 16 * 256 && cols > 16 * STEP ? 16 : 8};
   if (rows <= 32) return outs <= 32 * 128 ? Few{2, 1, 8} : Few{2, 2, 4};
@@ -620,7 +626,7 @@ using namespace seg;
 // How a product is launched (for tests): out = {Tiles, 0, parts of K}, or for few rows
 // {16-row blocks of a, of b, - waves}.
 extern "C" void seg_fp8_gemm_choice(int32_t rows, int32_t outs, int32_t cols, int32_t *out) {
-  if (rows <= FEW) {
+  if (is_few(rows, outs, cols)) {
     const Few f = few_choice(rows, outs, cols);
     out[0] = f.nb;
     out[1] = f.cb;
@@ -634,7 +640,7 @@ extern "C" void seg_fp8_gemm_choice(int32_t rows, int32_t outs, int32_t cols, in
 }
 
 extern "C" size_t seg_fp8_gemm_workspace_bytes(int32_t rows, int32_t outs, int32_t cols) {
-  if (!sizes_ok(rows, outs, cols) || rows <= FEW) return 0;
+  if (!sizes_ok(rows, outs, cols) || is_few(rows, outs, cols)) return 0;
   const Choice c = choice_of(rows, outs, cols);
   return c.parts > 1 ? align_up((size_t)c.parts * rows * ld_part(outs) * 4) : 0;
 }
@@ -664,7 +670,7 @@ extern "C" seg_status seg_fp8_gemm(int32_t rows, int32_t outs, int32_t cols, con
     };
     Gemm8 g{operand(a, rows), operand(b, outs), y, ldy, 0, (int)fp8::blocks_of(cols), (int)fp8::blocks_of(cols), 1, 0};
     ProfScope prof("fp8_gemm", stream);
-    if (rows <= FEW) {
+    if (is_few(rows, outs, cols)) {
       const Few f = few_choice(rows, outs, cols);
       if (dt == SEG_BF16) few<unsigned short>(g, f, stream);
       else few<float>(g, f, stream);

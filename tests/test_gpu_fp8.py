@@ -170,7 +170,7 @@ SHAPES = [(1, 1, 1), (1, 16, 128), (1, 300, 1000), (3, 33, 129), (16, 64, 256), 
           # each kernel for few rows, and each kind of tile
           (5, 4200, 2200), (9, 48, 2304), (20, 4200, 300), (25, 100, 1500), (40, 100, 1500), (50, 4200, 700), (47, 16500, 300),
           (300, 12000, 128), (400, 19000, 128), (65, 12000, 4096), (130, 5000, 16384), (130, 19000, 128), (65, 5504, 16384),
-          (700, 5504, 128), (1400, 1300, 16384), (257, 200, 17000)]
+          (700, 5504, 128), (1400, 1300, 16384), (257, 200, 17000), (40, 9000, 4000), (33, 3000, 12000)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
