@@ -310,3 +310,36 @@ def test_from_a_teacher_in_8_bits_to_the_student():
     # the teacher's logits are off by 2^-12 of their size (about 3): p by that
     assert rel(_np(out["loss_tok"]), ref["loss_tok"]) < 2.0 ** -8
     assert rel(_np(out["dh"]), ref["dh"]) < 2.0 ** -7 and rel(_np(out["dw"]), ref["dw"]) < 2.0 ** -7
+
+
+@pytest.mark.parametrize("rows", [3, 66])
+def test_largest_vocabulary(rows):
+    import torch
+    vocab, hidden, k = (1 << 20) - 256, 16, 256
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    h = torch.randn(rows, hidden, generator=gen, device="cuda").bfloat16()
+    w = torch.randn(vocab, hidden, generator=gen, device="cuda").bfloat16()
+    ids = (torch.arange(k, device="cuda") * 4095 + torch.arange(rows, device="cuda")[:, None]).int().contiguous()
+    ids[:, -1] = vocab - 1
+    logits = torch.randn(rows, k, generator=gen, device="cuda")
+    out = S.seg_distill_loss(h, None, w, ids, logits, S.DistillCfg(1.0, 1.0), dw_dtype=torch.bfloat16)
+    z = h.double() @ w.double().t()
+    p = torch.softmax(logits.double(), 1)
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    loss = (p * (p.log() - torch.gather(z, 1, ids.long()) + lse)).sum(1)
+    assert rel(_np(out["lse"]), _np(lse[:, 0])) < 2.0 ** -20 and rel(_np(out["loss_tok"]), _np(loss)) < 2.0 ** -18
+    dz = torch.exp(z - lse).scatter_add_(1, ids.long(), -p)
+    assert rel(_np(out["dh"]), _np(dz @ w.double())) < 2.0 ** -8
+    assert rel(_np(out["dw"]), _np(dz.t() @ h.double())) < 2.0 ** -8
+
+
+def test_weights_of_either_sign_and_scales_of_zero():
+    h, w, ids, logits, t_lse, weight = _inputs(30, 64, 200, 8)
+    weight[::3] *= -1
+    _check(h, w, ids, logits, t_lse, weight)
+    import torch
+    out = S.seg_distill_loss(h, None, w, ids, logits, S.DistillCfg(0.0, 0.0, 1.0), None, weight)
+    # both uniform: the student over the vocabulary, the teacher over its entries
+    want = weight * float(np.log(200 / 8))
+    assert bool((out["loss_tok"] - want).abs().max() < 1e-5)
+    assert not bool(out["dh"].any()) and not bool(out["dw"].any())

@@ -317,3 +317,31 @@ def test_packing_past_32_bits(block_rows):
     got = S.seg_fp8_unpack(a)
     assert torch.equal(got[first:], want) and bool(want[at - first:].any())
     assert float(got[7, 4099]) == 3.0 and int(got[:first].count_nonzero()) == 1
+
+
+@pytest.mark.parametrize("rows", [3, 200])
+def test_the_byte_that_stands_for_nan(rows):
+    """255 in an exponent array reads as NaN, and makes NaN of its block's rows and columns."""
+    import torch
+    a, b = _operands(rows, 150, 300)
+    want = S.seg_fp8_gemm(a, b)
+    a.exp[1, 2] = 255
+    b.exp[2, 1] = 255                                      # columns 128 to 149 of y
+    got = S.seg_fp8_gemm(a, b)
+    bad = torch.zeros_like(got, dtype=torch.bool)
+    bad[2], bad[:, 128:] = True, True
+    assert torch.equal(got.isnan(), bad) and torch.equal(got[~bad], want[~bad])
+    v = S.seg_fp8_unpack(a)
+    assert bool(v[2, 128:256].isnan().all()) and not bool(v[2, :128].isnan().any()) and not bool(v[0].isnan().any())
+
+
+@pytest.mark.parametrize("rows,outs,cols", [(1 << 20, 5, 16), (3, 1 << 20, 24), (66, (1 << 20) - 3, 16), (70, 9, 1 << 20)])
+def test_largest_sizes(rows, outs, cols):
+    """Against a product of the values in fp32, exact but for its order: codes of whole numbers."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    # whole numbers up to 4: products and sums of them are exact everywhere
+    x = torch.randint(-4, 5, (rows, cols), generator=gen, device="cuda").float()
+    w = torch.randint(-4, 5, (outs, cols), generator=gen, device="cuda").float()
+    got = S.seg_fp8_gemm(S.seg_fp8_pack(x), S.seg_fp8_pack(w, 128), torch.float32)
+    assert torch.equal(got, x @ w.t())
