@@ -208,6 +208,7 @@ __device__ __forceinline__ Cut threshold(K &&each, unsigned want, Pick &p) {
   hi = p.most;
   // as many numbers as threads are at least the smallest of the threads' largest
   if (want <= THREADS && p.own > 0) lo = p.own;
+  if (lo >= hi) __syncthreads();  // all have read these before another search of the block writes them
   while (lo < hi) {
     const int shift = max(0, 24 - (int)__builtin_clz(hi - lo));  // (hi - lo) >> shift is at most 255
     each([&](unsigned x) {

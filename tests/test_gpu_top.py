@@ -175,3 +175,15 @@ def test_no_rows():
     import torch
     got = S.seg_top_logits(torch.empty(0, 50, device="cuda"), 5)
     assert got["ids"].shape == (0, 5) and got["lse"].shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab,k", [(3000, 3000, 40), (1500, 9000, 200), (2500, 20000, 50), (40, 300000, 64), (40, 70000, 256)])
+def test_many_rows_of_one_value(rows, vocab, k, dtype):
+    """Two searches behind each other in every block, the first of which has nothing to cut."""
+    import torch
+    z = torch.arange(rows, device="cuda", dtype=torch.float32)[:, None].expand(rows, vocab).to(_dt(dtype)).contiguous()
+    first = torch.arange(k, device="cuda", dtype=torch.int32).expand(rows, k)
+    for _ in range(4):
+        got = S.seg_top_logits(z, k)
+        assert torch.equal(got["ids"], first) and torch.equal(got["logits"], z[:, :k].float())
