@@ -15,6 +15,12 @@ using gemm::ST;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 
+// A part of a softmax's sum as it is kept: NaN without a maximum gets one, so that it reaches
+// the whole.
+__device__ __forceinline__ float2 part_of(float mx2, float sm) {
+  return make_float2(sm != sm && mx2 == -INFINITY ? 0.f : mx2, sm);
+}
+
 // Epilogue of the logits GEMM (M = vocab, N = rows): writes zT, captures the
 // target logit (TARGET) and the per-(row, vocab tile) max / sum-exp partials.
 template <bool TARGET>
@@ -105,10 +111,17 @@ struct EpiLogits {
           for (int r = 0; r < 4; ++r)
             if (WHOLE || 16 * i + r < left)
               sm += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r] * scale, LOG2E, -mx2));
+      } else if constexpr (!TARGET) {  // -inf and NaN alone
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if ((WHOLE || 16 * i + r < left) && acc[i][j][r] != acc[i][j][r]) sm = acc[i][j][r];
       }
       sm += __shfl_xor(sm, 16, 64);
       sm += __shfl_xor(sm, 32, 64);
-      if (t.grp == 0 && nok) stats[(long)(slab_row / 128) * nrows + n] = make_float2(mx2, sm);
+      if (t.grp == 0 && nok)
+        stats[(long)(slab_row / 128) * nrows + n] = TARGET ? make_float2(mx2, sm) : part_of(mx2, sm);
       if constexpr (TARGET) {
         const int at = (nok ? target[n] : -1) - base;  // the target as a k of the lane
         const bool mine = at >= 0 && at < min(116, left) && !(at & 12);

@@ -165,10 +165,16 @@ __global__ void __launch_bounds__(64 * WAVES, NB < 4 ? 4 : 2) k_logits_few(const
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         if (v0 + 16 * b + 4 * lg + q < V) sm += __builtin_amdgcn_exp2f(fmaf(z[b][q], LOG2E, -mx2));
+  } else {  // -inf and NaN alone
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (v0 + 16 * b + 4 * lg + q < V && z[b][q] != z[b][q]) sm = z[b][q];
   }
   sm += __shfl_xor(sm, 16, 64);
   sm += __shfl_xor(sm, 32, 64);
-  if (lg == 0 && m < R) stats[(long)blockIdx.x * R + m] = make_float2(mx2, sm);
+  if (lg == 0 && m < R) stats[(long)blockIdx.x * R + m] = part_of(mx2, sm);
 }
 
 struct RowArgs {

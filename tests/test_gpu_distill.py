@@ -343,3 +343,17 @@ def test_weights_of_either_sign_and_scales_of_zero():
     want = weight * float(np.log(200 / 8))
     assert bool((out["loss_tok"] - want).abs().max() < 1e-5)
     assert not bool(out["dh"].any()) and not bool(out["dw"].any())
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("rows", [9, 30, 60, 150])
+def test_weights_of_nan_reach_every_row(rows, grad):
+    """128 rows of the vocabulary, a whole part of the softmax's statistics, and a column of one."""
+    for spoilt in (slice(128, 256), slice(290, 291)):
+        h, w, ids, logits, t_lse, weight = _inputs(rows, 64, 400, 8)
+        w[spoilt] = float("nan")
+        ids %= 128
+        weight[1] = 0
+        out = S.seg_distill_loss(h, None, w, ids, logits, S.DistillCfg(1.0, 1.0, 1.0, grad), t_lse, weight)
+        assert bool(out["lse"].isnan().all()) and bool(out["loss_sum"].isnan())
+        assert not bool(out["loss_tok"][1].any()) and int(out["loss_tok"].isnan().sum()) == rows - 1
