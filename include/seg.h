@@ -608,9 +608,10 @@ seg_status seg_top_logits(int32_t rows, int32_t vocab, int32_t k, seg_dtype dt, 
  * A row with weight 0 or no probability at any entry has loss 0 and no gradient, whatever
  * h, ids and logits hold there; an id of vocab or more makes its row NaN; the same id more than
  * once counts as often as it is there.
- * Outputs: loss_tok, lse [rows] fp32 (log sum exp z); loss_sum [1] fp32; with want_grad dh
- * [rows, hidden] (dtype dt) and dw [vocab, hidden] (dtype dw_dt), overwritten.  dz is
- * rounded to bf16 (2^-8) for the products, as in seg_logprob_loss.
+ * Outputs: loss_tok, lse [rows] fp32 (log sum exp z: -inf where all logits are -inf, NaN where
+ * one is NaN or +inf; sizes from 2^128 / log2(e) = 2.36e38 on count as infinite); loss_sum [1]
+ * fp32; with want_grad dh [rows, hidden] (dtype dt) and dw [vocab, hidden] (dtype dw_dt),
+ * overwritten.  dz is rounded to bf16 (2^-8) for the products, as in seg_logprob_loss.
  * hidden a multiple of 8, k <= 256 (SEG_ERR_UNSUPPORTED), all sizes below 2^20 - 256; a
  * bf16 w and the workspace on 16-byte boundaries; outputs and workspace overlap neither
  * an input nor each other (SEG_ERR_ARG).

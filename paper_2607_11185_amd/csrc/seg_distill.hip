@@ -230,8 +230,8 @@ __global__ void __launch_bounds__(256) k_distill_rows(const RowArgs a) {
     __syncthreads();
     if (part == 0) {
       for (int k = ROWS == 4 ? 16 : 1; k < SL; k += ROWS == 4 ? 16 : 1) s = meet(s, red[k][t]);
-      // (no sum: every logit of the row is NaN)
-      lse_of[t] = s.y == 0.f ? __builtin_nanf("") : (s.x + log2f(s.y)) * LN2;
+      // (no part with a sum: every logit of the row is -inf, and so is this)
+      lse_of[t] = (s.x + log2f(s.y)) * LN2;
     }
     __syncthreads();
   }

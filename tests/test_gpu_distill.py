@@ -357,3 +357,23 @@ def test_weights_of_nan_reach_every_row(rows, grad):
         out = S.seg_distill_loss(h, None, w, ids, logits, S.DistillCfg(1.0, 1.0, 1.0, grad), t_lse, weight)
         assert bool(out["lse"].isnan().all()) and bool(out["loss_sum"].isnan())
         assert not bool(out["loss_tok"][1].any()) and int(out["loss_tok"].isnan().sum()) == rows - 1
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("rows", [9, 30, 60, 150, 4100])
+def test_rows_of_minus_infinity(rows, grad):
+    """Every logit of a row is -inf: so is its log-sum-exp, as that of seg_top_logits; one
+    of +inf or NaN makes it NaN.  Rows without weight stay out of all else."""
+    import torch
+    inf = float("inf")
+    h, w, ids, logits, t_lse, weight = _inputs(rows, 64, 400, 8)
+    h[:, 0], w[:, 0] = 1.0, -inf
+    weight[::2] = 0
+    cfg = S.DistillCfg(1.0, 1.0, 1.0, grad)
+    out = S.seg_distill_loss(h, None, w, ids, logits, cfg, t_lse, weight)
+    assert bool((out["lse"] == -inf).all())
+    assert torch.equal(out["lse"], S.seg_top_logits(torch.full((rows, 400), -inf, device="cuda"), 1)["lse"])
+    assert not bool(out["loss_tok"][::2].any()) and bool(out["loss_tok"][1::2].isnan().all())
+    w[301, 0] = inf
+    out = S.seg_distill_loss(h, None, w, ids, logits, cfg, t_lse, weight)
+    assert bool(out["lse"].isnan().all()) and not bool(out["loss_tok"][::2].any())
