@@ -607,7 +607,8 @@ seg_status seg_top_logits(int32_t rows, int32_t vocab, int32_t k, seg_dtype dt, 
  *   t_lse, row_weight [rows] fp32, or NULL (row_weight: 1).
  * A row with weight 0 or no probability at any entry has loss 0 and no gradient, whatever
  * h, ids and logits hold there; an id of vocab or more makes its row NaN; the same id more than
- * once counts as often as it is there.
+ * once counts as often as it is there.  What makes a row NaN reaches loss_tok and dh of that
+ * row alone, but loss_sum and all of dw, which sum over the rows.
  * Outputs: loss_tok, lse [rows] fp32 (log sum exp z: -inf where all logits are -inf, NaN where
  * one is NaN or +inf; sizes from 2^128 / log2(e) = 2.36e38 on count as infinite); loss_sum [1]
  * fp32; with want_grad dh [rows, hidden] (dtype dt) and dw [vocab, hidden] (dtype dw_dt),

@@ -377,3 +377,23 @@ def test_rows_of_minus_infinity(rows, grad):
     w[301, 0] = inf
     out = S.seg_distill_loss(h, None, w, ids, logits, cfg, t_lse, weight)
     assert bool(out["lse"].isnan().all()) and not bool(out["loss_tok"][::2].any())
+
+
+@pytest.mark.parametrize("rows", [40, 100])
+@pytest.mark.parametrize("what", ["id", "index", "logit", "h"])
+def test_a_bad_row_reaches_the_sums(what, rows):
+    """NaN in loss_tok and dh of one row; in loss_sum and all of dw, which sum over rows."""
+    import torch
+    h, w, ids, logits, t_lse, weight = _inputs(rows, 128, 300, 10)
+    index = torch.arange(rows, device="cuda", dtype=torch.int32)
+    if what == "id":
+        ids[3, 2] = 300
+    elif what == "index":
+        index[3] = rows
+    else:
+        (logits if what == "logit" else h)[3, 1] = float("nan")
+    out = S.seg_distill_loss(h, index, w, ids, logits, S.DistillCfg(LS, TS), t_lse, weight)
+    bad = torch.arange(rows, device="cuda") == 3
+    assert torch.equal(out["loss_tok"].isnan(), bad) and torch.equal(out["dh"].isnan().all(1), bad)
+    assert torch.equal(out["dh"].isnan().any(1), bad)
+    assert bool(out["loss_sum"].isnan()) and bool(out["dw"].isnan().all())
