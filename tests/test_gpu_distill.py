@@ -397,3 +397,48 @@ def test_a_bad_row_reaches_the_sums(what, rows):
     assert torch.equal(out["loss_tok"].isnan(), bad) and torch.equal(out["dh"].isnan().all(1), bad)
     assert torch.equal(out["dh"].isnan().any(1), bad)
     assert bool(out["loss_sum"].isnan()) and bool(out["dw"].isnan().all())
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("k", [5, 200])
+def test_thousands_of_rows(k, given):
+    """Sixteen rows a block, every one with weight but for a few: missing and repeated
+    entries, and rows without weight or entries beside others."""
+    import torch
+    h, w, ids, logits, t_lse, weight = _inputs(4111, 64, 1003, k, given=given)
+    r = torch.arange(4111, device="cuda")
+    ids[r % 5 == 1, k // 2:] = -1
+    ids[r % 7 == 2, 1] = ids[r % 7 == 2, 0]
+    ids[r % 11 == 3, k - 1], ids[r % 11 == 3, 2] = ids[r % 11 == 3, 1], ids[r % 11 == 3, 1]
+    logits[r % 13 == 4, 0] = -float("inf")
+    none = (r % 17 == 5) | (r == 4110)
+    weight[none] = 0
+    empty = r % 19 == 6
+    ids[empty] = -3
+    out, _ = _check(h, w, ids, logits, t_lse, weight)
+    none |= empty
+    assert not bool(out["loss_tok"][none].any()) and not bool(out["dh"][none].any())
+    assert bool(out["dh"][~none].any(1).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [33, 200])
+def test_tensors_off_16_byte_boundaries(rows, dtype):
+    """One element into their storage (w in fp32 alone, as the header asks): the same bits."""
+    import torch
+
+    def off(t):
+        flat = torch.full((t.numel() + 1,), 9.0, dtype=t.dtype, device="cuda")
+        flat[1:] = t.reshape(-1)
+        return flat[1:].view(t.shape)
+
+    h, w, ids, logits, t_lse, weight = _inputs(rows, 72, 301, 6, dtype=dtype)
+    cfg = S.DistillCfg(LS, TS, 0.5, True)
+    for dw in ("bf16", "f32"):
+        want = S.seg_distill_loss(h, None, w, ids, logits, cfg, t_lse, weight, dw_dtype=_dt(dw))
+        out = {n: off(t) for n, t in want.items()}
+        for t in out.values():
+            t.fill_(5.0)
+        S.seg_distill_loss(off(h), None, off(w) if dtype == "f32" else w, off(ids), off(logits), cfg, t_lse, off(weight), out=out)
+        for n, t in want.items():
+            assert torch.equal(out[n], t), (n, dw)

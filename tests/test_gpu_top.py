@@ -187,3 +187,42 @@ def test_many_rows_of_one_value(rows, vocab, k, dtype):
     for _ in range(4):
         got = S.seg_top_logits(z, k)
         assert torch.equal(got["ids"], first) and torch.equal(got["logits"], z[:, :k].float())
+
+
+@pytest.mark.parametrize("scale", [1.0, -0.7])
+@pytest.mark.parametrize("k", [64, 256])
+@pytest.mark.parametrize("rows,vocab,wide,dtype", [(1700, 32003, 32003, "bf16"), (1700, 32003, 32010, "bf16"), (800, 33001, 33001, "f32"),
+                                                   (530, 151933, 151936, "bf16")])
+def test_logits_past_the_caches(rows, vocab, wide, dtype, k, scale):
+    """More than 96 MB, read past the caches: columns, values and log-sum-exp against torch in
+    64 bits (a stable sort has ties in the order of their columns)."""
+    import torch
+    z = _z(rows, wide, dtype)[:, :vocab]
+    z[3, 17], z[4, 5:], z[5, vocab - 1] = -float("inf"), -float("inf"), 30.0
+    z[7, 9], z[8] = float("nan"), -float("inf")
+    got = S.seg_top_logits(z, k, scale)
+    for at in range(0, rows, 200):
+        part = z[at:at + 200].double()
+        # (NaN sorts as the largest; -0 as 0)
+        value, column = torch.sort(part + 0.0, dim=1, descending=True, stable=True)
+        assert torch.equal(got["ids"][at:at + 200], column[:, :k].int())
+        assert torch.equal(got["logits"][at:at + 200].double().nan_to_num(7.0, 8.0, 9.0), value[:, :k].nan_to_num(7.0, 8.0, 9.0))
+        y = part * float(np.float32(scale))
+        want, lse = torch.logsumexp(y, 1), got["lse"][at:at + 200].double()
+        fine = want.isfinite()
+        assert torch.equal(fine, lse.isfinite())
+        assert torch.equal(want[~fine].nan_to_num(7.0, 8.0, 9.0), lse[~fine].nan_to_num(7.0, 8.0, 9.0))
+        tol = ((4 * np.log(vocab) + 8) + torch.where(y.isfinite(), y, 0).abs().amax(1) + vocab / 128 + 200) * 2.0 ** -24 + 2.0 ** -24 * want.abs()
+        assert bool(((want - lse).abs() <= tol)[fine].all())
+
+
+def test_sums_past_32_bits():
+    """Rows of one value each, behind 2^31 elements: its log-sum-exp is value + log(vocab)."""
+    import torch
+    rows, vocab = 15000, 151936
+    value = (torch.arange(rows, device="cuda") % 9 - 4).bfloat16()
+    got = S.seg_top_logits(value[:, None].expand(rows, vocab).contiguous(), 2, 0.5)
+    want = value.double() * 0.5 + float(np.log(vocab))
+    tol = ((4 * np.log(vocab) + 8) + 2 + vocab / 128 + 200) * 2.0 ** -24 + 2.0 ** -24 * want.abs()
+    assert bool(((got["lse"].double() - want).abs() <= tol).all())
+    assert torch.equal(got["logits"], value[:, None].float().expand(rows, 2))
