@@ -208,8 +208,11 @@ struct Grid {
   }
 };
 
-// What both entry points check; false where there is nothing to do.
-bool pack_args(int64_t rows, int32_t cols, seg_dtype dt, const void *x, int64_t ldx, const seg_fp8 *p,
+// Thread blocks of a launch: 2^31 threads (a launch may have 2^32 - 1).
+constexpr double MAX_BLOCKS = 1 << 23;
+
+// What both entry points check (packing: x is read); false where there is nothing to do.
+bool pack_args(int64_t rows, int32_t cols, seg_dtype dt, const void *x, int64_t ldx, const seg_fp8 *p, bool packing,
                PackArgs &a) {
   SEG_CHECK(dt == SEG_BF16 || dt == SEG_F32, SEG_ERR_UNSUPPORTED, "dtype %d not supported", (int)dt);
   SEG_CHECK(rows >= 0 && cols >= 1, SEG_ERR_ARG, "rows %lld or cols %d out of range", (long long)rows, cols);
@@ -223,8 +226,10 @@ bool pack_args(int64_t rows, int32_t cols, seg_dtype dt, const void *x, int64_t 
   SEG_CHECK(x, SEG_ERR_ARG, "x is NULL");
   fp8::check(p, "8 bits");
   SEG_CHECK(reinterpret_cast<uintptr_t>(x) % (dt == SEG_BF16 ? 2 : 4) == 0, SEG_ERR_ARG, "x is not aligned to its type");
-  // (blocks of 128 rows take fewer thread blocks)
-  SEG_CHECK(Grid(rows, cols).blocks <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "tensor too large for one launch");
+  // (packing of 128 x 128 blocks has a grid of its own: of few rows it is up to four times as large)
+  const double blocks = packing && p->block_rows != 1 ? (double)fp8::blocks_of(rows) * fp8::blocks_of(cols)
+                                                      : Grid(rows, cols).blocks;
+  SEG_CHECK(blocks <= MAX_BLOCKS, SEG_ERR_CAPACITY, "tensor too large for one launch");
   a = PackArgs{const_cast<void *>(x), ldx, p->code, p->exp, rows, fp8::ld_code(cols), fp8::ld_exp(rows, p->block_rows),
                cols, 0};
   return true;
@@ -265,7 +270,7 @@ extern "C" seg_status seg_fp8_pack(int64_t rows, int32_t cols, seg_dtype dt, con
                                    const seg_fp8 *out, hipStream_t stream) {
   return guarded([&] {
     PackArgs a{};
-    if (!pack_args(rows, cols, dt, x, ldx, out, a)) return;
+    if (!pack_args(rows, cols, dt, x, ldx, out, true, a)) return;
     const Memory m = memory_of(a, out->block_rows, dt);
     check_apart({m.code, m.exp}, {m.x});
     ProfScope prof("fp8_pack", stream);
@@ -291,7 +296,7 @@ extern "C" seg_status seg_fp8_unpack(int64_t rows, int32_t cols, seg_dtype dt, c
                                      int64_t ldx, hipStream_t stream) {
   return guarded([&] {
     PackArgs a{};
-    if (!pack_args(rows, cols, dt, x, ldx, in, a)) return;
+    if (!pack_args(rows, cols, dt, x, ldx, in, false, a)) return;
     const Memory m = memory_of(a, in->block_rows, dt);
     check_apart({m.x}, {m.code, m.exp});
     const int shift = in->block_rows == 1 ? 0 : 7;

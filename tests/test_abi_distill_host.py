@@ -170,3 +170,16 @@ def test_distillation_binding_refuses():
                 dict(t_lse=torch.zeros(3)), dict(row_weight=torch.zeros(4, 1)), dict(dw_dtype=torch.float16), dict()):
         with pytest.raises((AssertionError, TypeError)):
             S.seg_distill_loss(**{**good, **bad})
+
+
+@pytest.mark.parametrize("rows,cols,block_rows,pack,unpack", [
+    # 2^23 thread blocks of 16 rows, and one more; overlapping arrays are refused behind the size
+    (1 << 27, 1, 1, ARG, ARG), ((1 << 27) + 1, 1, 1, CAP, CAP),
+    # of 128 rows: their own grid when they are packed
+    (1, 1 << 30, 128, ARG, ARG), (128, 1 << 30, 128, ARG, CAP), (129, 1 << 30, 128, CAP, CAP), (1 << 30, 1, 128, ARG, CAP),
+    ((1 << 30) + 1, 1, 128, CAP, CAP)])
+def test_packing_is_bounded_by_its_own_grid(rows, cols, block_rows, pack, unpack):
+    L = _lib_or_skip()
+    s = _lib.SegFp8(256, 1 << 50, block_rows)
+    assert L.seg_fp8_pack(rows, cols, 0, 256, cols, ctypes.byref(s), None) == pack
+    assert L.seg_fp8_unpack(rows, cols, 0, ctypes.byref(s), 256, cols, None) == unpack

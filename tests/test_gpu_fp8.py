@@ -345,3 +345,31 @@ def test_largest_sizes(rows, outs, cols):
     w = torch.randint(-4, 5, (outs, cols), generator=gen, device="cuda").float()
     got = S.seg_fp8_gemm(S.seg_fp8_pack(x), S.seg_fp8_pack(w, 128), torch.float32)
     assert torch.equal(got, x @ w.t())
+
+
+@pytest.mark.parametrize("rows,cols,block_rows", [(1 << 27, 1, 1), ((1 << 28) + 5, 1, 128)])
+def test_largest_launches(rows, cols, block_rows):
+    """Of 2^23 thread blocks, and more rows in blocks of 128 than of one: parts packed alone."""
+    import torch
+    x = torch.randn(rows, cols, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda", dtype=torch.bfloat16)
+    a = S.seg_fp8_pack(x, block_rows)
+    for at in (0, rows // 256 * 128, rows // 128 * 128 - 4096):
+        to = min(rows, at + 100000)
+        part = S.seg_fp8_pack(x[at:to], block_rows)
+        n, first = -(-(to - at) // block_rows), at // block_rows
+        assert torch.equal(a.code[at:to], part.code) and torch.equal(a.exp[:, first:first + n], part.exp[:, :n])
+    if block_rows == 1:
+        got = S.seg_fp8_unpack(a)
+        for at in (0, rows // 256 * 128, rows - 100000):
+            assert torch.equal(got[at:at + 100000], S.seg_fp8_unpack(S.seg_fp8_pack(x[at:at + 100000])))
+
+
+def test_widest_row():
+    """2^30 columns: a block of 128 rows that holds one is the block of that row."""
+    import torch
+    x = torch.randn(1, 1 << 30, generator=torch.Generator(device="cuda").manual_seed(4), device="cuda", dtype=torch.bfloat16)
+    x[0, -128:] *= 1000
+    a, b = S.seg_fp8_pack(x), S.seg_fp8_pack(x, 128)
+    assert torch.equal(a.code, b.code) and torch.equal(a.exp, b.exp)
+    part = S.seg_fp8_pack(x[:, -1280:], 128)
+    assert torch.equal(part.code, b.code[:, -1280:]) and torch.equal(part.exp, b.exp[-10:])
