@@ -373,3 +373,19 @@ def test_widest_row():
     assert torch.equal(a.code, b.code) and torch.equal(a.exp, b.exp)
     part = S.seg_fp8_pack(x[:, -1280:], 128)
     assert torch.equal(part.code, b.code[:, -1280:]) and torch.equal(part.exp, b.exp[-10:])
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("rows,cols,dtype", [(9000, 4099, BF), (5133, 4099, F32)])
+def test_tensors_past_the_caches(rows, cols, dtype, block_rows):
+    """More than 96 MB in and out, read and written past the caches: as their parts alone."""
+    import torch
+    x = torch.randn(rows, cols, generator=torch.Generator(device="cuda").manual_seed(rows), device="cuda").to(_dt(dtype))
+    a = S.seg_fp8_pack(x, block_rows)
+    got = S.seg_fp8_unpack(a, x.dtype)
+    for at in range(0, rows, 1024):
+        part = S.seg_fp8_pack(x[at:at + 1024], block_rows)
+        n = -(-part.shape[0] // block_rows)
+        assert torch.equal(a.code[at:at + 1024], part.code)
+        assert torch.equal(a.exp[:, at // block_rows:at // block_rows + n], part.exp[:, :n])
+        assert torch.equal(got[at:at + 1024], S.seg_fp8_unpack(part, x.dtype))
