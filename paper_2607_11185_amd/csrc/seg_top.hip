@@ -534,7 +534,8 @@ extern "C" seg_status seg_top_logits(int32_t rows, int32_t vocab, int32_t k, seg
     const size_t e = dt == SEG_BF16 ? 2 : 4;
     SEG_CHECK(reinterpret_cast<uintptr_t>(z) % e == 0, SEG_ERR_ARG, "z is not aligned to its type");
     SEG_CHECK(w.total == 0 || reinterpret_cast<uintptr_t>(ws) % 16 == 0, SEG_ERR_UNSUPPORTED, "the workspace is not on a 16-byte boundary");
-    SEG_CHECK((double)rows * w.parts <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "too many rows for one launch");
+    // (the way by parts alone launches more than a block a row)
+    SEG_CHECK(w.total == 0 || (double)rows * w.parts <= 0x7fffffffL / 256, SEG_ERR_CAPACITY, "too many rows for one launch");
     check_apart({{ids, (size_t)rows * k * 4}, {logits, (size_t)rows * k * 4}, {lse, (size_t)rows * 4},
                  {w.total ? ws : nullptr, w.total}},
                 {{z, ((size_t)(rows - 1) * ldz + vocab) * e}});

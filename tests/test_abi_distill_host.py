@@ -183,3 +183,11 @@ def test_packing_is_bounded_by_its_own_grid(rows, cols, block_rows, pack, unpack
     s = _lib.SegFp8(256, 1 << 50, block_rows)
     assert L.seg_fp8_pack(rows, cols, 0, 256, cols, ctypes.byref(s), None) == pack
     assert L.seg_fp8_unpack(rows, cols, 0, ctypes.byref(s), 256, cols, None) == unpack
+
+
+@pytest.mark.parametrize("rows,vocab,want", [(1 << 20, 131072, ARG), (1 << 20, 262144, ARG), (1 << 20, 262145, CAP), (1 << 18, 524289, CAP),
+                                             ((1 << 18) - 1, 524288, ARG)])
+def test_top_logits_are_bounded_by_what_is_launched(rows, vocab, want):
+    """Parts of 16,384 columns a block, 2^23 - 1 of them, unless a block takes a row; an output
+    on the logits is refused behind that."""
+    assert _top(rows=rows, vocab=vocab, ldz=vocab, z=1 << 30, ids=1 << 31, ws=1 << 60, logits=1 << 61, lse=1 << 59, ws_bytes=1 << 50) == want
