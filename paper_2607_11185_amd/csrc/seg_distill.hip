@@ -317,6 +317,11 @@ __global__ void __launch_bounds__(256) k_distill_places(const int32_t *__restric
   }
 }
 
+// dw of no rows, of 2-byte elements at any alignment of theirs.
+__global__ void __launch_bounds__(256) k_zero16(unsigned short *__restrict__ d, long n) {
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) d[i] = 0;
+}
+
 struct DistillWs {
   size_t hb, wb, zt, stats, factor, place, dzt, total;
   long zt_elems;
@@ -491,9 +496,16 @@ extern "C" seg_status seg_distill_loss(int32_t rows, int32_t hidden, int32_t voc
     const size_t e = dt == SEG_BF16 ? 2 : 4, ew = dw_dt == SEG_BF16 ? 2 : 4, H = hidden, R = rows;
     if (rows == 0) {
       SEG_CHECK(!grad || dw, SEG_ERR_ARG, "dw is NULL with want_grad");
-      SEG_CHECK(!grad || reinterpret_cast<uintptr_t>(dw) % 4 == 0, SEG_ERR_UNSUPPORTED, "dw is not on a 4-byte boundary");
+      SEG_CHECK(!grad || reinterpret_cast<uintptr_t>(dw) % ew == 0, SEG_ERR_ARG, "dw is not aligned to its type");
       fill32(loss_sum, 1, 0u, stream);
-      if (grad) fill32(dw, (long)(vocab * H * ew / 4), 0u, stream);
+      if (!grad) return;
+      if (reinterpret_cast<uintptr_t>(dw) % 4 == 0) {
+        fill32(dw, (long)(vocab * H * ew / 4), 0u, stream);
+      } else {
+        const long n = (long)(vocab * H);
+        k_zero16<<<(unsigned)std::min<long>(16384, (n + 255) / 256), 256, 0, stream>>>(static_cast<unsigned short *>(dw), n);
+        SEG_LAUNCH_CHECK();
+      }
       return;
     }
     SEG_CHECK(h && w && ids && logits && loss_tok && lse && ws, SEG_ERR_ARG, "a tensor pointer is NULL");

@@ -442,3 +442,18 @@ def test_tensors_off_16_byte_boundaries(rows, dtype):
         S.seg_distill_loss(off(h), None, off(w) if dtype == "f32" else w, off(ids), off(logits), cfg, t_lse, off(weight), out=out)
         for n, t in want.items():
             assert torch.equal(out[n], t), (n, dw)
+
+
+@pytest.mark.parametrize("dw", ["bf16", "f32"])
+def test_no_rows_into_any_element_of_a_buffer(dw):
+    """dw one element into its storage, as calls with rows take it; nothing beside it is written."""
+    import torch
+    e = torch.empty
+    w = torch.randn(50, 64, device="cuda").bfloat16()
+    flat = torch.full((1 + 50 * 64 + 5,), 9.0, dtype=_dt(dw), device="cuda")
+    out = {"loss_tok": e(0, device="cuda"), "lse": e(0, device="cuda"), "loss_sum": e(1, device="cuda"),
+           "dh": e(0, 64, device="cuda").bfloat16(), "dw": flat[1:1 + 50 * 64].view(50, 64)}
+    S.seg_distill_loss(e(0, 64, device="cuda").bfloat16(), None, w, e(0, 4, dtype=torch.int32, device="cuda"), e(0, 4, device="cuda"),
+                       S.DistillCfg(), out=out)
+    assert float(out["loss_sum"]) == 0 and not bool(out["dw"].any())
+    assert float(flat[0]) == 9 and bool((flat[1 + 50 * 64:] == 9).all())
