@@ -510,8 +510,8 @@ extern "C" seg_status seg_distill_loss(int32_t rows, int32_t hidden, int32_t voc
     }
     SEG_CHECK(h && w && ids && logits && loss_tok && lse && ws, SEG_ERR_ARG, "a tensor pointer is NULL");
     SEG_CHECK(!grad || (dh && dw), SEG_ERR_ARG, "dh or dw is NULL with want_grad");
-    SEG_CHECK(reinterpret_cast<uintptr_t>(h) % e == 0 && reinterpret_cast<uintptr_t>(dh) % e == 0 &&
-                  reinterpret_cast<uintptr_t>(dw) % ew == 0,
+    SEG_CHECK(reinterpret_cast<uintptr_t>(h) % e == 0 &&
+                  (!grad || (reinterpret_cast<uintptr_t>(dh) % e == 0 && reinterpret_cast<uintptr_t>(dw) % ew == 0)),
               SEG_ERR_ARG, "h, dh or dw is not aligned to its type");
     SEG_CHECK(reinterpret_cast<uintptr_t>(w) % (dt == SEG_BF16 ? 16 : 4) == 0 && reinterpret_cast<uintptr_t>(ws) % 16 == 0,
               SEG_ERR_UNSUPPORTED, "w or the workspace is not on a 16-byte boundary");

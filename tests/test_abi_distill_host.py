@@ -191,3 +191,10 @@ def test_top_logits_are_bounded_by_what_is_launched(rows, vocab, want):
     """Parts of 16,384 columns a block, 2^23 - 1 of them, unless a block takes a row; an output
     on the logits is refused behind that."""
     assert _top(rows=rows, vocab=vocab, ldz=vocab, z=1 << 30, ids=1 << 31, ws=1 << 60, logits=1 << 61, lse=1 << 59, ws_bytes=1 << 50) == want
+
+
+def test_forward_alone_does_not_look_at_gradients():
+    """Misaligned dh and dw go unnoticed without want_grad (w's own check is behind theirs)."""
+    kw = dict(dh=8 * MB + 1, dw=9 * MB + 2, dw_dt=1, w=2 * MB + 8)
+    assert _distill(cfg=(1.0, 1.0, 1.0, 0), **kw) == UNS
+    assert _distill(**kw) == ARG
