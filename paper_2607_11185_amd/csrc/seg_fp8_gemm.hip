@@ -527,8 +527,8 @@ long tiles_of(int rows, int outs, Tiles v) {
 //   1,024 x 5,504 x 2,048    128 x 128 20.0; 25.7 / 20.3 / - / 25.6
 //   1,500 x 5,001 x 2,040    128 x 256 22.9; 29.0 / - / 23.5 / 28.4
 //   1,500 x 18,944 x 3,584   256 x 256 97.4; - / 128 / 128 / 140
-// (8,192 x 18,944 x 3,584 in two launches, nine rounds and the rest in quarters of tiles:
-// 478, in one 470.)
+// (The wait at the end of the loop came later: it adds 0.2 to 0.6 us to each but DEEP.  8,192 x
+// 18,944 x 3,584 in two launches, nine rounds and the rest in quarters of tiles: 478, in one 470.)
 double expect(int v, long blocks, double s) {
   const long slots = v == TWO ? 512 : 256, full = blocks / slots, rest = blocks % slots;
   auto round = [&](double n) {  // n blocks, at most the slots
@@ -568,9 +568,11 @@ void few_as(const Gemm8 &g, hipStream_t st) {
   SEG_LAUNCH_CHECK();
 }
 
-// Above 32 rows many of b's bytes are better read by tiles: 64 rows, this way / by tiles,
-// 4,096 x 4,096 9.9 / 15.0, 8,192 x 8,192 22.1 / 20.7, 3,584 x 18,944 33.3 / 22.9, 18,944 x
-// 3,584 24.6 / 21.6, 151,936 x 3,584 125 / 129.
+// Above 32 rows many of b's bytes are better read by tiles, or as well: us, rows x outs x
+// cols, this way / by tiles, 64 x 4,096 x 4,096 9.5 / 15.0; 64 x 8,192 x 8,192 19.7 / 19.5; 64 x
+// 3,584 x 18,944 31.9 / 21.3; 64 x 18,944 x 3,584 23.8 / 19.0, 40 rows 22.3 / 18.7; the rule loses
+// a little only where there are very many outs: 64 x 151,936 x 3,584 121.1 / 122.5, 48 rows
+// 113 / 119.
 bool is_few(int rows, int outs, int cols) {
   return rows <= FEW / 2 || (rows <= FEW && (double)outs * cols < (1 << 25));
 }
