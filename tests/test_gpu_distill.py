@@ -457,3 +457,24 @@ def test_no_rows_into_any_element_of_a_buffer(dw):
                        S.DistillCfg(), out=out)
     assert float(out["loss_sum"]) == 0 and not bool(out["dw"].any())
     assert float(flat[0]) == 9 and bool((flat[1 + 50 * 64:] == 9).all())
+
+
+@pytest.mark.parametrize("rows", [9, 40, 150])
+def test_logits_near_the_end_of_fp32(rows):
+    """Sizes from 2^128 / log2(e) on count as infinite: below it they add nothing, above they are NaN."""
+    import torch
+    h, w, ids, logits, t_lse, weight = _inputs(rows, 64, 400, 8)
+    cfg = S.DistillCfg(1.0, 1.0, 1.0, False)
+    h[:, 0], w[:, 0] = 2.0 ** 64, 0.0
+    want = torch.logsumexp(h.double() @ w[:140].double().t(), 1)
+    w[140:, 0] = -1.36e19                                 # logits of -2.5e38, a whole part of the sums among them
+    out = S.seg_distill_loss(h, None, w, ids % 140, logits, cfg, t_lse, weight)
+    # fp32 sums of 64 products of about 0.25 each, and exponentials and sums as elsewhere
+    assert bool(((out["lse"].double() - want).abs() <= 66 * 2.0 ** -24 * 64 + 40 * 2.0 ** -22).all())
+    assert bool(out["loss_tok"].isfinite().all())
+    w[:, 0] = -1.36e19
+    out = S.seg_distill_loss(h, None, w, ids, logits, cfg, t_lse, weight)
+    assert bool((out["lse"] == -float("inf")).all())
+    w[5, 0] = 1.36e19
+    out = S.seg_distill_loss(h, None, w, ids, logits, cfg, t_lse, weight)
+    assert bool(out["lse"].isnan().all())
